@@ -340,6 +340,116 @@ int la_recurrent_steps(const void *q, const void *k, const void *v, float *S, fl
                        int T, int B, int H, int D, int M, float eps, la_dtype t, void *stream);
 
 /*
+ * ---- The layer around the attention --------------------------------------------------------
+ * A residual layer of eq. 1 is T(x) = f(A(x) + x).  The entry points below are what such a layer
+ * runs next to the attention: the residual sum and the layer norm behind it (la_norm_*), and a
+ * second recurrent mixer A with a decay that depends on the token, the selective state space
+ * scan (la_scan_*) behind its short causal convolution (la_conv_*).  Both recurrences take and
+ * return their state, so a prompt runs in parallel and continues token by token, and hand its
+ * gradient from piece to piece.
+ *
+ * The conventions above hold, with these sizes and types:
+ *   t          LA_F32 or LA_BF16: the element type of the token-sized tensors.  Parameters
+ *              (gamma, beta, w, bias, A, D, dt_bias), their gradients, mean, rstd and the scan's
+ *              states are fp32, and so is all arithmetic; a result is rounded once, when stored.
+ *   Rows       Token-major: [B, N, E] is B * N rows of E elements.  Where a leading dimension
+ *              ld* is given, row (b, n) starts (b * N + n) * ld elements behind the pointer, ld
+ *              at least the row's width (a part of a wider projection's output); all others are dense.
+ *              Widths and leading dimensions need no alignment unless said; pointers need 16 bytes.
+ *   lengths    [B] int32 on the device, or NULL (every sequence has N tokens).  Tokens from
+ *              lengths[b] on are not part of sequence b: nothing is read from their rows, their rows of
+ *              the outputs (and of the gradients) are zero, and the state handed out is that behind the
+ *              last real token.  0 is a sequence without tokens; values outside 0 .. N are taken as
+ *              the nearest of these.
+ *   LA_ERR_SHAPE also for sizes whose launch would not fit a grid: B * N * E from 2^36 on, and as said below.
+ *   Non-finite inputs are outside the contract, but for causality: outputs before token t do not
+ *              depend on what the tensors hold from token t on, and rows behind lengths[b] may hold anything.
+ */
+
+/*
+ * Layer norm of `rows` rows of E elements, 1 <= E <= 16384 (LA_ERR_UNSUPPORTED beyond):
+ *   s = x + r,   y = (s - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps),
+ * var the mean square around the mean.  r [rows,E]: a residual, or NULL.  s [rows,E] out, or NULL: the
+ * sum, rounded to t; it is the rounded sum that is normalised.  (Without r, s is x and is not written:
+ * pass NULL.)  gamma, beta [E] or NULL (ones, zeros).  mean, rstd [rows] out, or NULL; la_norm_bwd takes both.
+ */
+int la_norm_fwd(const void *x, const void *r, const float *gamma, const float *beta, void *y, void *s,
+                float *mean, float *rstd, int rows, int E, float eps, la_dtype t, void *stream);
+/*
+ * Its gradient: with xhat = (s - mean) * rstd and g = dy * gamma,
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)) + ds,   dgamma = sum dy * xhat,   dbeta = sum dy,
+ * the last two over all rows.  s: what was normalised (the forward's s, or x without a residual); ds: the
+ * gradient that reaches the sum s from elsewhere, or NULL; dx is the gradient of x and of r.  dgamma,
+ * dbeta [E] out, each or NULL.  ws: la_norm_bwd_workspace() bytes (not needed if both are NULL).
+ */
+size_t la_norm_bwd_workspace(int rows, int E, la_dtype t);
+int la_norm_bwd(const void *s, const float *gamma, const float *mean, const float *rstd, const void *dy,
+                const void *ds, void *dx, float *dgamma, float *dbeta, int rows, int E, la_dtype t,
+                void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Causal convolution along the tokens, one filter of W = 2, 3 or 4 taps per channel:
+ *   p_t = bias + sum_k w[:,k] x_{t-W+1+k},   y_t = p_t * sigmoid(p_t) if silu, else p_t.
+ * x [B,N,E] (ldx); w [E,W]; bias [E] or NULL; y [B,N,E].  x0 [B,W-1,E]: the rows before token 0, or NULL (zeros);
+ * x1 [B,W-1,E] out, or NULL: the last W - 1 rows (of x0 and x together), for the next call or la_conv_step.
+ */
+int la_conv_fwd(const void *x, int ldx, const float *w, const float *bias, const void *x0, const int *lengths,
+                void *y, void *x1, int B, int N, int E, int W, int silu, la_dtype t, void *stream);
+/*
+ * Its gradient for x, w, bias and x0 (p is formed again from x).  dx1 [B,W-1,E]: gradient that reaches the rows
+ * handed out as x1, or NULL; it is added to dx and dx0.  dx0 [B,W-1,E] out, or NULL.  dw [E,W], db [E] out, each
+ * or NULL.  ws: la_conv_bwd_workspace() bytes (not needed if both are NULL).
+ */
+size_t la_conv_bwd_workspace(int B, int N, int E, int W, la_dtype t);
+int la_conv_bwd(const void *x, int ldx, const float *w, const float *bias, const void *x0, const int *lengths,
+                const void *dy, const void *dx1, void *dx, float *dw, float *db, void *dx0,
+                int B, int N, int E, int W, int silu, la_dtype t, void *ws, size_t ws_bytes, void *stream);
+/*
+ * One token of every sequence: x, y [B,E]; state [B,W-1,E] in and out (the W - 1 rows before the token, then
+ * those before the next).
+ */
+int la_conv_step(const void *x, const float *w, const float *bias, void *state, void *y, int B, int E, int W,
+                 int silu, la_dtype t, void *stream);
+
+/*
+ * Selective state space scan over E channels of S = 8, 16 or 32 states:
+ *   d_t = softplus(dt_t + dt_bias)  (LA_SCAN_SOFTPLUS; else dt_t + dt_bias),
+ *   h_t = exp(d_t A) h_{t-1} + d_t x_t B_t,   v_t = C_t . h_t + D x_t,   y_t = v_t * z_t * sigmoid(z_t).
+ * x, dt, z [B,N,E] (ldx, lddt, ldz); z NULL: y = v.  Bt, Ct [B,N,G,S] (ldb, ldc: between tokens, multiples of 16 bytes,
+ * LA_ERR_ALIGN otherwise): channel e has those of group e / (E / G), G divides E.  A [E,S] (negative for a decay); D,
+ * dt_bias [E], each or NULL (zeros).  h0 [B,E,S]: the state before token 0, or NULL (zero); h1 [B,E,S] out, or NULL: the
+ * state behind the last token.  y [B,N,E].
+ * LA_SCAN_KEEP: the workspace then holds, behind the call, the states before every 16th token, 4 S / 16 bytes per
+ * token and channel, which la_scan_bwd starts from.  ws: la_scan_fwd_workspace() bytes with the same flags (0 is possible).
+ * LA_ERR_SHAPE: G does not divide E, or B * E from 2^28 on.  LA_ERR_UNSUPPORTED: S, or an unknown flag.
+ */
+#define LA_SCAN_SOFTPLUS 1
+#define LA_SCAN_KEEP 2
+size_t la_scan_fwd_workspace(int B, int N, int E, int G, int S, la_dtype t, int flags);
+int la_scan_fwd(const void *x, int ldx, const void *dt, int lddt, const void *z, int ldz, const void *Bt, int ldb,
+                const void *Ct, int ldc, const float *A, const float *D, const float *dt_bias, const float *h0,
+                const int *lengths, void *y, float *h1, int B, int N, int E, int G, int S, int flags, la_dtype t,
+                void *ws, size_t ws_bytes, void *stream);
+/*
+ * Its gradient: dy [B,N,E] in; dx, ddt, dz [B,N,E] (dz NULL exactly if z is), dB, dC [B,N,G,S] and dA [E,S] out; dD,
+ * ddt_bias [E] out, each or NULL.  dh1 [B,E,S]: gradient that reaches h1, or NULL (zero); dh0 [B,E,S] out, or NULL.
+ * fwd_ws: the workspace of la_scan_fwd with LA_SCAN_KEEP on the same inputs and sizes, untouched since, or NULL: the
+ * states are formed again.  ws: la_scan_bwd_workspace() bytes; its flags have LA_SCAN_KEEP if fwd_ws is given.
+ */
+size_t la_scan_bwd_workspace(int B, int N, int E, int G, int S, la_dtype t, int flags);
+int la_scan_bwd(const void *x, int ldx, const void *dt, int lddt, const void *z, int ldz, const void *Bt, int ldb,
+                const void *Ct, int ldc, const float *A, const float *D, const float *dt_bias, const float *h0,
+                const int *lengths, const void *fwd_ws, const void *dy, const float *dh1, void *dx, void *ddt,
+                void *dz, void *dB, void *dC, float *dA, float *dD, float *ddt_bias, float *dh0,
+                int B, int N, int E, int G, int S, int flags, la_dtype t, void *ws, size_t ws_bytes, void *stream);
+/*
+ * One token of every sequence: x, dt, z, y [B,E]; Bt, Ct [B,G,S]; h [B,E,S] in and out.  flags: LA_SCAN_SOFTPLUS or 0.
+ */
+int la_scan_step(const void *x, const void *dt, const void *z, const void *Bt, const void *Ct, const float *A,
+                 const float *D, const float *dt_bias, float *h, void *y, int B, int E, int G, int S, int flags,
+                 la_dtype t, void *stream);
+
+/*
  * Optional profiling hook (measurement aid, not part of the method).  The caller creates a
  * la_profile object and owns it.  Between la_profile_begin(p, mask) and la_profile_end(p, ...)
  * every launch that THE CALLING THREAD makes of a kernel whose bit (1u << la_kernel_id) is set

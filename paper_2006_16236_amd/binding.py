@@ -25,7 +25,10 @@ EXPORTS = ("la_status_string", "la_version", "la_causal_fwd_workspace", "la_caus
            "la_causal_fwd_state_bnhd", "la_causal_bwd_state_bnhd", "la_profile_create", "la_profile_destroy",
            "la_global_fwd", "la_global_bwd", "la_global_fwd_bnhd", "la_global_bwd_bnhd",
            "la_recurrent_step", "la_recurrent_steps", "la_causal_fwd_noalloc", "la_kernel_name", "la_profile_begin",
-           "la_profile_end", "la_tuning_reload")
+           "la_profile_end", "la_tuning_reload", "la_norm_fwd", "la_norm_bwd_workspace", "la_norm_bwd", "la_conv_fwd",
+           "la_conv_bwd_workspace", "la_conv_bwd", "la_conv_step", "la_scan_fwd_workspace", "la_scan_fwd",
+           "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step")
+LA_SCAN_SOFTPLUS, LA_SCAN_KEEP = 1, 2
 LA_K_COUNT = 8
 
 
@@ -96,6 +99,18 @@ def _load() -> ctypes.CDLL:
     lib.la_profile_begin.argtypes = [vp, ctypes.c_uint]
     lib.la_profile_end.restype = i
     lib.la_profile_end.argtypes = [vp, ctypes.POINTER(f), ctypes.POINTER(i)]
+    for name, restype, argtypes in (
+            ("la_norm_fwd", i, [vp] * 8 + [i, i, f, i, vp]), ("la_norm_bwd_workspace", sz, [i, i, i]),
+            ("la_norm_bwd", i, [vp] * 9 + [i, i, i, vp, sz, vp]),
+            ("la_conv_fwd", i, [vp, i] + [vp] * 6 + [i] * 6 + [vp]), ("la_conv_bwd_workspace", sz, [i] * 5),
+            ("la_conv_bwd", i, [vp, i] + [vp] * 10 + [i] * 6 + [vp, sz, vp]),
+            ("la_conv_step", i, [vp] * 5 + [i] * 5 + [vp]),
+            ("la_scan_fwd_workspace", sz, [i] * 7), ("la_scan_bwd_workspace", sz, [i] * 7),
+            ("la_scan_fwd", i, [vp, i] * 5 + [vp] * 7 + [i] * 7 + [vp, sz, vp]),
+            ("la_scan_bwd", i, [vp, i] * 5 + [vp] * 17 + [i] * 7 + [vp, sz, vp]),
+            ("la_scan_step", i, [vp] * 10 + [i] * 6 + [vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = restype, argtypes
     return lib
 
 

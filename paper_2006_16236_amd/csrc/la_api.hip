@@ -10,15 +10,17 @@
 #include <vector>
 
 #include "../../include/la.h"
+#include "la_checks.h"
 #include "la_launch.h"
 #include "la_plan.h"
 
 namespace {
 
 using namespace la_plan;
+using namespace la_check;
 static_assert(kChunk == la::kChunk && state_stride(32, 64) == la::state_stride(32, 64), "la_plan.h and the kernels");
 
-constexpr int kVersion = 401;   // 0.4.1
+constexpr int kVersion = 500;   // 0.5.0
 
 int env_int(const char *name, int dflt) {
     const char *s = getenv(name);
@@ -74,42 +76,6 @@ int check_dims(int B, int H, int N, int D, int M, float eps, la_dtype t) {
     if ((double)B * H >= 1048576.0) return LA_ERR_SHAPE;               // grid size stays in int
     return LA_OK;
 }
-
-bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-// Aliasing: no buffer that a call writes may overlap any other buffer of the call.
-struct Span {
-    const void *p;
-    size_t bytes;
-};
-bool overlap(const Span &a, const Span &b) {
-    if (a.p == nullptr || b.p == nullptr || a.bytes == 0 || b.bytes == 0) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return x < y + b.bytes && y < x + a.bytes;
-}
-// outs: written (or read and written); ins: read only
-template <size_t NO, size_t NI>
-bool aliased(const Span (&outs)[NO], const Span (&ins)[NI]) {
-    for (size_t i = 0; i < NO; ++i) {
-        for (size_t j = i + 1; j < NO; ++j)
-            if (overlap(outs[i], outs[j])) return true;
-        for (size_t j = 0; j < NI; ++j)
-            if (overlap(outs[i], ins[j])) return true;
-    }
-    return false;
-}
-
-struct Carver {
-    char *base;
-    size_t off;
-    void *take(size_t bytes) {
-        void *p = base + off;
-        off += align256(bytes);
-        return p;
-    }
-};
-
-int hip_status(hipError_t e) { return e == hipSuccess ? LA_OK : LA_ERR_HIP; }
 
 // ---- built-in scratch of la_causal_fwd_noalloc --------------------------------------------------
 // Device memory that belongs to the library's code object: every GPU the library runs on holds

@@ -1,0 +1,274 @@
+// Short causal convolution, one filter of W taps per channel:
+//   p_t = bias + sum_k w[k] x_{t-W+1+k},   y_t = p_t sigmoid(p_t)  (or p_t),
+// its gradient, and the step for one token of every sequence.
+//
+// Bound by memory (2 tensors forward, 3 backward).  A thread takes 16 bytes of channels and a run of consecutive
+// tokens: the W - 1 rows before a token stay in its registers, so a row is read once per run plus W - 1
+// rows at its start, which the neighbouring run has just brought into the caches.
+#include "la_layer.h"
+
+namespace la {
+namespace {
+
+template <typename T> constexpr int kV = 16 / sizeof(T);
+constexpr int kAhead = 4;            // rows of a run on their way at a time
+
+// p -> silu(p) and its slope: q = sigmoid(p), p q, q (1 + p (1 - q))
+__device__ __forceinline__ float silu_slope(float p, float q) { return q * fmaf(p, 1.0f - q, 1.0f); }
+
+__device__ __forceinline__ int length_of(const int *lengths, int b, int N) {
+    return lengths == nullptr ? N : min(max(lengths[b], 0), N);
+}
+
+template <typename T, int W> struct Filter {
+    static constexpr int V = kV<T>;
+    float w[W][V], bias[V];
+    __device__ __forceinline__ Filter(const float *pw, const float *pb, int e, int valid) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int k = 0; k < W; ++k) w[k][i] = i < valid ? pw[(size_t)(e + i) * W + k] : 0.0f;
+        }
+        load_params<V>(pb == nullptr ? nullptr : pb + e, valid, bias);
+    }
+};
+
+// row t of the sequence, t >= -(W - 1): x0 (zeros without it) before token 0, nothing from `end` on
+template <typename T, int W> struct Rows {
+    const T *x, *x0;                 // at this sequence and channel; x0: its first row
+    long ldx;
+    int E, valid, end;
+    __device__ __forceinline__ Piece<T, kV<T>> operator()(int t) const {
+        if (t >= 0) return load_piece<T, kV<T>>(x + (size_t)t * ldx, t < end ? valid : 0);
+        return load_piece<T, kV<T>>(x0 + (size_t)(t + W - 1) * E, x0 == nullptr ? 0 : valid);
+    }
+};
+
+template <typename T, int W> __global__ __launch_bounds__(256) void conv_fwd_kernel(const ConvArgs a) {
+    constexpr int V = kV<T>;
+    const int pieces = (a.E + V - 1) / V;
+    const long id = (long)blockIdx.x * 256 + threadIdx.x;
+    const long cut = id / pieces;
+    if (cut >= (long)a.B * a.runs) return;
+    const int e = (int)(id - cut * pieces) * V, b = (int)(cut / a.runs), t0 = (int)(cut - (long)b * a.runs) * a.run;
+    const int valid = a.E - e, t1 = min(t0 + a.run, a.N), len = length_of(a.lengths, b, a.N);
+    const T *x = (const T *)a.x + (size_t)b * a.N * a.ldx + e;
+    const T *x0 = a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * a.E + e;
+    T *y = (T *)a.y + (size_t)b * a.N * a.E + e;
+    if (a.x1 != nullptr && t0 == 0) {        // the last W - 1 rows of the sequence, rows of x0 among them if it is short
+        const Rows<T, W> all{x, x0, a.ldx, a.E, valid, len};
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+            store_piece<T, V>((T *)a.x1 + ((size_t)b * (W - 1) + k) * a.E + e, valid, all(len - (W - 1) + k));
+    }
+    const Rows<T, W> row{x, x0, a.ldx, a.E, valid, len};
+    const Filter<T, W> f(a.w, a.bias, e, valid);
+    Piece<T, V> win[W - 1];
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) win[k] = row(t0 - (W - 1) + k);
+    for (int t = t0; t < t1; t += kAhead) {
+        Piece<T, V> next[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) next[j] = row(t + j);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            float o[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float p = f.bias[i];
+#pragma unroll
+                for (int k = 0; k < W; ++k) {
+                    const int at = j + k - (W - 1);      // row of the tap among `win`, `next`
+                    p = fmaf(f.w[k][i], at < 0 ? win[at + W - 1].get(i) : next[at].get(i), p);
+                }
+                o[i] = t + j < len ? (a.silu ? p * sigmoid(p) : p) : 0.0f;
+            }
+            if (t + j < t1) store_row<T, V>(y + (size_t)(t + j) * a.E, valid, o);
+        }
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) win[k] = next[kAhead - (W - 1) + k];
+    }
+}
+
+// A run [t0, t1) of the gradient: dp_t = dy_t slope(p_t) for t0 <= t < t1 + W - 1 (the last W - 1 belong to the next run
+// and are formed again here), dx_t = sum_k w[k] dp_{t+W-1-k}, dw[k] = sum_t dp_t x_{t-W+1+k}, db = sum_t dp_t.
+// lpr lanes take the pieces of a row side by side, 256 / lpr runs at once; their dw and db are added up in LDS.
+template <typename T, int W> __global__ __launch_bounds__(256) void conv_bwd_kernel(const ConvArgs a) {
+    constexpr int V = kV<T>;
+    extern __shared__ float red[];           // [256 / lpr][lpr][V]
+    const int lane = threadIdx.x % a.lpr, slot = threadIdx.x / a.lpr, slots = 256 / a.lpr;
+    const int group = (int)(blockIdx.x % a.groups);
+    const long set = blockIdx.x / a.groups, cut = set * slots + slot;
+    const int e = (group * a.lpr + lane) * V, valid = a.E - e;
+    float dw[W + 1][V] = {};                 // dw[W]: db
+    if (cut < (long)a.B * a.runs && valid > 0) {
+        const int b = (int)(cut / a.runs), t0 = (int)(cut - (long)b * a.runs) * a.run, t1 = min(t0 + a.run, a.N);
+        const int len = length_of(a.lengths, b, a.N);
+        const Rows<T, W> row{(const T *)a.x + (size_t)b * a.N * a.ldx + e,
+                             a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * a.E + e, a.ldx, a.E, valid, len};
+        const T *dy = (const T *)a.dy + (size_t)b * a.N * a.E + e;
+        T *dx = (T *)a.dx + (size_t)b * a.N * a.E + e;
+        const size_t state = (size_t)b * (W - 1) * a.E + e;
+        const Filter<T, W> f(a.w, a.bias, e, valid);
+        float win[W - 1][V], dp[W][V] = {};  // x_{t-W+1} .. x_{t-1}; dp_{t-W+1} .. dp_t
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) {
+            const Piece<T, V> p = row(t0 - (W - 1) + k);
+#pragma unroll
+            for (int i = 0; i < V; ++i) win[k][i] = p.get(i);
+        }
+        for (int t = t0; t < t1 + W - 1; t += kAhead) {
+            Piece<T, V> nx[kAhead], nd[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const bool wanted = t + j < t1 + W - 1;
+                nx[j] = load_piece<T, V>(row.x + (size_t)(t + j) * a.ldx, wanted && t + j < len ? valid : 0);
+                nd[j] = load_piece<T, V>(dy + (size_t)(t + j) * a.E, wanted && t + j < len ? valid : 0);
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int now = t + j;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float x = nx[j].get(i);
+                    float p = fmaf(f.w[W - 1][i], x, f.bias[i]);
+#pragma unroll
+                    for (int k = 0; k < W - 1; ++k) p = fmaf(f.w[k][i], win[k][i], p);
+                    float d = nd[j].get(i);
+                    if (a.silu) d *= silu_slope(p, sigmoid(p));
+                    d = now < len ? d : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < W - 1; ++k) dp[k][i] = dp[k + 1][i];
+                    dp[W - 1][i] = d;
+                    const float mine = now < t1 ? d : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < W - 1; ++k) dw[k][i] = fmaf(mine, win[k][i], dw[k][i]);
+                    dw[W - 1][i] = fmaf(mine, x, dw[W - 1][i]);
+                    dw[W][i] += mine;
+#pragma unroll
+                    for (int k = 0; k + 1 < W - 1; ++k) win[k][i] = win[k + 1][i];
+                    win[W - 2][i] = x;
+                    o[i] = 0.0f;             // dx_{now - W + 1} = sum_k w[k] dp_{now - k}
+#pragma unroll
+                    for (int k = 0; k < W; ++k) o[i] = fmaf(f.w[k][i], dp[W - 1 - k][i], o[i]);
+                }
+                const int out = now - (W - 1);
+                // gradient that arrives at the rows handed on: x1 holds rows len - W + 1 .. len - 1
+                if (a.dx1 != nullptr && out >= len - (W - 1) && out < len) {
+                    const Piece<T, V> g = load_piece<T, V>((const T *)a.dx1 + state + (size_t)(out - (len - (W - 1))) * a.E, valid);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] += g.get(i);
+                }
+                if (out >= t0 && out < t1) store_row<T, V>(dx + (size_t)out * a.E, valid, o);
+                else if (out < 0 && a.dx0 != nullptr && t0 == 0) store_row<T, V>((T *)a.dx0 + state + (size_t)(out + W - 1) * a.E, valid, o);
+            }
+        }
+    }
+    if (a.part == nullptr) return;
+    for (int k = 0; k <= W; ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float v = dw[0][i];
+#pragma unroll
+            for (int m = 1; m <= W; ++m) v = k == m ? dw[m][i] : v;
+            red[(size_t)(slot * a.lpr + lane) * V + i] = v;
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.lpr * V; c += 256) {
+            const int at = group * a.lpr * V + c;
+            if (at >= a.E) continue;
+            float v = 0.0f;
+            for (int r = 0; r < slots; ++r) v += red[(size_t)r * a.lpr * V + c];
+            // [E][W] of the taps, then [E] of the bias, as the sums of all workgroups are handed out
+            a.part[(size_t)set * a.E * (W + 1) + (k < W ? (size_t)at * W + k : (size_t)a.E * W + at)] = v;
+        }
+    }
+}
+
+template <typename T, int W> __global__ __launch_bounds__(256) void conv_step_kernel(const T *x, const float *w, const float *bias, T *state, T *y,
+                                                                                   int B, int E, bool silu) {
+    constexpr int V = kV<T>;
+    const int pieces = (E + V - 1) / V;
+    const long id = (long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= (long)B * pieces) return;
+    const long b = id / pieces;
+    const int e = (int)(id - b * pieces) * V, valid = E - e;
+    T *rows = state + (size_t)b * (W - 1) * E + e;
+    Piece<T, V> r[W];
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) r[k] = load_piece<T, V>(rows + (size_t)k * E, valid);
+    r[W - 1] = load_piece<T, V>(x + (size_t)b * E + e, valid);
+    const Filter<T, W> f(w, bias, e, valid);
+    float o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        float p = f.bias[i];
+#pragma unroll
+        for (int k = 0; k < W; ++k) p = fmaf(f.w[k][i], r[k].get(i), p);
+        o[i] = silu ? p * sigmoid(p) : p;
+    }
+    store_row<T, V>(y + (size_t)b * E + e, valid, o);
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) store_piece<T, V>(rows + (size_t)k * E, valid, r[k + 1]);
+}
+
+#define LA_CONV_DISPATCH(W, dtype, ...)                                                                      \
+    do {                                                                                                     \
+        if ((dtype) == 0) {                                                                                  \
+            using TT = float;                                                                                \
+            if ((W) == 2) { constexpr int kW = 2; __VA_ARGS__; }                                             \
+            else if ((W) == 3) { constexpr int kW = 3; __VA_ARGS__; }                                        \
+            else { constexpr int kW = 4; __VA_ARGS__; }                                                      \
+        } else {                                                                                             \
+            using TT = bf16_t;                                                                               \
+            if ((W) == 2) { constexpr int kW = 2; __VA_ARGS__; }                                             \
+            else if ((W) == 3) { constexpr int kW = 3; __VA_ARGS__; }                                        \
+            else { constexpr int kW = 4; __VA_ARGS__; }                                                      \
+        }                                                                                                    \
+    } while (0)
+
+int pieces_of(int E, int dtype) { return dtype == 0 ? (E + 3) / 4 : (E + 7) / 8; }
+
+}  // namespace
+
+hipError_t launch_conv_fwd(ConvArgs a, int dtype, hipStream_t s) {
+    const long pieces = pieces_of(a.E, dtype);
+    // 16 tokens a run; shorter ones where those are too few threads for the machine
+    a.run = 16;
+    while (a.run > 4 && a.B * pieces * ((a.N + a.run - 1) / a.run) < 256 * 1024) a.run /= 2;
+    a.runs = (a.N + a.run - 1) / a.run;
+    const long threads = (long)a.B * a.runs * pieces;
+    LA_CONV_DISPATCH(a.W, dtype, conv_fwd_kernel<TT, kW><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a));
+    return hipGetLastError();
+}
+
+long conv_plan_bwd(ConvArgs &a, int dtype) {
+    const int pieces = pieces_of(a.E, dtype);
+    a.lpr = 64;
+    while (a.lpr / 2 >= pieces && a.lpr > 1) a.lpr /= 2;
+    a.groups = (pieces + a.lpr - 1) / a.lpr;
+    a.run = 32;
+    while (a.run > 8 && (long)a.B * pieces * ((a.N + a.run - 1) / a.run) < 128 * 1024) a.run /= 2;
+    a.runs = (a.N + a.run - 1) / a.run;
+    const long cuts = (long)a.B * a.runs, slots = 256 / a.lpr;
+    return (cuts + slots - 1) / slots;
+}
+
+hipError_t launch_conv_bwd(const ConvArgs &a, int dtype, hipStream_t s) {
+    ConvArgs p = a;
+    const long sets = conv_plan_bwd(p, dtype);
+    LA_CONV_DISPATCH(a.W, dtype, conv_bwd_kernel<TT, kW><<<(unsigned)(sets * p.groups), 256, 256 * kV<TT> * sizeof(float), s>>>(p));
+    return hipGetLastError();
+}
+
+hipError_t launch_conv_step(const void *x, const float *w, const float *bias, void *state, void *y, int B, int E, int W,
+                            bool silu, int dtype, hipStream_t s) {
+    const long threads = (long)B * pieces_of(E, dtype);
+    LA_CONV_DISPATCH(W, dtype, conv_step_kernel<TT, kW><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(
+        (const TT *)x, w, bias, (TT *)state, (TT *)y, B, E, silu));
+    return hipGetLastError();
+}
+
+}  // namespace la

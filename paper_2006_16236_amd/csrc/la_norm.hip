@@ -1,0 +1,261 @@
+// Layer norm over rows of E elements, y = (s - mean) * rstd * gamma + beta with s = x + r, and its gradient.
+//
+// Bound by memory: forward 2 tensors (4 with a residual and its sum), backward 3 (4).  A row lives in the
+// registers of the lanes that share it, so that each element is read once: mean, then the sum of squares around it
+// (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  64 lanes share rows
+// up to 1024 elements, 256 up to 4096, 1024 up to 16384: 16 elements a lane at most, which leaves room for
+// the backward's two sums per column.
+#include "la_layer.h"
+
+namespace la {
+namespace {
+
+constexpr int kSumSlices = 16;
+constexpr long kMaxGrid = 1 << 20;       // workgroups of a launch; more rows go round again
+
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ part, long rows, const SumTargets out) {
+    __shared__ float red[kSumSlices][kWave];
+    const int lane = threadIdx.x % kWave, slice = threadIdx.x / kWave;
+    const long cols = out.n[0] + out.n[1] + out.n[2], c = (long)blockIdx.x * kWave + lane;
+    float v = 0.0f;
+    if (c < cols) {
+        long r = slice;
+        for (; r + 3 * kSumSlices < rows; r += 4 * kSumSlices) {        // four loads on their way at a time
+            float t[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = part[(r + i * kSumSlices) * cols + c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v += t[i];
+        }
+        for (; r < rows; r += kSumSlices) v += part[r * cols + c];
+    }
+    red[slice][lane] = v;
+    __syncthreads();
+    if (slice != 0 || c >= cols) return;
+#pragma unroll
+    for (int i = 1; i < kSumSlices; ++i) v += red[i][lane];
+    const int k = c < out.n[0] ? 0 : c < out.n[0] + out.n[1] ? 1 : 2;
+    const long at = c - (k > 0 ? out.n[0] : 0) - (k > 1 ? out.n[1] : 0);
+    float *to = k == 0 ? out.to[0] : k == 1 ? out.to[1] : out.to[2];
+    if (to != nullptr) to[at] = v;
+}
+
+// sum over the TPR lanes that share a row; `red`: one slot per wave of the workgroup
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float *red) {
+    v = wave_sum(v);
+    if constexpr (TPR > kWave) {
+        const int wave = threadIdx.x / kWave, first = wave / (TPR / kWave) * (TPR / kWave);
+        __syncthreads();
+        if (threadIdx.x % kWave == 0) red[wave] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TPR / kWave; ++i) v += red[first + i];
+    }
+    return v;
+}
+
+// TPR lanes per row, NV pieces of V elements per lane (piece j of lane l starts at element (j * TPR + l) * V)
+template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(const NormArgs a) {
+    constexpr int V = 16 / sizeof(T), kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
+    __shared__ float red[kThreads / kWave];
+    const int E = a.E, l = threadIdx.x % TPR;
+    for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
+    const long row = first + threadIdx.x / TPR;
+    const bool live = row < a.rows;          // whole waves; all of a workgroup's waves meet in row_sum
+    float f[NV][V];
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
+        const size_t at = (size_t)row * E + e;
+        Piece<T, V> p = load_piece<T, V>((const T *)a.x + at, valid);
+        if (a.r != nullptr) {
+            const Piece<T, V> q = load_piece<T, V>((const T *)a.r + at, valid);
+            float t[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) t[i] = p.get(i) + q.get(i);
+            // the stored sum is what the backward (and the next layer) reads: it is what is normalised
+            p = pack_piece<T, V>(t);
+            if (a.s != nullptr) store_piece<T, V>((T *)a.s + at, valid, p);
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum += f[j][i] = p.get(i);
+    }
+    const float mean = row_sum<TPR>(sum, red) / E;
+    float sq = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            f[j][i] -= mean;
+            if ((j * TPR + l) * V + i < E) sq = fmaf(f[j][i], f[j][i], sq);
+        }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, red) / E + a.eps);
+    if (l == 0 && live) {
+        if (a.mean != nullptr) a.mean[row] = mean;
+        if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (j * TPR + l) * V;
+        float g[V], b[V];
+        load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, g, 1.0f);
+        load_params<V>(a.beta == nullptr ? nullptr : a.beta + e, E - e, b);
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = fmaf(f[j][i] * rstd, g[i], b[i]);
+        store_row<T, V>((T *)a.y + (size_t)row * E + e, live ? E - e : 0, g);
+    }
+    }
+}
+
+// xhat = (s - mean) rstd, g = dy gamma, dx = rstd (g - mean(g) - xhat mean(g xhat)) + ds; a workgroup takes every
+// gridDim-th group of rows and keeps its part of dgamma = sum dy xhat, dbeta = sum dy in registers.
+template <typename T, int TPR, int NV> __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormArgs a) {
+    constexpr int V = 16 / sizeof(T), kRows = 1024 / TPR;
+    __shared__ float red[2 * 1024 / kWave];
+    extern __shared__ float cols[];          // [2][E], kRows > 1 only
+    const int E = a.E, l = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    float dg[NV][V] = {}, db[NV][V] = {}, gamma[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (j * TPR + l) * V;
+        load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, gamma[j], 1.0f);
+    }
+    for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
+        const long row = first + slot;
+        const bool live = row < a.rows;
+        const float mean = live ? a.mean_in[row] : 0.0f, rstd = live ? a.rstd_in[row] : 0.0f;
+        Piece<T, V> s[NV], d[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
+            s[j] = load_piece<T, V>((const T *)a.x + (size_t)row * E + e, valid);
+            d[j] = load_piece<T, V>((const T *)a.dy + (size_t)row * E + e, valid);
+        }
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float xhat = (s[j].get(i) - mean) * rstd, dy = d[j].get(i), g = dy * gamma[j][i];
+                s1 += g;
+                s2 = fmaf(g, xhat, s2);
+                dg[j][i] = fmaf(dy, xhat, dg[j][i]);
+                db[j][i] += dy;
+            }
+        }
+        s1 = wave_sum(s1), s2 = wave_sum(s2);
+        if constexpr (TPR > kWave) {
+            const int wave = threadIdx.x / kWave, w0 = wave / (TPR / kWave) * (TPR / kWave);
+            __syncthreads();
+            if (threadIdx.x % kWave == 0) red[2 * wave] = s1, red[2 * wave + 1] = s2;
+            __syncthreads();
+            s1 = s2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < TPR / kWave; ++i) s1 += red[2 * (w0 + i)], s2 += red[2 * (w0 + i) + 1];
+        }
+        s1 /= E, s2 /= E;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
+            const size_t at = (size_t)row * E + e;
+            Piece<T, V> ds{};
+            if (a.r != nullptr) ds = load_piece<T, V>((const T *)a.r + at, valid);
+            float o[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float xhat = (s[j].get(i) - mean) * rstd, g = d[j].get(i) * gamma[j][i];
+                o[i] = fmaf(rstd, g - fmaf(xhat, s2, s1), a.r != nullptr ? ds.get(i) : 0.0f);
+            }
+            store_row<T, V>((T *)a.y + at, valid, o);
+        }
+    }
+    if (a.part == nullptr) return;
+    // the rows' slots one after the other (a fixed order), each lane on its own columns
+    if constexpr (kRows > 1) {
+        for (int k = 0; k < kRows; ++k) {
+            if (slot == k) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int e = (j * TPR + l) * V + i;
+                        if (e < E) {
+                            cols[e] = k == 0 ? dg[j][i] : cols[e] + dg[j][i];
+                            cols[E + e] = k == 0 ? db[j][i] : cols[E + e] + db[j][i];
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * E; c += 1024) a.part[(size_t)blockIdx.x * 2 * E + c] = cols[c];
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int e = (j * TPR + l) * V + i;
+                if (e < E) {
+                    a.part[(size_t)blockIdx.x * 2 * E + e] = dg[j][i];
+                    a.part[(size_t)blockIdx.x * 2 * E + E + e] = db[j][i];
+                }
+            }
+        }
+    }
+}
+
+int lanes_of(int E) { return E <= 1024 ? 64 : E <= 4096 ? 256 : 1024; }
+
+}  // namespace
+
+hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, hipStream_t s) {
+    const long cols = out.n[0] + out.n[1] + out.n[2];
+    sum_rows_kernel<<<(unsigned)((cols + kWave - 1) / kWave), 1024, 0, s>>>(part, rows, out);
+    return hipGetLastError();
+}
+
+int norm_groups(int rows, int E) {
+    const int per = 1024 / lanes_of(E);
+    const long sets = ((long)rows + per - 1) / per, turns = (sets + 255) / 256;     // equal shares for up to 256 workgroups
+    return (int)((sets + turns - 1) / turns);
+}
+
+// pieces per lane: 1, 2 or 4 (fp32: 16 elements are four pieces; bf16: two)
+#define LA_NORM_DISPATCH(KERNEL)                                                                         \
+    do {                                                                                                 \
+        const int tpr = lanes_of(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);     \
+        if (dtype == 0) {                                                                                \
+            if (tpr == 64) { if (nv <= 1) KERNEL(float, 64, 1); else if (nv == 2) KERNEL(float, 64, 2); else KERNEL(float, 64, 4); }   \
+            else if (tpr == 256) { if (nv == 2) KERNEL(float, 256, 2); else KERNEL(float, 256, 4); }     \
+            else { if (nv == 2) KERNEL(float, 1024, 2); else KERNEL(float, 1024, 4); }                   \
+        } else {                                                                                         \
+            if (tpr == 64) { if (nv <= 1) KERNEL(bf16_t, 64, 1); else KERNEL(bf16_t, 64, 2); }           \
+            else if (tpr == 256) { if (nv <= 1) KERNEL(bf16_t, 256, 1); else KERNEL(bf16_t, 256, 2); }   \
+            else { if (nv <= 1) KERNEL(bf16_t, 1024, 1); else KERNEL(bf16_t, 1024, 2); }                 \
+        }                                                                                                \
+    } while (0)
+
+hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
+#define LA_KERNEL(T, TPR, NV)                                                                                        \
+    do {                                                                                                             \
+        constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR;                                          \
+        const long sets = ((long)a.rows + per - 1) / per;                                                            \
+        norm_fwd_kernel<T, TPR, NV><<<(unsigned)(sets < kMaxGrid ? sets : kMaxGrid), threads, 0, s>>>(a);            \
+    } while (0)
+    LA_NORM_DISPATCH(LA_KERNEL);
+#undef LA_KERNEL
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
+    const int groups = norm_groups(a.rows, a.E);
+#define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, 1024, TPR < 1024 ? 2 * a.E * sizeof(float) : 0, s>>>(a)
+    LA_NORM_DISPATCH(LA_KERNEL);
+#undef LA_KERNEL
+    return hipGetLastError();
+}
+
+}  // namespace la
