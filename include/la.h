@@ -415,8 +415,8 @@ int la_conv_step(const void *x, const float *w, const float *bias, void *state, 
  * Selective state space scan over E channels of S = 8, 16 or 32 states:
  *   d_t = softplus(dt_t + dt_bias)  (LA_SCAN_SOFTPLUS; else dt_t + dt_bias),
  *   h_t = exp(d_t A) h_{t-1} + d_t x_t B_t,   v_t = C_t . h_t + D x_t,   y_t = v_t * z_t * sigmoid(z_t).
- * x, dt, z [B,N,E] (ldx, lddt, ldz); z NULL: y = v.  Bt, Ct [B,N,G,S] (ldb, ldc: between tokens, multiples of 16 bytes,
- * LA_ERR_ALIGN otherwise): channel e has those of group e / (E / G), G divides E.  A [E,S] (negative for a decay); D,
+ * x, dt, z [B,N,E] (ldx, lddt, ldz); z NULL: y = v.  Bt, Ct [B,N,G,S] (ldb, ldc: between tokens): channel e has those
+ * of group e / (E / G), G divides E.  A [E,S] (negative for a decay); D,
  * dt_bias [E], each or NULL (zeros).  h0 [B,E,S]: the state before token 0, or NULL (zero); h1 [B,E,S] out, or NULL: the
  * state behind the last token.  y [B,N,E].
  * LA_SCAN_KEEP: the workspace then holds, behind the call, the states before every 16th token, 4 S / 16 bytes per

@@ -107,21 +107,6 @@ __device__ __forceinline__ float add_rows(float v) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return add_halves(add_rows(row_sum16(v))); }
 
-// A load through the scalar unit: the address is the same in every lane, and nothing writes there while the kernel runs.
-template <int N> struct Words { uint32_t w[N]; };
-typedef const __attribute__((address_space(4))) uint32_t *scalar_words;
-template <int N> __device__ __forceinline__ Words<N> load_uniform(const void *p, size_t byte) {
-    const scalar_words q = (scalar_words)(uintptr_t)(static_cast<const char *>(p) + byte);
-    Words<N> r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) r.w[i] = q[i];
-    return r;
-}
-template <typename T, int V> __device__ __forceinline__ float word_value(const Words<V * sizeof(T) / 4> &r, int i) {
-    if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
-    else return __uint_as_float(r.w[i]);
-}
-
 // ---- launchers --------------------------------------------------------------------------------------
 // Column sums of part [rows][cols], cols = n[0] + n[1] + n[2]: the first n[0] go to to[0], and so on (NULL: not wanted).
 // The rows of a column are added in an order that their number alone decides.
@@ -164,7 +149,7 @@ hipError_t launch_conv_step(const void *x, const float *w, const float *bias, vo
                             bool silu, int dtype, hipStream_t s);
 
 // The scan's tokens go in tiles of kScanTile; the states before each tile are what a backward starts from.
-constexpr int kScanTile = 16, kScanLanes = 64, kScanPer = 4;      // channels of a workgroup; states of a wave
+constexpr int kScanTile = 16, kScanLanes = 64;                    // tokens of a tile, channels of a workgroup
 struct ScanArgs {
     const void *x, *dt, *z, *Bt, *Ct, *dy;
     const float *A, *D, *bias, *h0, *dh1;

@@ -74,8 +74,6 @@ struct Scan {
     }
 };
 bool bad_rows(int ld, int width) { return ld < width; }
-// B_t and C_t are loaded by the scalar unit, 16 bytes at a time
-bool bad_stride(int ld, la_dtype t) { return ((size_t)ld * esize_of(t)) % 16 != 0; }
 }  // namespace
 
 extern "C" {
@@ -197,7 +195,7 @@ int la_scan_fwd(const void *x, int ldx, const void *dt, int lddt, const void *z,
     if (st != LA_OK) return st;
     if (bad_rows(ldx, E) || bad_rows(lddt, E) || (z != nullptr && bad_rows(ldz, E)) || bad_rows(ldb, G * S) || bad_rows(ldc, G * S))
         return LA_ERR_SHAPE;
-    if (any_misaligned(x, dt, z, Bt, Ct, A, D, dt_bias, h0, lengths, y, h1, ws) || bad_stride(ldb, t) || bad_stride(ldc, t))
+    if (any_misaligned(x, dt, z, Bt, Ct, A, D, dt_bias, h0, lengths, y, h1, ws))
         return LA_ERR_ALIGN;
     Scan k(B, N, E, G, S);
     const size_t need = k.fwd_bytes(flags);
@@ -234,8 +232,7 @@ int la_scan_bwd(const void *x, int ldx, const void *dt, int lddt, const void *z,
     if (st != LA_OK) return st;
     if (bad_rows(ldx, E) || bad_rows(lddt, E) || (z != nullptr && bad_rows(ldz, E)) || bad_rows(ldb, G * S) || bad_rows(ldc, G * S))
         return LA_ERR_SHAPE;
-    if (any_misaligned(x, dt, z, Bt, Ct, A, D, dt_bias, h0, lengths, fwd_ws, dy, dh1, dx, ddt, dz, dB, dC, dA, dD, ddt_bias, dh0, ws) ||
-        bad_stride(ldb, t) || bad_stride(ldc, t))
+    if (any_misaligned(x, dt, z, Bt, Ct, A, D, dt_bias, h0, lengths, fwd_ws, dy, dh1, dx, ddt, dz, dB, dC, dA, dD, ddt_bias, dh0, ws))
         return LA_ERR_ALIGN;
     Scan k(B, N, E, G, S);
     const size_t need = k.bwd_bytes(fwd_ws != nullptr ? LA_SCAN_KEEP : 0);

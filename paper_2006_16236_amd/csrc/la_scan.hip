@@ -7,9 +7,8 @@
 //
 // A decay per channel and state leaves no matrix product: the work is an exp2 and four vector instructions per
 // state and token (13 in the backward), and vector issue is the bound, not memory.  So:
-// * A lane is a channel, a wave kScanPer = 4 states of 64 channels, S / 4 waves a workgroup.  B_t and C_t are then the
-//   same in all lanes of a wave: they come through the scalar unit and enter the vector instructions as
-//   scalar operands, with no vector load, LDS read or register of their own.
+// * A lane is a channel, a wave P = 2 (32 states: 4) states of 64 channels, S / P waves a workgroup.  B_t and C_t are then
+//   the same in all lanes of a wave: read from LDS at one address for all of them.
 // * What a token needs once per channel (softplus, d x, the gate, D x, conversions) is done by all waves together, a
 //   tile of 16 tokens at a time, and handed over through LDS; the waves' partial C . h come back the same way.
 // * Sequences too few to fill the machine are cut into pieces: the state each piece adds from zero, a scan over the
@@ -19,7 +18,7 @@
 namespace la {
 namespace {
 
-constexpr int T = kScanTile, kLanes = kScanLanes, P = kScanPer;
+constexpr int T = kScanTile, kLanes = kScanLanes;
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ int length_of(const int *lengths, int b, int N) {
@@ -42,191 +41,287 @@ struct Where {
     }
 };
 
-// The elements of a tile that a thread prepares and finishes: EPT channels of one token.
-template <typename TT, int NW> struct Mine {
-    static constexpr int EPT = T * kLanes / (64 * NW);            // 8, 4, 2 for 2, 4, 8 waves
-    int t, c, valid;
-    __device__ __forceinline__ Mine(int channels) {
-        t = threadIdx.x / (kLanes / EPT), c = threadIdx.x % (kLanes / EPT) * EPT, valid = channels - c;
+// Elements of a channel, as they are in memory, for the tokens of a tile that a thread prepares and finishes: wave q takes
+// tokens q K .. q K + K - 1 of its 64 channels, so that K tokens of a channel go through LDS side by side.
+template <typename TT> struct Raw;
+template <> struct Raw<float> { using type = float; };
+template <> struct Raw<bf16_t> { using type = uint16_t; };
+template <typename TT, int K> struct Column {
+    typename Raw<TT>::type v[K];
+    // p: the first token's element; tokens [0, n) are there (n is the same in all lanes)
+    __device__ __forceinline__ void load(const TT *p, long ld, int n) {
+        const auto *r = reinterpret_cast<const typename Raw<TT>::type *>(p);
+        if (n >= K) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = r[k * ld];
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = 0;
+                if (k < n) v[k] = r[k * ld];
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int k) const {
+        if constexpr (sizeof(TT) == 2) return __uint_as_float((uint32_t)v[k] << 16);
+        else return v[k];
     }
 };
 
-__device__ __forceinline__ size_t state_at(const ScanArgs &a, int b, int slots, int slot, int q, int e) {
-    return ((((size_t)b * slots + slot) * (a.S / P) + q) * a.E + e) * P;
+// P consecutive states from n0 on of a channel, in the layout of the kept states
+template <int P> __device__ __forceinline__ size_t state_at(const ScanArgs &a, int b, int slots, int slot, int n0, int e) {
+    return ((((size_t)b * slots + slot) * (a.S / 4) + n0 / 4) * a.E + e) * 4 + n0 % 4;
 }
 
-// B_t or C_t of a wave's states
-template <typename TT> using Row = Words<P * sizeof(TT) / 4>;
-template <typename TT> __device__ __forceinline__ Row<TT> row_of(const void *base, long ld, size_t first, int t, int last) {
-    return load_uniform<P * sizeof(TT) / 4>(base, (first + (size_t)min(t, last) * ld) * sizeof(TT));
+// B_t and C_t of a tile as fp32 pairs in LDS: a wave reads the 2 P values of a token at one address for all its lanes.
+// A thread brings kEach values of a tile there, neighbouring threads neighbouring ones.
+template <typename TT, int NW, int P> struct Pairs {
+    static constexpr int S = NW * P, kEach = 2 * T * S / (64 * NW);        // T * S / 32 / NW: 1 or 2
+    float (*lds)[T][S][2];
+    const TT *from;                  // this thread's first value of the next tile
+    long ld;
+    typename Raw<TT>::type far[kEach], near[kEach];
+    int t[kEach], which, n;
+    // values v = thread + 64 NW i of a tile: token v / (2 S), B before C
+    __device__ __forceinline__ Pairs(const ScanArgs &a, const Where &w, float (*l)[T][S][2], int first) : lds(l) {
+        const int c = threadIdx.x % (2 * S);
+        which = c / S, n = c % S, ld = which ? a.ldc : a.ldb;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) t[i] = (threadIdx.x + 64 * NW * i) / (2 * S);
+        from = (const TT *)(which ? a.Ct : a.Bt) + ((size_t)w.b * a.N + first) * ld + (size_t)w.g * S + n;
+    }
+    // tokens [0, there) of the tile belong to the sequence; step: tiles from this to the next one fetched, 1 or -1
+    __device__ __forceinline__ void fetch(int there, int step) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            near[i] = far[i], far[i] = 0;
+            if (t[i] < there) far[i] = reinterpret_cast<const typename Raw<TT>::type *>(from)[t[i] * ld];
+        }
+        from += step * T * ld;
+    }
+    __device__ __forceinline__ void park(int buf) const {                  // the tile fetched before the last fetch
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if constexpr (sizeof(TT) == 2) lds[buf][t[i]][n][which] = __uint_as_float((uint32_t)near[i] << 16);
+            else lds[buf][t[i]][n][which] = near[i];
+        }
+    }
+};
+template <int P> struct Pair {
+    float v[2 * P];
+    __device__ __forceinline__ float B(int n) const { return v[2 * n]; }
+    __device__ __forceinline__ float C(int n) const { return v[2 * n + 1]; }
+};
+template <int P> __device__ __forceinline__ Pair<P> read_pair(const float (*at)[2]) {
+    Pair<P> r;
+    __builtin_memcpy(r.v, __builtin_assume_aligned(at, 16), sizeof(r.v));
+    return r;
 }
 
-// kLocal: only what a piece adds to a state of zero, and its sum of d
-template <typename TT, int NW, bool kLocal> __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(const ScanArgs a) {
-    using M = Mine<TT, NW>;
-    constexpr int EPT = M::EPT;
-    __shared__ float2 in[T][kLanes];                              // d, d x
-    __shared__ float out[kLocal ? 1 : NW][T][kLanes];
+// kLocal: only what a piece adds to a state of zero, and its sum of d.
+// Two buffers in LDS and one barrier a tile: between two barriers a wave finishes tile i - 1 (C . h of all waves, gate,
+// store), prepares tile i + 1 and runs tile i, so that one wave's chains of functions hide behind another's states.
+// The elements come two tiles ahead.
+template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(64 * NW, 2) void scan_fwd_kernel(const ScanArgs a) {
+    constexpr int K = T / NW;
+    __shared__ __align__(16) float bc[2][T][NW * P][2];
+    __shared__ __align__(16) float2 in[2][T / 2][kLanes][2];      // d, d x of two tokens
+    __shared__ __align__(16) float out[kLocal ? 1 : 2][kLocal ? 1 : NW][NW][kLanes][K];
     const Where w(a);
-    const M me(w.channels);
     if (kLocal && w.piece == a.pieces - 1) return;                // nothing comes after it
-    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n0 = q * P;
     const int e = w.e0 + min(lane, w.channels - 1);               // lanes without a channel repeat the last one's
     const bool live = lane < w.channels;
     float A[P], h[P], sum_d = 0.0f;
 #pragma unroll
-    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + q * P + n] * kLog2e, h[n] = 0.0f;
+    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, h[n] = 0.0f;
     if constexpr (!kLocal) {
-        if (a.pieces > 1) __builtin_memcpy(h, a.piece_h + state_at(a, w.b, a.pieces, w.piece, q, e), sizeof(h));
-        else if (a.h0 != nullptr) __builtin_memcpy(h, a.h0 + ((size_t)w.b * a.E + e) * a.S + q * P, sizeof(h));
+        if (a.pieces > 1) __builtin_memcpy(h, a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), sizeof(h));
+        else if (a.h0 != nullptr) __builtin_memcpy(h, a.h0 + ((size_t)w.b * a.E + e) * a.S + n0, sizeof(h));
     }
-    float bias[EPT], D[EPT];
-    load_params<EPT>(a.bias == nullptr ? nullptr : a.bias + w.e0 + me.c, me.valid, bias);
-    load_params<EPT>(a.D == nullptr ? nullptr : a.D + w.e0 + me.c, me.valid, D);
-    const size_t row0 = (size_t)w.b * a.N;
-    const size_t bfirst = row0 * a.ldb + (size_t)w.g * a.S + q * P, cfirst = row0 * a.ldc + (size_t)w.g * a.S + q * P;
-
-    Piece<TT, EPT> x, dt, z{};
-    auto fetch = [&](int t) {
-        const size_t r = row0 + t + me.t;
-        const int valid = t + me.t < w.end ? me.valid : 0;
-        x = load_piece<TT, EPT>((const TT *)a.x + r * a.ldx + w.e0 + me.c, valid);
-        dt = load_piece<TT, EPT>((const TT *)a.dt + r * a.lddt + w.e0 + me.c, valid);
-        if (!kLocal && a.z != nullptr) z = load_piece<TT, EPT>((const TT *)a.z + r * a.ldz + w.e0 + me.c, valid);
+    const float bias = a.bias == nullptr ? 0.0f : a.bias[e], D = a.D == nullptr ? 0.0f : a.D[e];
+    Pairs<TT, NW, P> pairs(a, w, bc, w.t0);
+    const int mine = w.t0 + q * K;                                // this thread's first token
+    const size_t row = (size_t)w.b * a.N + mine;
+    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e;
+    const TT *pz = (const TT *)a.z + row * a.ldz + e;
+    TT *py = (TT *)a.y + row * a.E + e;
+    float *pk = a.keep + state_at<P>(a, w.b, a.tiles, w.t0 / T, n0, e);
+    const bool gated = !kLocal && a.z != nullptr, kept = !kLocal && a.keep != nullptr && live;
+    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0;
+    struct Tile { Column<TT, K> x, dt, z; } far, near, done;      // tiles i + 2, i + 1 and i
+    int there = w.end - mine;                                     // tokens of the sequence from this thread's next to fetch on
+    auto fetch = [&](Tile &f) {
+        f.x.load(px, a.ldx, there), f.dt.load(pdt, a.lddt, there);
+        if (gated) f.z.load(pz, a.ldz, there);
+        pairs.fetch(there + q * K, 1);
+        px += T * a.ldx, pdt += T * a.lddt, pz += T * a.ldz, there -= T;
     };
-    fetch(w.t0);
-    for (int t = w.t0; t < w.end; t += T) {
-        const Piece<TT, EPT> xt = x, zt = z;
-        const bool real = t + me.t < w.end;
+    auto prepare = [&](const Tile &f, int i, int buf) {           // d and d x of tile i
+        pairs.park(buf);
+        float d[K];
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) {
-            float d = dt.get(i) + bias[i];
-            if (a.softplus) d = softplus(d);
-            if (!real) d = 0.0f;                                  // a step of zero leaves the state as it is
-            in[me.t][me.c + i] = make_float2(d, d * x.get(i));
+        for (int k = 0; k < K; ++k) {
+            d[k] = f.dt.get(k) + bias;
+            if (a.softplus) d[k] = softplus(d[k]);
+            if (mine + i * T + k >= w.end) d[k] = 0.0f;           // a step of zero leaves the state as it is
         }
-        __syncthreads();
-        if (t + T < w.end) fetch(t + T);
-        if (!kLocal && a.keep != nullptr && live)
-            __builtin_memcpy(a.keep + state_at(a, w.b, a.tiles, t / T, q, e), h, sizeof(h));
+#pragma unroll
+        for (int k = 0; k < K; ++k) in[buf][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(d[k], d[k] * f.x.get(k));
+    };
+    fetch(near);
+    fetch(far);
+    if (tiles > 0) prepare(near, 0, 0);
+    __syncthreads();
+    for (int i = 0; i < tiles; ++i) {
+        const int buf = i & 1;
+        done = near, near = far;
+        fetch(far);
+        if (i + 1 < tiles) prepare(near, i + 1, buf ^ 1);
+        if (kept) __builtin_memcpy(pk, h, sizeof(h));
+        pk += (size_t)a.E * (NW * P);
+        float y[T];
 #pragma unroll
         for (int j = 0; j < T; ++j) {
-            const float2 v = in[j][lane];
-            const Row<TT> B = row_of<TT>(a.Bt, a.ldb, bfirst, t + j, w.end - 1);
-            float y = 0.0f;
-            if constexpr (kLocal) {
-                sum_d += v.x;
+            const float2 v = in[buf][j / 2][lane][j % 2];
+            const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
+            if constexpr (kLocal) sum_d += v.x;
+            y[j] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < P; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(v.x * A[n]), h[n], v.y * word_value<TT, P>(B, n));
-            } else {
-                const Row<TT> C = row_of<TT>(a.Ct, a.ldc, cfirst, t + j, w.end - 1);
-#pragma unroll
-                for (int n = 0; n < P; ++n) {
-                    h[n] = fmaf(__builtin_amdgcn_exp2f(v.x * A[n]), h[n], v.y * word_value<TT, P>(B, n));
-                    y = fmaf(word_value<TT, P>(C, n), h[n], y);
-                }
-                out[q][j][lane] = y;
+            for (int n = 0; n < P; ++n) {
+                h[n] = fmaf(__builtin_amdgcn_exp2f(v.x * A[n]), h[n], v.y * p.B(n));
+                y[j] = fmaf(p.C(n), h[n], y[j]);
+            }
+            if constexpr (!kLocal) {
+                if (j % K == K - 1) __builtin_memcpy(__builtin_assume_aligned(out[buf][q][j / K][lane], 4 * K), &y[j - K + 1], K * sizeof(float));
             }
         }
         __syncthreads();
         if constexpr (!kLocal) {
-            if (a.y != nullptr && t + me.t < w.t1) {
-                float o[EPT];
+            if (a.y != nullptr) {
+                float v[K];
 #pragma unroll
-                for (int i = 0; i < EPT; ++i) {
-                    float v = D[i] * xt.get(i);
+                for (int k = 0; k < K; ++k) v[k] = D * done.x.get(k);
 #pragma unroll
-                    for (int k = 0; k < NW; ++k) v += out[k][me.t][me.c + i];
-                    if (a.z != nullptr) v *= zt.get(i) * sigmoid(zt.get(i));
-                    o[i] = real ? v : 0.0f;
+                for (int m = 0; m < NW; ++m) {
+                    float part[K];
+                    __builtin_memcpy(part, out[buf][m][q][lane], sizeof(part));
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v[k] += part[k];
                 }
-                store_row<TT, EPT>((TT *)a.y + (row0 + t + me.t) * a.E + w.e0 + me.c, me.valid, o);
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const int t = mine + i * T + k;
+                    if (gated) v[k] *= done.z.get(k) * sigmoid(done.z.get(k));
+                    if (live && t < w.t1) store_elem<false>(py + (size_t)k * a.E, t < w.end ? v[k] : 0.0f);
+                }
+                py += (size_t)T * a.E;
             }
         }
     }
     if constexpr (kLocal) {
         if (live) {
-            __builtin_memcpy(a.piece_h + state_at(a, w.b, a.pieces, w.piece, q, e), h, sizeof(h));
+            __builtin_memcpy(a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), h, sizeof(h));
             if (q == 0) a.piece_d[((size_t)w.b * a.pieces + w.piece) * a.E + e] = sum_d;
         }
         return;
     }
+    if (!live) return;
     if (a.y != nullptr) {                                         // rows behind the sequence
-        const float zero[EPT] = {};
-        const int done = w.end > w.t0 ? w.t0 + (w.end - w.t0 + T - 1) / T * T : w.t0;
-        for (int t = done + me.t; t < w.t1; t += T) store_row<TT, EPT>((TT *)a.y + (row0 + t) * a.E + w.e0 + me.c, me.valid, zero);
+        for (int t = w.t0 + tiles * T + q; t < w.t1; t += NW) store_elem<false>((TT *)a.y + ((size_t)w.b * a.N + t) * a.E + e, 0.0f);
     }
-    if (a.h1 != nullptr && w.piece == a.pieces - 1 && live)
-        __builtin_memcpy(a.h1 + ((size_t)w.b * a.E + e) * a.S + q * P, h, sizeof(h));
+    if (a.h1 != nullptr && w.piece == a.pieces - 1) __builtin_memcpy(a.h1 + ((size_t)w.b * a.E + e) * a.S + n0, h, sizeof(h));
 }
 
 // What the pieces add from zero becomes the state before each piece (kReverse: the gradient behind it), in place.
 template <bool kReverse> __global__ __launch_bounds__(256) void scan_pieces_kernel(const ScanArgs a) {
+    constexpr int kAhead = 8;                                     // pieces on their way at a time
     const long per = (long)a.E * a.S;
     for (long id = (long)blockIdx.x * 256 + threadIdx.x; id < a.B * per; id += (long)gridDim.x * 256) {
-    const int b = (int)(id / per), q = (int)(id % per / ((long)a.E * P)), e = (int)(id % ((long)a.E * P) / P), n = (int)(id % P);
-    const float A = a.A[(size_t)e * a.S + q * P + n] * kLog2e;
-    const float *start = kReverse ? a.dh1 : a.h0;
-    float h = start == nullptr ? 0.0f : start[((size_t)b * a.E + e) * a.S + q * P + n];
-    for (int i = 0; i < a.pieces; ++i) {
-        const int k = kReverse ? a.pieces - 1 - i : i;
-        float *at = a.piece_h + state_at(a, b, a.pieces, k, q, e) + n;
-        if (i + 1 == a.pieces) {                                  // nothing is added behind the last
-            *at = h;
-            break;
+        const int b = (int)(id / per), e = (int)(id % ((long)a.E * 4) / 4), n = (int)(id % per / ((long)a.E * 4)) * 4 + (int)(id % 4);
+        const float A = a.A[(size_t)e * a.S + n] * kLog2e;
+        const float *start = kReverse ? a.dh1 : a.h0;
+        float h = start == nullptr ? 0.0f : start[((size_t)b * a.E + e) * a.S + n];
+        for (int i0 = 0; i0 < a.pieces; i0 += kAhead) {
+            float add[kAhead], d[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {                    // nothing is added behind the last
+                const int k = kReverse ? a.pieces - 1 - (i0 + i) : i0 + i;
+                const bool used = i0 + i + 1 < a.pieces;
+                add[i] = used ? a.piece_h[state_at<1>(a, b, a.pieces, k, n, e)] : 0.0f;
+                d[i] = used ? a.piece_d[((size_t)b * a.pieces + k) * a.E + e] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (i0 + i >= a.pieces) break;
+                const int k = kReverse ? a.pieces - 1 - (i0 + i) : i0 + i;
+                a.piece_h[state_at<1>(a, b, a.pieces, k, n, e)] = h;
+                h = fmaf(__builtin_amdgcn_exp2f(A * d[i]), h, add[i]);
+            }
         }
-        const float add = *at;
-        *at = h;
-        h = fmaf(__builtin_amdgcn_exp2f(A * a.piece_d[((size_t)b * a.pieces + k) * a.E + e]), h, add);
-    }
     }
 }
 
 // What a piece sends to the piece before it of a gradient of zero behind it: exp(d A) g at its first token, and its sum of d.
-template <typename TT, int NW> __global__ __launch_bounds__(64 * NW) void scan_local_bwd_kernel(const ScanArgs a) {
-    using M = Mine<TT, NW>;
-    constexpr int EPT = M::EPT;
-    __shared__ float2 in[T][kLanes];                              // d, dv
+template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) void scan_local_bwd_kernel(const ScanArgs a) {
+    constexpr int K = T / NW;
+    __shared__ __align__(16) float bc[2][T][NW * P][2];
+    __shared__ __align__(16) float2 in[2][T / 2][kLanes][2];      // d, dv of two tokens
     const Where w(a);
     if (w.piece == 0) return;                                     // nothing comes before it
-    const M me(w.channels);
-    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n0 = q * P;
     const int e = w.e0 + min(lane, w.channels - 1);
     float A[P], g[P], sum_d = 0.0f;
 #pragma unroll
-    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + q * P + n] * kLog2e, g[n] = 0.0f;
-    float bias[EPT];
-    load_params<EPT>(a.bias == nullptr ? nullptr : a.bias + w.e0 + me.c, me.valid, bias);
-    const size_t row0 = (size_t)w.b * a.N, cfirst = row0 * a.ldc + (size_t)w.g * a.S + q * P;
-    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0;
-    for (int i = tiles - 1; i >= 0; --i) {
-        const int t = w.t0 + i * T;
-        const size_t r = row0 + t + me.t;
-        const int valid = t + me.t < w.end ? me.valid : 0;
-        const Piece<TT, EPT> dt = load_piece<TT, EPT>((const TT *)a.dt + r * a.lddt + w.e0 + me.c, valid);
-        const Piece<TT, EPT> dy = load_piece<TT, EPT>((const TT *)a.dy + r * a.E + w.e0 + me.c, valid);
-        Piece<TT, EPT> z{};
-        if (a.z != nullptr) z = load_piece<TT, EPT>((const TT *)a.z + r * a.ldz + w.e0 + me.c, valid);
-        __syncthreads();
+    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, g[n] = 0.0f;
+    const float bias = a.bias == nullptr ? 0.0f : a.bias[e];
+    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
+    Pairs<TT, NW, P> pairs(a, w, bc, last);
+    const int mine = last + q * K;
+    const size_t row = (size_t)w.b * a.N + mine;
+    const TT *pdt = (const TT *)a.dt + row * a.lddt + e, *pz = (const TT *)a.z + row * a.ldz + e, *pdy = (const TT *)a.dy + row * a.E + e;
+    const bool gated = a.z != nullptr;
+    struct Tile { Column<TT, K> dt, dy, z; } far, near;           // tiles i - 2 and i - 1
+    int there = w.end - mine, left = tiles;
+    auto fetch = [&](Tile &f) {                                   // the tiles from the last on
+        const int n = left > 0 ? there : 0;
+        f.dt.load(pdt, a.lddt, n), f.dy.load(pdy, a.E, n);
+        if (gated) f.z.load(pz, a.ldz, n);
+        pairs.fetch(left > 0 ? there + q * K : 0, -1);
+        pdt -= T * a.lddt, pdy -= (long)T * a.E, pz -= T * a.ldz, there += T, --left;
+    };
+    auto prepare = [&](const Tile &f, int i, int buf) {
+        pairs.park(buf);
 #pragma unroll
-        for (int k = 0; k < EPT; ++k) {
-            float d = dt.get(k) + bias[k], dv = dy.get(k);
+        for (int k = 0; k < K; ++k) {
+            float d = f.dt.get(k) + bias, dv = f.dy.get(k);
             if (a.softplus) d = softplus(d);
-            if (a.z != nullptr) dv *= z.get(k) * sigmoid(z.get(k));
-            in[me.t][me.c + k] = make_float2(t + me.t < w.end ? d : 0.0f, t + me.t < w.end ? dv : 0.0f);
+            if (gated) dv *= f.z.get(k) * sigmoid(f.z.get(k));
+            const bool real = w.t0 + i * T + q * K + k < w.end;
+            in[buf][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(real ? d : 0.0f, real ? dv : 0.0f);
         }
-        __syncthreads();
+    };
+    fetch(near);
+    fetch(far);
+    if (tiles > 0) prepare(near, tiles - 1, (tiles - 1) & 1);
+    __syncthreads();
+    for (int i = tiles - 1; i >= 0; --i) {
+        const int buf = i & 1;
+        near = far;
+        fetch(far);
+        if (i > 0) prepare(near, i - 1, buf ^ 1);
 #pragma unroll
         for (int j = T - 1; j >= 0; --j) {
-            const float2 v = in[j][lane];
-            const Row<TT> C = row_of<TT>(a.Ct, a.ldc, cfirst, t + j, w.end - 1);
+            const float2 v = in[buf][j / 2][lane][j % 2];
+            const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
             sum_d += v.x;
 #pragma unroll
-            for (int n = 0; n < P; ++n) g[n] = __builtin_amdgcn_exp2f(v.x * A[n]) * fmaf(word_value<TT, P>(C, n), v.y, g[n]);
+            for (int n = 0; n < P; ++n) g[n] = __builtin_amdgcn_exp2f(v.x * A[n]) * fmaf(p.C(n), v.y, g[n]);
         }
+        __syncthreads();
     }
     if (lane < w.channels) {
-        __builtin_memcpy(a.piece_h + state_at(a, w.b, a.pieces, w.piece, q, e), g, sizeof(g));
+        __builtin_memcpy(a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), g, sizeof(g));
         if (q == 0) a.piece_d[((size_t)w.b * a.pieces + w.piece) * a.E + e] = sum_d;
     }
 }
@@ -257,165 +352,188 @@ template <int K, int CTRL> __device__ __forceinline__ void fold_row(float *v, bo
 }
 
 // One tile after the other from the last to the first: the states of a tile are formed again from the kept state before
-// it and stay in registers (16 tokens x 4 states, and the decays), then the adjoint runs back over them.  dB and
-// dC are sums over channels, which are lanes: the 8 products of a token are folded over the wave as they appear.
-template <typename TT, int NW> __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(const ScanArgs a) {
-    using M = Mine<TT, NW>;
-    constexpr int EPT = M::EPT;
-    __shared__ float2 in[T][kLanes];                              // d, d x
-    __shared__ float in_v[T][kLanes];                             // dv
-    __shared__ float out[3][NW][T][kLanes];                       // g . B, sum A g a h, C . h
+// it and stay in registers (16 tokens x P states, and the decays), then the adjoint runs back over them.  dB and
+// dC are sums over channels, which are lanes: the 2 P products of a token are folded over the wave as they appear.
+// Between two barriers a wave prepares tile i - 1 and runs tile i; the second barrier only spans the reading of the
+// waves' partial sums, whose buffer does not fit twice.
+template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(const ScanArgs a) {
+    constexpr int K = T / NW;
+    __shared__ __align__(16) float bc[2][T][NW * P][2];
+    __shared__ __align__(16) float2 in[2][T / 2][kLanes][2];      // d, d x of two tokens
+    __shared__ __align__(16) float in_v[2][T / 2][kLanes][2];     // dv of two tokens
+    __shared__ __align__(16) float out[3][NW][NW][kLanes][K];     // g . B, sum A g a h, C . h
     const Where w(a);
-    const M me(w.channels);
-    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int e = w.e0 + min(lane, w.channels - 1);
+    const int lane = threadIdx.x % 64, q = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n0 = q * P;
+    const int e = w.e0 + min(lane, w.channels - 1);               // lanes without a channel repeat the last one's
     const bool live = lane < w.channels;
     float A[P], g[P], dA[P];
 #pragma unroll
-    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + q * P + n] * kLog2e, g[n] = dA[n] = 0.0f;
-    if (a.pieces > 1) __builtin_memcpy(g, a.piece_h + state_at(a, w.b, a.pieces, w.piece, q, e), sizeof(g));
-    else if (a.dh1 != nullptr) __builtin_memcpy(g, a.dh1 + ((size_t)w.b * a.E + e) * a.S + q * P, sizeof(g));
-    float bias[EPT], D[EPT], dD[EPT] = {}, db[EPT] = {};
-    load_params<EPT>(a.bias == nullptr ? nullptr : a.bias + w.e0 + me.c, me.valid, bias);
-    load_params<EPT>(a.D == nullptr ? nullptr : a.D + w.e0 + me.c, me.valid, D);
-    const size_t row0 = (size_t)w.b * a.N;
-    const size_t bfirst = row0 * a.ldb + (size_t)w.g * a.S + q * P, cfirst = row0 * a.ldc + (size_t)w.g * a.S + q * P;
-    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0;
+    for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, g[n] = dA[n] = 0.0f;
+    if (a.pieces > 1) __builtin_memcpy(g, a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), sizeof(g));
+    else if (a.dh1 != nullptr) __builtin_memcpy(g, a.dh1 + ((size_t)w.b * a.E + e) * a.S + n0, sizeof(g));
+    const float bias = a.bias == nullptr ? 0.0f : a.bias[e], D = a.D == nullptr ? 0.0f : a.D[e];
+    float dD = 0.0f, db = 0.0f;
+    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
+    Pairs<TT, NW, P> pairs(a, w, bc, last);
     const bool gated = a.z != nullptr;
-
-    Piece<TT, EPT> x, dt, z{}, dy;
-    auto fetch = [&](int t) {
-        const size_t r = row0 + t + me.t;
-        const int valid = t + me.t < w.end ? me.valid : 0;
-        x = load_piece<TT, EPT>((const TT *)a.x + r * a.ldx + w.e0 + me.c, valid);
-        dt = load_piece<TT, EPT>((const TT *)a.dt + r * a.lddt + w.e0 + me.c, valid);
-        dy = load_piece<TT, EPT>((const TT *)a.dy + r * a.E + w.e0 + me.c, valid);
-        if (gated) z = load_piece<TT, EPT>((const TT *)a.z + r * a.ldz + w.e0 + me.c, valid);
+    const int mine = last + q * K;                                // this thread's first token of the last tile
+    const size_t row = (size_t)w.b * a.N + mine;
+    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e, *pz = (const TT *)a.z + row * a.ldz + e;
+    const TT *pdy = (const TT *)a.dy + row * a.E + e;
+    size_t dense = row * a.E + e;                                 // of dx, ddt and dz
+    const float *pk = a.keep + state_at<P>(a, w.b, a.tiles, last / T, n0, e);
+    float *pbc = a.part_bc + (((size_t)w.block * a.B + w.b) * a.N + last) * (2 * NW * P) + n0;
+    struct Tile { Column<TT, K> x, dt, z, dy; } far, near;        // tiles i - 2 and i - 1
+    struct Ready { float d[K], slope[K], gate[K], x[K], z[K], dy[K]; } soon, cur;     // tiles i - 1 and i
+    int there = w.end - mine, left = tiles;
+    auto fetch = [&](Tile &f) {                                   // the tiles from the last on
+        const int n = left > 0 ? there : 0;
+        f.x.load(px, a.ldx, n), f.dt.load(pdt, a.lddt, n), f.dy.load(pdy, a.E, n);
+        if (gated) f.z.load(pz, a.ldz, n);
+        pairs.fetch(left > 0 ? there + q * K : 0, -1);
+        px -= T * a.ldx, pdt -= T * a.lddt, pz -= T * a.ldz, pdy -= (long)T * a.E, there += T, --left;
     };
-    if (tiles > 0) fetch(w.t0 + (tiles - 1) * T);
-    for (int i = tiles - 1; i >= 0; --i) {
-        const int t = w.t0 + i * T;
-        const bool real = t + me.t < w.end;
-        const Piece<TT, EPT> xt = x, zt = z, dyt = dy;
-        float d[EPT], slope[EPT], gate[EPT];
+    auto prepare = [&](const Tile &f, Ready &r, int i, int buf) {
+        pairs.park(buf);
 #pragma unroll
-        for (int k = 0; k < EPT; ++k) {
-            const float raw = dt.get(k) + bias[k];
-            d[k] = real ? (a.softplus ? softplus(raw) : raw) : 0.0f;
-            slope[k] = real ? (a.softplus ? sigmoid(raw) : 1.0f) : 0.0f;
-            gate[k] = sigmoid(zt.get(k));
-            const float dv = gated ? dyt.get(k) * zt.get(k) * gate[k] : dyt.get(k);
-            in[me.t][me.c + k] = make_float2(d[k], d[k] * xt.get(k));
-            in_v[me.t][me.c + k] = real ? dv : 0.0f;
+        for (int k = 0; k < K; ++k) {
+            // behind the sequence and in lanes without a channel: a step of zero, and nothing for any sum
+            const bool real = live && w.t0 + i * T + q * K + k < w.end;
+            const float raw = f.dt.get(k) + bias;
+            r.d[k] = real ? (a.softplus ? softplus(raw) : raw) : 0.0f;
+            r.slope[k] = real ? (a.softplus ? sigmoid(raw) : 1.0f) : 0.0f;
+            r.x[k] = real ? f.x.get(k) : 0.0f, r.dy[k] = real ? f.dy.get(k) : 0.0f;
+            r.z[k] = gated ? f.z.get(k) : 0.0f, r.gate[k] = sigmoid(r.z[k]);
+            const int t = q * K + k;
+            in[buf][t / 2][lane][t % 2] = make_float2(r.d[k], r.d[k] * r.x[k]);
+            in_v[buf][t / 2][lane][t % 2] = gated ? r.dy[k] * r.z[k] * r.gate[k] : r.dy[k];
         }
-        __syncthreads();
+    };
+    fetch(near);
+    fetch(far);
+    float start[P] = {};                                          // the kept state before the next tile
+    if (tiles > 0) {
+        __builtin_memcpy(start, pk, sizeof(start));
+        prepare(near, soon, tiles - 1, (tiles - 1) & 1);
+    }
+    __syncthreads();
+    for (int i = tiles - 1; i >= 0; --i) {
+        const int t = w.t0 + i * T, buf = i & 1;
+        cur = soon, near = far;
+        fetch(far);
         float h[T + 1][P], dec[T][P];
-        __builtin_memcpy(h[0], a.keep + state_at(a, w.b, a.tiles, t / T, q, e), sizeof(h[0]));
-        if (i > 0) fetch(t - T);
+#pragma unroll
+        for (int n = 0; n < P; ++n) h[0][n] = start[n];
+        pk -= (size_t)a.E * (NW * P);
+        if (i > 0) __builtin_memcpy(start, pk, sizeof(start));
+        if (i > 0) prepare(near, soon, i - 1, buf ^ 1);
 #pragma unroll
         for (int j = 0; j < T; ++j) {
-            const float2 v = in[j][lane];
-            const Row<TT> B = row_of<TT>(a.Bt, a.ldb, bfirst, t + j, w.end - 1);
+            const float2 v = in[buf][j / 2][lane][j % 2];
+            const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
 #pragma unroll
             for (int n = 0; n < P; ++n) {
                 dec[j][n] = __builtin_amdgcn_exp2f(v.x * A[n]);
-                h[j + 1][n] = fmaf(dec[j][n], h[j][n], v.y * word_value<TT, P>(B, n));
+                h[j + 1][n] = fmaf(dec[j][n], h[j][n], v.y * p.B(n));
             }
         }
-        float acc[2 * T];                                         // two registers a token, each a value per 16 lanes
+        constexpr int kHeld = P / 2;                              // registers a token's folded products take
+        float acc[kHeld * T], sum[3][K];
 #pragma unroll
         for (int j = T - 1; j >= 0; --j) {
-            const float2 v = in[j][lane];
-            const float dv = in_v[j][lane];
-            const Row<TT> B = row_of<TT>(a.Bt, a.ldb, bfirst, t + j, w.end - 1);
-            const Row<TT> C = row_of<TT>(a.Ct, a.ldc, cfirst, t + j, w.end - 1);
-            float gB = 0.0f, gA = 0.0f, y = 0.0f, bc[2 * P];
+            const float2 v = in[buf][j / 2][lane][j % 2];
+            const float dv = in_v[buf][j / 2][lane][j % 2];
+            const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
+            float gB = 0.0f, gA = 0.0f, y = 0.0f, prod[2 * P];
 #pragma unroll
             for (int n = 0; n < P; ++n) {
-                y = fmaf(word_value<TT, P>(C, n), h[j + 1][n], y);
-                g[n] = fmaf(word_value<TT, P>(C, n), dv, g[n]);
-                gB = fmaf(word_value<TT, P>(B, n), g[n], gB);
-                bc[n] = live ? g[n] * v.y : 0.0f;
-                bc[P + n] = live ? h[j + 1][n] * dv : 0.0f;
+                y = fmaf(p.C(n), h[j + 1][n], y);
+                g[n] = fmaf(p.C(n), dv, g[n]);
+                gB = fmaf(p.B(n), g[n], gB);
+                prod[n] = g[n] * v.y;
+                prod[P + n] = h[j + 1][n] * dv;
                 g[n] *= dec[j][n];                                // now the gradient for h_{t-1}
                 const float through = g[n] * h[j][n];
                 gA = fmaf(through, A[n], gA);
                 dA[n] = fmaf(through, v.x, dA[n]);
             }
-            out[0][q][j][lane] = gB;
-            out[1][q][j][lane] = gA;
-            if (gated) out[2][q][j][lane] = y;
-            fold32<P>(bc);
-            fold16<P / 2>(bc);
-            acc[2 * j] = bc[0], acc[2 * j + 1] = bc[1];
-        }
-        fold_row<T, 0x128>(acc, lane & 8);
-        fold_row<T / 2, 0x141>(acc, lane & 4);
-        fold_row<T / 4, 0x4e>(acc, lane & 2);
-        fold_row<T / 8, 0xb1>(acc, lane & 1);
-        // Which value a lane ends up with: register pair (2j, 2j + 1) held, by bits 5 and 4 of the lane, values
-        // {bc[4r + 2 bit4 + bit5]}; the folds chose r by bit 3 and the token by bits 2, 1, 0 of the lane and the register.
+            sum[0][j % K] = gB, sum[1][j % K] = gA, sum[2][j % K] = y;
+            if (j % K == 0) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int j = k * 8 + ((lane & 1) << 2) + (lane & 2) + ((lane & 4) >> 2);
-            const int value = ((lane & 8) >> 1) + ((lane & 16) >> 3) + ((lane & 32) >> 5);
-            if (t + j < w.end) {
-                const int which = value / P, n = q * P + value % P;
-                a.part_bc[((((size_t)w.block * a.B + w.b) * a.N + t + j) * 2 + which) * a.S + n] = acc[k];
+                for (int r = 0; r < 3; ++r)
+                    if (r < 2 || gated) __builtin_memcpy(__builtin_assume_aligned(out[r][q][j / K][lane], 4 * K), sum[r], sizeof(sum[r]));
+            }
+            fold32<P>(prod);
+            fold16<P / 2>(prod);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) acc[kHeld * j + r] = prod[r];
+        }
+        // Lanes that differ in bits 5 and 4 now hold different products: value 4 r + 2 bit4 + bit5 of a token's 2 P.  The
+        // folds within 16 lanes choose between the two halves r (P = 4) by bit 3, and between tokens by the rest.
+        fold_row<P * T / 4, 0x128>(acc, lane & 8);
+        fold_row<P * T / 8, 0x141>(acc, lane & 4);
+        fold_row<P * T / 16, 0x4e>(acc, lane & 2);
+        fold_row<P * T / 32, 0xb1>(acc, lane & 1);
+#pragma unroll
+        for (int k = 0; k < P * T / 32; ++k) {
+            const int low = ((lane & 1) << 2) + (lane & 2) + ((lane & 4) >> 2);
+            const int j = P == 4 ? k * 8 + low : 2 * low + ((lane & 8) >> 3);
+            const int value = (P == 4 ? (lane & 8) >> 1 : 0) + ((lane & 16) >> 3) + ((lane & 32) >> 5);
+            if (t + j < w.end) pbc[(2 * j + value / P) * (NW * P) + value % P] = acc[k];
+        }
+        pbc -= T * 2 * NW * P;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) sum[0][k] = sum[1][k] = sum[2][k] = 0.0f;
+#pragma unroll
+        for (int m = 0; m < NW; ++m) {
+#pragma unroll
+            for (int r = 0; r < 3; ++r) {
+                if (r == 2 && !gated) break;
+                float part[K];
+                __builtin_memcpy(part, out[r][m][q][lane], sizeof(part));
+#pragma unroll
+                for (int k = 0; k < K; ++k) sum[r][k] += part[k];
             }
         }
         __syncthreads();
-        if (real) {
-            float o[EPT], od[EPT], oz[EPT];
 #pragma unroll
-            for (int k = 0; k < EPT; ++k) {
-                float gB = 0.0f, gA = 0.0f, y = 0.0f;
-#pragma unroll
-                for (int m = 0; m < NW; ++m) {
-                    gB += out[0][m][me.t][me.c + k];
-                    gA += out[1][m][me.t][me.c + k];
-                    if (gated) y += out[2][m][me.t][me.c + k];
-                }
-                const float xv = xt.get(k), zv = zt.get(k), dyv = dyt.get(k), dv = gated ? dyv * zv * gate[k] : dyv;
-                o[k] = fmaf(d[k], gB, D[k] * dv);
-                od[k] = fmaf(xv, gB, gA * (1.0f / kLog2e)) * slope[k];
-                y = fmaf(D[k], xv, y);
-                oz[k] = dyv * y * gate[k] * fmaf(zv, 1.0f - gate[k], 1.0f);
-                dD[k] = fmaf(dv, xv, dD[k]);
-                db[k] += od[k];
+        for (int k = 0; k < K; ++k) {
+            const float gB = sum[0][k], gA = sum[1][k] * (1.0f / kLog2e), y = fmaf(D, cur.x[k], sum[2][k]);
+            const float dv = gated ? cur.dy[k] * cur.z[k] * cur.gate[k] : cur.dy[k];
+            const float ddt = fmaf(cur.x[k], gB, gA) * cur.slope[k];
+            dD = fmaf(dv, cur.x[k], dD), db += ddt;
+            if (live && t + q * K + k < w.end) {
+                const size_t at = dense + (size_t)k * a.E;
+                store_elem<false>((TT *)a.dx + at, fmaf(cur.d[k], gB, D * dv));
+                store_elem<false>((TT *)a.ddt + at, ddt);
+                if (gated) store_elem<false>((TT *)a.dz + at, cur.dy[k] * y * cur.gate[k] * fmaf(cur.z[k], 1.0f - cur.gate[k], 1.0f));
             }
-            const size_t at = (row0 + t + me.t) * a.E + w.e0 + me.c;
-            store_row<TT, EPT>((TT *)a.dx + at, me.valid, o);
-            store_row<TT, EPT>((TT *)a.ddt + at, me.valid, od);
-            if (gated) store_row<TT, EPT>((TT *)a.dz + at, me.valid, oz);
         }
+        dense -= (size_t)T * a.E;
     }
-    {   // rows behind the sequence
-        const float zero[EPT] = {};
-        for (int t = max(w.end, w.t0) + me.t; t < w.t1; t += T) {
-            const size_t at = (row0 + t) * a.E + w.e0 + me.c;
-            store_row<TT, EPT>((TT *)a.dx + at, me.valid, zero);
-            store_row<TT, EPT>((TT *)a.ddt + at, me.valid, zero);
-            if (gated) store_row<TT, EPT>((TT *)a.dz + at, me.valid, zero);
+    if (live) {                                                   // rows behind the sequence
+        for (int t = max(w.end, w.t0) + q; t < w.t1; t += NW) {
+            const size_t at = ((size_t)w.b * a.N + t) * a.E + e;
+            store_elem<false>((TT *)a.dx + at, 0.0f);
+            store_elem<false>((TT *)a.ddt + at, 0.0f);
+            if (gated) store_elem<false>((TT *)a.dz + at, 0.0f);
         }
     }
     float *sums = a.part + ((size_t)w.b * a.pieces + w.piece) * a.E * (a.S + 2);
     if (live) {
-        __builtin_memcpy(sums + (size_t)e * a.S + q * P, dA, sizeof(dA));
-        if (a.dh0 != nullptr && w.piece == 0) __builtin_memcpy(a.dh0 + ((size_t)w.b * a.E + e) * a.S + q * P, g, sizeof(g));
+        __builtin_memcpy(sums + (size_t)e * a.S + n0, dA, sizeof(dA));
+        if (a.dh0 != nullptr && w.piece == 0) __builtin_memcpy(a.dh0 + ((size_t)w.b * a.E + e) * a.S + n0, g, sizeof(g));
     }
-    // dD and the bias's gradient: over the 16 tokens of the tile's rows
-    float *red = &out[0][0][0][0];                                // [2][T][64]
+    // dD and the bias's gradient: over the waves, which had different tokens
+    float(*red)[NW][kLanes] = reinterpret_cast<float(*)[NW][kLanes]>(&out[0][0][0][0][0]);
+    red[0][q][lane] = dD, red[1][q][lane] = db;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < EPT; ++k) red[me.t * kLanes + me.c + k] = dD[k], red[(T + me.t) * kLanes + me.c + k] = db[k];
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * kLanes; c += 64 * NW) {
-        const int ch = c % kLanes, which = c / kLanes;
+    if (q < 2 && live) {
         float v = 0.0f;
 #pragma unroll
-        for (int j = 0; j < T; ++j) v += red[(which * T + j) * kLanes + ch];
-        if (ch < w.channels) sums[(size_t)a.E * (a.S + which) + w.e0 + ch] = v;
+        for (int m = 0; m < NW; ++m) v += red[q][m][lane];
+        sums[(size_t)a.E * (a.S + q) + e] = v;
     }
 }
 
@@ -475,11 +593,12 @@ template <typename TT, int S> __global__ __launch_bounds__(256) void scan_step_k
         if ((dtype) == 0) { using TT = float; __VA_ARGS__; }                  \
         else { using TT = bf16_t; __VA_ARGS__; }                              \
     } while (0)
+// waves of a workgroup and states of a wave
 #define LA_SCAN_DISPATCH(S, dtype, ...)                                       \
     do {                                                                      \
-        if ((S) == 8) { constexpr int NW = 2; LA_SCAN_T(dtype, __VA_ARGS__); }       \
-        else if ((S) == 16) { constexpr int NW = 4; LA_SCAN_T(dtype, __VA_ARGS__); } \
-        else { constexpr int NW = 8; LA_SCAN_T(dtype, __VA_ARGS__); }         \
+        if ((S) == 8) { constexpr int NW = 4, P = 2; LA_SCAN_T(dtype, __VA_ARGS__); }       \
+        else if ((S) == 16) { constexpr int NW = 8, P = 2; LA_SCAN_T(dtype, __VA_ARGS__); } \
+        else { constexpr int NW = 8, P = 4; LA_SCAN_T(dtype, __VA_ARGS__); }  \
     } while (0)
 
 unsigned blocks_for(long n) { return (unsigned)((n + 255) / 256 < (1 << 20) ? (n + 255) / 256 : 1 << 20); }
@@ -492,7 +611,7 @@ void scan_cut(ScanArgs &a) {
     a.tiles = (a.N + T - 1) / T;
     const long whole = (long)a.B * scan_blocks(a.E, a.G);
     long pieces = 1;
-    if (whole < 160) pieces = (512 + whole - 1) / whole;
+    if (whole < 160) pieces = (1024 + whole - 1) / whole;
     const long most = a.tiles / 4 > 1 ? a.tiles / 4 : 1;          // no piece shorter than 64 tokens
     if (pieces > most) pieces = most;
     a.piece_tiles = (int)((a.tiles + pieces - 1) / pieces);
@@ -503,10 +622,10 @@ hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s) {
     const unsigned grid = (unsigned)((long)a.B * a.pieces * scan_blocks(a.E, a.G));
     LA_SCAN_DISPATCH(a.S, dtype, {
         if (a.pieces > 1) {
-            scan_fwd_kernel<TT, NW, true><<<grid, 64 * NW, 0, s>>>(a);
+            scan_fwd_kernel<TT, NW, P, true><<<grid, 64 * NW, 0, s>>>(a);
             scan_pieces_kernel<false><<<blocks_for((long)a.B * a.E * a.S), 256, 0, s>>>(a);
         }
-        scan_fwd_kernel<TT, NW, false><<<grid, 64 * NW, 0, s>>>(a);
+        scan_fwd_kernel<TT, NW, P, false><<<grid, 64 * NW, 0, s>>>(a);
     });
     return hipGetLastError();
 }
@@ -515,12 +634,12 @@ hipError_t launch_scan_bwd(const ScanArgs &a, int dtype, hipStream_t s) {
     const unsigned grid = (unsigned)((long)a.B * a.pieces * scan_blocks(a.E, a.G));
     LA_SCAN_DISPATCH(a.S, dtype, {
         if (a.pieces > 1) {
-            scan_local_bwd_kernel<TT, NW><<<grid, 64 * NW, 0, s>>>(a);
+            scan_local_bwd_kernel<TT, NW, P><<<grid, 64 * NW, 0, s>>>(a);
             scan_pieces_kernel<true><<<blocks_for((long)a.B * a.E * a.S), 256, 0, s>>>(a);
         }
-        scan_bwd_kernel<TT, NW><<<grid, 64 * NW, 0, s>>>(a);
-        scan_sum_bc_kernel<TT><<<blocks_for((long)a.B * a.N * a.G * 2 * a.S), 256, 0, s>>>(a);
+        scan_bwd_kernel<TT, NW, P><<<grid, 64 * NW, 0, s>>>(a);
     });
+    LA_SCAN_T(dtype, scan_sum_bc_kernel<TT><<<blocks_for((long)a.B * a.N * a.G * 2 * a.S), 256, 0, s>>>(a));
     return hipGetLastError();
 }
 
