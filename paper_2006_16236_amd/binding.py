@@ -123,13 +123,17 @@ def _bind_call():
     names what is wrong with it.  A build without torch's headers has no _call.so: all calls go that way."""
     if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_call.so")):
         class c:
-            fwd = bwd = step = staticmethod(lambda *args: None)
+            fwd = bwd = step = norm_fwd = norm_bwd = conv_fwd = conv_bwd = conv_step = scan_fwd = scan_bwd = scan_step = \
+                staticmethod(lambda *args: None)
         return c
     from . import _call as c
     names = ["la_recurrent_step"]
     names += [f"la_{kind}_{way}{layout}" for way in ("fwd", "bwd") for kind in ("causal", "global") for layout in ("", "_bnhd")]
     names += [f"la_{kind}_{way}_workspace" for way in ("fwd", "bwd") for kind in ("causal", "global")]
     c.bind([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names])
+    names = ["la_norm_fwd", "la_norm_bwd_workspace", "la_norm_bwd", "la_conv_fwd", "la_conv_bwd_workspace", "la_conv_bwd", "la_conv_step",
+             "la_scan_fwd_workspace", "la_scan_fwd", "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step"]
+    c.bind_layer([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names])
     return c
 
 

@@ -4,13 +4,16 @@ convolution and the selective state space scan of include/la.h.
 As in binding.py this is argument checking and marshalling only.  Inputs called rows [B, N, E] may be parts of a
 wider tensor (the half of a projection's output): their last dimension dense, their tokens at one distance.
 Everything else is dense.  A call runs on its tensors' device, on `stream` or that device's current stream.
+
+Each function first offers the call to its native counterpart (csrc/la_call.cpp), which takes it where all is as
+expected and the tensors are on the current device; otherwise it goes through the checks here, which name what is wrong.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as _b
-from .binding import LA_SCAN_KEEP, LA_SCAN_SOFTPLUS, _bytes, _check, _lib, _like
+from .binding import LA_SCAN_KEEP, LA_SCAN_SOFTPLUS, _bytes, _call, _check, _lib, _like
 
 _F32 = torch.float32
 _CODES = {torch.float32: _b.LA_F32, torch.bfloat16: _b.LA_BF16}
@@ -96,6 +99,9 @@ def la_norm_bwd_workspace(rows, E, dtype_code=_b.LA_F32) -> int:
 def la_norm_fwd(x, gamma, beta, y, mean=None, rstd=None, r=None, s=None, eps=1e-5, stream=None):
     """y = layer norm of s = x + r over the last dimension of x [..., E]; gamma, beta [E] fp32 or None.  s: where
     the sum goes (only with r); mean, rstd [...] fp32: what la_norm_bwd needs."""
+    took = _call.norm_fwd(x, gamma, beta, y, mean, rstd, r, s, eps) if stream is None else None
+    if took is not None:
+        return _check(took, "la_norm_fwd")
     t, shape, dt, dev = _code("x", x), x.shape, x.dtype, x.device
     if len(shape) < 1:
         raise ValueError("x must have at least one dimension")
@@ -118,6 +124,11 @@ def la_norm_fwd(x, gamma, beta, y, mean=None, rstd=None, r=None, s=None, eps=1e-
 def la_norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ds=None, ws=None, stream=None):
     """dx (the gradient of x and of r), dgamma, dbeta from dy; s: what was normalised; ds: the gradient of the
     sum from elsewhere.  Returns the workspace it used (None if it needed none)."""
+    took = _call.norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma, dbeta, ds, ws) if stream is None else None
+    if took is not None:
+        if type(took) is int:
+            _check(took, "la_norm_bwd")
+        return took
     t, shape, dt, dev = _code("s", s), s.shape, s.dtype, s.device
     if len(shape) < 1:
         raise ValueError("s must have at least one dimension")
@@ -160,6 +171,9 @@ def _conv_checks(x, w, bias, n):
 def la_conv_fwd(x, w, bias, y, x0=None, x1=None, lengths=None, silu=True, stream=None):
     """Causal convolution of x [B, N, E] with w [E, W] fp32 and bias [E] or None into y; x0, x1 [B, W-1, E]: the rows
     before the first token and the last ones; lengths [B] int32."""
+    took = _call.conv_fwd(x, w, bias, y, x0, x1, lengths, silu) if stream is None else None
+    if took is not None:
+        return _check(took, "la_conv_fwd")
     t, dt, dev, (B, N, E), W = _conv_checks(x, w, bias, 3)
     ldx = _rows("x", x, (B, N, E), dt, dev)
     _like("y", y, (B, N, E), dt, dev)
@@ -174,6 +188,11 @@ def la_conv_bwd(x, w, bias, dy, dx, dw=None, db=None, x0=None, dx1=None, dx0=Non
                 stream=None):
     """dx, dw, db, dx0 of la_conv_fwd from dy and dx1, the gradient of the rows handed on.  Returns the workspace
     it used (None if it needed none)."""
+    took = _call.conv_bwd(x, w, bias, dy, dx, dw, db, x0, dx1, dx0, lengths, silu, ws) if stream is None else None
+    if took is not None:
+        if type(took) is int:
+            _check(took, "la_conv_bwd")
+        return took
     t, dt, dev, (B, N, E), W = _conv_checks(x, w, bias, 3)
     ldx = _rows("x", x, (B, N, E), dt, dev)
     _like("dy", dy, (B, N, E), dt, dev)
@@ -193,6 +212,9 @@ def la_conv_bwd(x, w, bias, dy, dx, dw=None, db=None, x0=None, dx1=None, dx0=Non
 
 def la_conv_step(x, w, bias, state, y, silu=True, stream=None):
     """One token of every sequence: x, y [B, E]; state [B, W-1, E] holds the rows before it and is moved on."""
+    took = _call.conv_step(x, w, bias, state, y, silu) if stream is None else None
+    if took is not None:
+        return _check(took, "la_conv_step")
     t, dt, dev, (B, E), W = _conv_checks(x, w, bias, 2)
     _like("x", x, (B, E), dt, dev)
     _like("y", y, (B, E), dt, dev)
@@ -248,6 +270,11 @@ def la_scan_fwd(x, dt, A, Bt, Ct, y, D=None, z=None, dt_bias=None, h0=None, h1=N
     """Selective scan of x, dt, z [B, N, E] with Bt, Ct [B, N, G, S], A [E, S], D and dt_bias [E] fp32 into y; h0, h1
     [B, E, S] fp32: the states before and after; lengths [B] int32.  Returns the workspace it used; with
     keep=True it holds what la_scan_bwd starts from (fwd_ws)."""
+    took = _call.scan_fwd(x, dt, A, Bt, Ct, y, D, z, dt_bias, h0, h1, lengths, softplus, keep, ws) if stream is None else None
+    if took is not None:
+        if type(took) is int:
+            _check(took, "la_scan_fwd")
+        return took
     k = _Scan(x, dt, A, Bt, Ct, D, z, dt_bias, lengths)
     _like("y", y, k.rows, k.dtype, k.dev)
     k.states(h0=h0, h1=h1)
@@ -264,6 +291,11 @@ def la_scan_bwd(x, dt, A, Bt, Ct, dy, dx, ddt, dA, dB, dC, D=None, z=None, dt_bi
     """The gradients of la_scan_fwd from dy [B, N, E] and dh1 [B, E, S], the gradient of the state handed on.  fwd_ws: the
     workspace of la_scan_fwd(keep=True) on the same inputs (None: its states are formed again).  Returns the
     workspace it used."""
+    took = _call.scan_bwd(x, dt, A, Bt, Ct, dy, dx, ddt, dA, dB, dC, D, z, dt_bias, dD, dz, ddt_bias, h0, dh1, dh0, lengths, softplus, fwd_ws, ws) if stream is None else None
+    if took is not None:
+        if type(took) is int:
+            _check(took, "la_scan_bwd")
+        return took
     k = _Scan(x, dt, A, Bt, Ct, D, z, dt_bias, lengths)
     for name, v in (("dy", dy), ("dx", dx), ("ddt", ddt)):
         _like(name, v, k.rows, k.dtype, k.dev)
@@ -294,6 +326,9 @@ def la_scan_bwd(x, dt, A, Bt, Ct, dy, dx, ddt, dA, dB, dC, D=None, z=None, dt_bi
 
 def la_scan_step(x, dt, A, Bt, Ct, h, y, D=None, z=None, dt_bias=None, softplus=True, stream=None):
     """One token of every sequence: x, dt, z, y [B, E]; Bt, Ct [B, G, S]; h [B, E, S] fp32, updated in place."""
+    took = _call.scan_step(x, dt, A, Bt, Ct, h, y, D, z, dt_bias, softplus) if stream is None else None
+    if took is not None:
+        return _check(took, "la_scan_step")
     t, dtype, dev = _code("x", x), x.dtype, x.device
     B, E = _dims("x", x, 2)
     if not isinstance(Bt, torch.Tensor) or Bt.dim() != 3:
