@@ -11,6 +11,7 @@ namespace la {
 namespace {
 
 constexpr int kSumSlices = 16;
+constexpr int kBwdThreads = 512, kBwdGroups = 512;
 constexpr long kMaxGrid = 1 << 20;       // workgroups of a launch; more rows go round again
 
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ part, long rows, const SumTargets out) {
@@ -111,18 +112,14 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? 
 }
 
 // xhat = (s - mean) rstd, g = dy gamma, dx = rstd (g - mean(g) - xhat mean(g xhat)) + ds; a workgroup takes every
-// gridDim-th group of rows and keeps its part of dgamma = sum dy xhat, dbeta = sum dy in registers.
-template <typename T, int TPR, int NV> __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormArgs a) {
-    constexpr int V = 16 / sizeof(T), kRows = 1024 / TPR;
-    __shared__ float red[2 * 1024 / kWave];
-    extern __shared__ float cols[];          // [2][E], kRows > 1 only
+// gridDim-th set of rows and keeps its part of dgamma = sum dy xhat, dbeta = sum dy in registers.  Up to 32 elements a lane
+// (bf16 rows of one wave: 64), so that most rows belong to one wave and the loop over rows has no barrier.
+template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const NormArgs a) {
+    constexpr int V = 16 / sizeof(T), kRows = kBwdThreads / TPR, kHalf = kRows > 1 ? kRows / 2 : 1, kCols = NV * V;
+    __shared__ float red[2 * kBwdThreads / kWave];
+    __shared__ float part[kHalf][kCols][TPR];
     const int E = a.E, l = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    float dg[NV][V] = {}, db[NV][V] = {}, gamma[NV][V];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int e = (j * TPR + l) * V;
-        load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, gamma[j], 1.0f);
-    }
+    float dg[NV][V] = {}, db[NV][V] = {};
     for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
         const long row = first + slot;
         const bool live = row < a.rows;
@@ -137,9 +134,11 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(1024) void n
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            float gamma[V];
+            load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + (j * TPR + l) * V, E - (j * TPR + l) * V, gamma, 1.0f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float xhat = (s[j].get(i) - mean) * rstd, dy = d[j].get(i), g = dy * gamma[j][i];
+                const float xhat = (s[j].get(i) - mean) * rstd, dy = d[j].get(i), g = dy * gamma[i];
                 s1 += g;
                 s2 = fmaf(g, xhat, s2);
                 dg[j][i] = fmaf(dy, xhat, dg[j][i]);
@@ -161,53 +160,48 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(1024) void n
         for (int j = 0; j < NV; ++j) {
             const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
             const size_t at = (size_t)row * E + e;
+            float gamma[V], o[V];
+            load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, gamma, 1.0f);
             Piece<T, V> ds{};
             if (a.r != nullptr) ds = load_piece<T, V>((const T *)a.r + at, valid);
-            float o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float xhat = (s[j].get(i) - mean) * rstd, g = d[j].get(i) * gamma[j][i];
+                const float xhat = (s[j].get(i) - mean) * rstd, g = d[j].get(i) * gamma[i];
                 o[i] = fmaf(rstd, g - fmaf(xhat, s2, s1), a.r != nullptr ? ds.get(i) : 0.0f);
             }
             store_row<T, V>((T *)a.y + at, valid, o);
         }
     }
     if (a.part == nullptr) return;
-    // the rows' slots one after the other (a fixed order), each lane on its own columns
-    if constexpr (kRows > 1) {
-        for (int k = 0; k < kRows; ++k) {
-            if (slot == k) {
+    // the row slots' sums, halving their number with every step
+    auto gather = [&](float(&v)[NV][V]) {
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
+        for (int half = kRows / 2; half >= 1; half /= 2) {
+            __syncthreads();
+            if (slot >= half && slot < 2 * half) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int e = (j * TPR + l) * V + i;
-                        if (e < E) {
-                            cols[e] = k == 0 ? dg[j][i] : cols[e] + dg[j][i];
-                            cols[E + e] = k == 0 ? db[j][i] : cols[E + e] + db[j][i];
-                        }
-                    }
-                }
+                for (int c = 0; c < kCols; ++c) part[slot - half][c][l] = v[c / V][c % V];
             }
             __syncthreads();
-        }
-        for (int c = threadIdx.x; c < 2 * E; c += 1024) a.part[(size_t)blockIdx.x * 2 * E + c] = cols[c];
-    } else {
+            if (slot < half) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int e = (j * TPR + l) * V + i;
-                if (e < E) {
-                    a.part[(size_t)blockIdx.x * 2 * E + e] = dg[j][i];
-                    a.part[(size_t)blockIdx.x * 2 * E + E + e] = db[j][i];
-                }
+                for (int c = 0; c < kCols; ++c) v[c / V][c % V] += part[slot][c][l];
             }
         }
+    };
+    gather(dg);
+    gather(db);
+    if (slot != 0) return;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (j * TPR + l) * V;
+        store_row<float, V>(a.part + (size_t)blockIdx.x * 2 * E + e, E - e, dg[j]);
+        store_row<float, V>(a.part + (size_t)blockIdx.x * 2 * E + E + e, E - e, db[j]);
     }
 }
 
 int lanes_of(int E) { return E <= 1024 ? 64 : E <= 4096 ? 256 : 1024; }
+int lanes_of_bwd(int E) { return E <= 2048 ? 64 : E <= 8192 ? 256 : 512; }
 
 }  // namespace
 
@@ -218,8 +212,8 @@ hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, 
 }
 
 int norm_groups(int rows, int E) {
-    const int per = 1024 / lanes_of(E);
-    const long sets = ((long)rows + per - 1) / per, turns = (sets + 255) / 256;     // equal shares for up to 256 workgroups
+    const int per = kBwdThreads / lanes_of_bwd(E);
+    const long sets = ((long)rows + per - 1) / per, turns = (sets + kBwdGroups - 1) / kBwdGroups;      // equal shares
     return (int)((sets + turns - 1) / turns);
 }
 
@@ -251,9 +245,32 @@ hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
 }
 
 hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
-    const int groups = norm_groups(a.rows, a.E);
-#define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, 1024, TPR < 1024 ? 2 * a.E * sizeof(float) : 0, s>>>(a)
-    LA_NORM_DISPATCH(LA_KERNEL);
+    const int groups = norm_groups(a.rows, a.E), tpr = lanes_of_bwd(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);
+#define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, kBwdThreads, 0, s>>>(a)
+    if (dtype == 0) {
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(float, 64, 1);
+            else if (nv == 2) LA_KERNEL(float, 64, 2);
+            else if (nv <= 4) LA_KERNEL(float, 64, 4);
+            else LA_KERNEL(float, 64, 8);
+        } else if (tpr == 256) {
+            if (nv <= 4) LA_KERNEL(float, 256, 4);
+            else LA_KERNEL(float, 256, 8);
+        } else {
+            LA_KERNEL(float, 512, 8);
+        }
+    } else {
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
+            else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);
+            else LA_KERNEL(bf16_t, 64, 4);
+        } else if (tpr == 256) {
+            if (nv <= 2) LA_KERNEL(bf16_t, 256, 2);
+            else LA_KERNEL(bf16_t, 256, 4);
+        } else {
+            LA_KERNEL(bf16_t, 512, 4);
+        }
+    }
 #undef LA_KERNEL
     return hipGetLastError();
 }
