@@ -166,9 +166,9 @@ struct ScanArgs {
     int B, N, E, G, S, tiles, pieces, piece_tiles;
     bool softplus;
 };
-// channel blocks of all groups; pieces a sequence is cut into (piece_tiles tiles each)
+// channel blocks of all groups; pieces that a pass cuts a sequence into (piece_tiles tiles each)
 int scan_blocks(int E, int G);
-void scan_cut(ScanArgs &a);
+void scan_cut(ScanArgs &a, bool backward);
 // the states before each piece (pieces > 1), then outputs, kept states and the final state; y NULL: kept states only
 hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s);
 hipError_t launch_scan_bwd(const ScanArgs &a, int dtype, hipStream_t s);

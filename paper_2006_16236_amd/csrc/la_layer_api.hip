@@ -50,27 +50,35 @@ int scan_sizes(int B, int N, int E, int G, int S, la_dtype t, int flags) {
     if ((double)B * N * G * S >= 68719476736.0 || (double)G * S >= 2147483648.0) return LA_ERR_SHAPE;
     return LA_OK;
 }
-// a scan's sizes, cut into pieces, and the parts of its workspace
+// a scan's sizes, and the parts of its workspace.  Each pass has its own cut; what the forward keeps does not depend on it.
 struct Scan {
     la::ScanArgs a{};
-    size_t keep, piece_h, piece_d, part_bc, part;
+    size_t states, keep, part_bc;
     Scan(int B, int N, int E, int G, int S) {
         a.B = B, a.N = N, a.E = E, a.G = G, a.S = S;
-        la::scan_cut(a);
-        const size_t states = (size_t)B * E * S * sizeof(float);
+        la::scan_cut(a, false);
+        states = (size_t)B * E * S * sizeof(float);
         keep = align256(states * a.tiles);
-        piece_h = a.pieces > 1 ? align256(states * a.pieces) : 0;
-        piece_d = a.pieces > 1 ? align256((size_t)B * a.pieces * E * sizeof(float)) : 0;
         part_bc = align256((size_t)la::scan_blocks(E, G) * B * N * 2 * S * sizeof(float));
-        part = align256((size_t)B * a.pieces * E * (S + 2) * sizeof(float));
     }
-    // the kept states come first: the backward finds them whatever the cut
-    size_t fwd_bytes(int flags) const { return (flags & LA_SCAN_KEEP ? keep : 0) + piece_h + piece_d; }
-    size_t bwd_bytes(int flags) const { return (flags & LA_SCAN_KEEP ? 0 : keep) + piece_h + piece_d + part_bc + part; }
+    size_t pieces_bytes() const {
+        if (a.pieces < 2) return 0;
+        return align256(states * a.pieces) + align256((size_t)a.B * a.pieces * a.E * sizeof(float));
+    }
+    size_t part_bytes() const { return align256((size_t)a.B * a.pieces * a.E * (a.S + 2) * sizeof(float)); }
     void carve_pieces(Carver &cv) {
         if (a.pieces < 2) return;
-        a.piece_h = static_cast<float *>(cv.take(piece_h));
-        a.piece_d = static_cast<float *>(cv.take(piece_d));
+        a.piece_h = static_cast<float *>(cv.take(states * a.pieces));
+        a.piece_d = static_cast<float *>(cv.take((size_t)a.B * a.pieces * a.E * sizeof(float)));
+    }
+    // the kept states come first: the backward finds them at the workspace's start
+    size_t fwd_bytes(int flags) const { return (flags & LA_SCAN_KEEP ? keep : 0) + pieces_bytes(); }
+    // without the forward's states these are formed here, by a forward whose pieces' states share the backward's room
+    size_t bwd_bytes(int flags) const {
+        Scan back = *this;
+        la::scan_cut(back.a, true);
+        const size_t mine = back.pieces_bytes(), rebuilt = flags & LA_SCAN_KEEP ? 0 : pieces_bytes();
+        return (flags & LA_SCAN_KEEP ? 0 : keep) + (mine > rebuilt ? mine : rebuilt) + part_bc + back.part_bytes();
     }
 };
 bool bad_rows(int ld, int width) { return ld < width; }
@@ -253,15 +261,25 @@ int la_scan_bwd(const void *x, int ldx, const void *dt, int lddt, const void *z,
     a.ldx = ldx, a.lddt = lddt, a.ldz = ldz, a.ldb = ldb, a.ldc = ldc;
     a.softplus = (flags & LA_SCAN_SOFTPLUS) != 0;
     Carver cv{static_cast<char *>(ws), 0};
-    if (fwd_ws != nullptr) a.keep = const_cast<float *>(static_cast<const float *>(fwd_ws));
-    else a.keep = static_cast<float *>(cv.take(k.keep));
-    k.carve_pieces(cv);
-    a.part_bc = static_cast<float *>(cv.take(k.part_bc));
-    a.part = static_cast<float *>(cv.take(k.part));
     hipStream_t q = static_cast<hipStream_t>(stream);
-    int done = LA_OK;
-    if (fwd_ws == nullptr) done = hip_status(la::launch_scan_fwd(a, t, q));       // no outputs but the states before each tile
-    if (done == LA_OK) done = hip_status(la::launch_scan_bwd(a, t, q));
+    if (fwd_ws != nullptr) {
+        a.keep = const_cast<float *>(static_cast<const float *>(fwd_ws));
+    } else {
+        a.keep = static_cast<float *>(cv.take(k.keep));
+        Carver shared = cv;
+        k.carve_pieces(shared);
+        const int done = hip_status(la::launch_scan_fwd(a, t, q));                 // no outputs but the states before each tile
+        if (done != LA_OK) return done;
+    }
+    const size_t forward = fwd_ws != nullptr ? 0 : k.pieces_bytes();
+    la::scan_cut(a, true);
+    const size_t mine = k.pieces_bytes();
+    Carver pieces = cv;
+    k.carve_pieces(pieces);
+    cv.off += mine > forward ? mine : forward;
+    a.part_bc = static_cast<float *>(cv.take(k.part_bc));
+    a.part = static_cast<float *>(cv.take(k.part_bytes()));
+    const int done = hip_status(la::launch_scan_bwd(a, t, q));
     if (done != LA_OK) return done;
     return hip_status(la::launch_sum_rows(a.part, (long)B * a.pieces, {{dA, dD, ddt_bias}, {(long)E * S, E, E}}, q));
 }

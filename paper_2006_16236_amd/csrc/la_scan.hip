@@ -13,6 +13,8 @@
 //   tile of 16 tokens at a time, and handed over through LDS; the waves' partial C . h come back the same way.
 // * Sequences too few to fill the machine are cut into pieces: the state each piece adds from zero, a scan over the
 //   pieces (a piece decays as exp(A sum d)), then the pass itself from the right states.
+#include <type_traits>
+
 #include "la_layer.h"
 
 namespace la {
@@ -48,19 +50,12 @@ template <> struct Raw<float> { using type = float; };
 template <> struct Raw<bf16_t> { using type = uint16_t; };
 template <typename TT, int K> struct Column {
     typename Raw<TT>::type v[K];
-    // p: the first token's element; tokens [0, n) are there (n is the same in all lanes)
-    __device__ __forceinline__ void load(const TT *p, long ld, int n) {
+    // the K tokens from t on of a piece whose first element is *p; tokens behind the last one repeat it.  (No branch: where
+    // two ways of loading met, the loads would be waited for.)
+    __device__ __forceinline__ void load(const TT *p, unsigned ld, int t, int last) {
         const auto *r = reinterpret_cast<const typename Raw<TT>::type *>(p);
-        if (n >= K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] = r[k * ld];
-        } else {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                v[k] = 0;
-                if (k < n) v[k] = r[k * ld];
-            }
-        }
+        for (int k = 0; k < K; ++k) v[k] = r[(uint64_t)(unsigned)min(t + k, last) * ld];
     }
     __device__ __forceinline__ float get(int k) const {
         if constexpr (sizeof(TT) == 2) return __uint_as_float((uint32_t)v[k] << 16);
@@ -78,32 +73,28 @@ template <int P> __device__ __forceinline__ size_t state_at(const ScanArgs &a, i
 template <typename TT, int NW, int P> struct Pairs {
     static constexpr int S = NW * P, kEach = 2 * T * S / (64 * NW);        // T * S / 32 / NW: 1 or 2
     float (*lds)[T][S][2];
-    const TT *from;                  // this thread's first value of the next tile
-    long ld;
-    typename Raw<TT>::type far[kEach], near[kEach];
+    const TT *from;                  // this thread's value of the piece's first token
+    unsigned ld;
+    typename Raw<TT>::type held[2][kEach];
     int t[kEach], which, n;
     // values v = thread + 64 NW i of a tile: token v / (2 S), B before C
-    __device__ __forceinline__ Pairs(const ScanArgs &a, const Where &w, float (*l)[T][S][2], int first) : lds(l) {
+    __device__ __forceinline__ Pairs(const ScanArgs &a, const Where &w, float (*l)[T][S][2]) : lds(l) {
         const int c = threadIdx.x % (2 * S);
         which = c / S, n = c % S, ld = which ? a.ldc : a.ldb;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) t[i] = (threadIdx.x + 64 * NW * i) / (2 * S);
-        from = (const TT *)(which ? a.Ct : a.Bt) + ((size_t)w.b * a.N + first) * ld + (size_t)w.g * S + n;
+        from = (const TT *)(which ? a.Ct : a.Bt) + ((size_t)w.b * a.N + w.t0) * ld + (size_t)w.g * S + n;
     }
-    // tokens [0, there) of the tile belong to the sequence; step: tiles from this to the next one fetched, 1 or -1
-    __device__ __forceinline__ void fetch(int there, int step) {
+    __device__ __forceinline__ void fetch(int slot, int i, int last) {     // tile i
+        const auto *r = reinterpret_cast<const typename Raw<TT>::type *>(from);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            near[i] = far[i], far[i] = 0;
-            if (t[i] < there) far[i] = reinterpret_cast<const typename Raw<TT>::type *>(from)[t[i] * ld];
-        }
-        from += step * T * ld;
+        for (int k = 0; k < kEach; ++k) held[slot][k] = r[(uint64_t)(unsigned)min(i * T + t[k], last) * ld];
     }
-    __device__ __forceinline__ void park(int buf) const {                  // the tile fetched before the last fetch
+    __device__ __forceinline__ void park(int slot) const {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            if constexpr (sizeof(TT) == 2) lds[buf][t[i]][n][which] = __uint_as_float((uint32_t)near[i] << 16);
-            else lds[buf][t[i]][n][which] = near[i];
+        for (int k = 0; k < kEach; ++k) {
+            if constexpr (sizeof(TT) == 2) lds[slot][t[k]][n][which] = __uint_as_float((uint32_t)held[slot][k] << 16);
+            else lds[slot][t[k]][n][which] = held[slot][k];
         }
     }
 };
@@ -140,84 +131,92 @@ template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(
         else if (a.h0 != nullptr) __builtin_memcpy(h, a.h0 + ((size_t)w.b * a.E + e) * a.S + n0, sizeof(h));
     }
     const float bias = a.bias == nullptr ? 0.0f : a.bias[e], D = a.D == nullptr ? 0.0f : a.D[e];
-    Pairs<TT, NW, P> pairs(a, w, bc, w.t0);
-    const int mine = w.t0 + q * K;                                // this thread's first token
-    const size_t row = (size_t)w.b * a.N + mine;
-    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e;
-    const TT *pz = (const TT *)a.z + row * a.ldz + e;
-    TT *py = (TT *)a.y + row * a.E + e;
-    float *pk = a.keep + state_at<P>(a, w.b, a.tiles, w.t0 / T, n0, e);
+    Pairs<TT, NW, P> pairs(a, w, bc);
+    const size_t row = (size_t)w.b * a.N + w.t0;
     const bool gated = !kLocal && a.z != nullptr, kept = !kLocal && a.keep != nullptr && live;
-    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0;
-    struct Tile { Column<TT, K> x, dt, z; } far, near, done;      // tiles i + 2, i + 1 and i
-    int there = w.end - mine;                                     // tokens of the sequence from this thread's next to fetch on
-    auto fetch = [&](Tile &f) {
-        f.x.load(px, a.ldx, there), f.dt.load(pdt, a.lddt, there);
-        if (gated) f.z.load(pz, a.ldz, there);
-        pairs.fetch(there + q * K, 1);
-        px += T * a.ldx, pdt += T * a.lddt, pz += T * a.ldz, there -= T;
+    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e;
+    const TT *pz = gated ? (const TT *)a.z + row * a.ldz + e : px;
+    const unsigned ldz = gated ? a.ldz : a.ldx;
+    TT *py = (TT *)a.y + (row + q * K) * a.E + e;
+    float *pk = a.keep + state_at<P>(a, w.b, a.tiles, w.t0 / T, n0, e);
+    const int tokens = w.end - w.t0, tiles = tokens > 0 ? (tokens + T - 1) / T : 0;
+    // by the tile's parity: elements two tiles ahead, what the store of a tile needs, one tile ahead
+    struct Tile { Column<TT, K> x, dt, z; } raw[2];
+    struct Ready { float dx[K], gate[K]; } ready[2];
+    auto fetch = [&](int slot, int i) {
+        const int t = i * T + q * K;
+        raw[slot].x.load(px, a.ldx, t, tokens - 1), raw[slot].dt.load(pdt, a.lddt, t, tokens - 1);
+        if constexpr (!kLocal) raw[slot].z.load(pz, ldz, t, tokens - 1);
+        pairs.fetch(slot, i, tokens - 1);
     };
-    auto prepare = [&](const Tile &f, int i, int buf) {           // d and d x of tile i
-        pairs.park(buf);
-        float d[K];
+    auto prepare = [&](int slot, int i) {
+        pairs.park(slot);
+        const int n = tokens - i * T - q * K;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            d[k] = f.dt.get(k) + bias;
-            if (a.softplus) d[k] = softplus(d[k]);
-            if (mine + i * T + k >= w.end) d[k] = 0.0f;           // a step of zero leaves the state as it is
+            const float x = raw[slot].x.get(k), v = raw[slot].dt.get(k) + bias, sp = softplus(v);
+            const float d = k < n ? (a.softplus ? sp : v) : 0.0f; // a step of zero leaves the state as it is
+            in[slot][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(d, d * x);
+            if constexpr (!kLocal) {
+                const float z = raw[slot].z.get(k), gate = z * sigmoid(z);
+                ready[slot].dx[k] = D * x, ready[slot].gate[k] = gated ? gate : 1.0f;
+            }
         }
-#pragma unroll
-        for (int k = 0; k < K; ++k) in[buf][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(d[k], d[k] * f.x.get(k));
     };
-    fetch(near);
-    fetch(far);
-    if (tiles > 0) prepare(near, 0, 0);
-    __syncthreads();
-    for (int i = 0; i < tiles; ++i) {
-        const int buf = i & 1;
-        done = near, near = far;
-        fetch(far);
-        if (i + 1 < tiles) prepare(near, i + 1, buf ^ 1);
+    auto step = [&](auto parity, int i) {
+        constexpr int buf = decltype(parity)::value;
         if (kept) __builtin_memcpy(pk, h, sizeof(h));
         pk += (size_t)a.E * (NW * P);
+        fetch(buf, i + 2);                                        // this tile's elements are used up
         float y[T];
 #pragma unroll
         for (int j = 0; j < T; ++j) {
             const float2 v = in[buf][j / 2][lane][j % 2];
             const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
             if constexpr (kLocal) sum_d += v.x;
-            y[j] = 0.0f;
 #pragma unroll
             for (int n = 0; n < P; ++n) {
                 h[n] = fmaf(__builtin_amdgcn_exp2f(v.x * A[n]), h[n], v.y * p.B(n));
-                y[j] = fmaf(p.C(n), h[n], y[j]);
+                y[j] = n == 0 ? p.C(n) * h[n] : fmaf(p.C(n), h[n], y[j]);
             }
             if constexpr (!kLocal) {
                 if (j % K == K - 1) __builtin_memcpy(__builtin_assume_aligned(out[buf][q][j / K][lane], 4 * K), &y[j - K + 1], K * sizeof(float));
             }
         }
+        prepare(buf ^ 1, i + 1);                                  // behind the last tile: of nothing, read by nobody
         __syncthreads();
         if constexpr (!kLocal) {
-            if (a.y != nullptr) {
-                float v[K];
+            if (a.y == nullptr) return;
+            float v[K];
 #pragma unroll
-                for (int k = 0; k < K; ++k) v[k] = D * done.x.get(k);
+            for (int k = 0; k < K; ++k) v[k] = ready[buf].dx[k];
 #pragma unroll
-                for (int m = 0; m < NW; ++m) {
-                    float part[K];
-                    __builtin_memcpy(part, out[buf][m][q][lane], sizeof(part));
+            for (int m = 0; m < NW; ++m) {
+                float part[K];
+                __builtin_memcpy(part, __builtin_assume_aligned(out[buf][m][q][lane], 4 * K), sizeof(part));
 #pragma unroll
-                    for (int k = 0; k < K; ++k) v[k] += part[k];
-                }
+                for (int k = 0; k < K; ++k) v[k] += part[k];
+            }
+            const int n = tokens - i * T - q * K, rows = w.t1 - w.t0 - i * T - q * K;
+            if (live) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const int t = mine + i * T + k;
-                    if (gated) v[k] *= done.z.get(k) * sigmoid(done.z.get(k));
-                    if (live && t < w.t1) store_elem<false>(py + (size_t)k * a.E, t < w.end ? v[k] : 0.0f);
+                    v[k] *= ready[buf].gate[k];
+                    if (k < rows) store_elem<false>(py + (size_t)k * a.E, k < n ? v[k] : 0.0f);
                 }
-                py += (size_t)T * a.E;
             }
+            py += (size_t)T * a.E;
         }
+    };
+    if (tiles > 0) {
+        fetch(0, 0);
+        fetch(1, 1);
+        prepare(0, 0);
+    }
+    __syncthreads();
+    for (int i = 0; i < tiles; i += 2) {
+        step(std::integral_constant<int, 0>{}, i);
+        if (i + 1 < tiles) step(std::integral_constant<int, 1>{}, i + 1);
     }
     if constexpr (kLocal) {
         if (live) {
@@ -275,41 +274,32 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
 #pragma unroll
     for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, g[n] = 0.0f;
     const float bias = a.bias == nullptr ? 0.0f : a.bias[e];
-    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
-    Pairs<TT, NW, P> pairs(a, w, bc, last);
-    const int mine = last + q * K;
-    const size_t row = (size_t)w.b * a.N + mine;
-    const TT *pdt = (const TT *)a.dt + row * a.lddt + e, *pz = (const TT *)a.z + row * a.ldz + e, *pdy = (const TT *)a.dy + row * a.E + e;
+    const int tokens = w.end - w.t0, tiles = tokens > 0 ? (tokens + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
+    Pairs<TT, NW, P> pairs(a, w, bc);
+    const size_t row = (size_t)w.b * a.N + w.t0;
     const bool gated = a.z != nullptr;
-    struct Tile { Column<TT, K> dt, dy, z; } far, near;           // tiles i - 2 and i - 1
-    int there = w.end - mine, left = tiles;
-    auto fetch = [&](Tile &f) {                                   // the tiles from the last on
-        const int n = left > 0 ? there : 0;
-        f.dt.load(pdt, a.lddt, n), f.dy.load(pdy, a.E, n);
-        if (gated) f.z.load(pz, a.ldz, n);
-        pairs.fetch(left > 0 ? there + q * K : 0, -1);
-        pdt -= T * a.lddt, pdy -= (long)T * a.E, pz -= T * a.ldz, there += T, --left;
+    const TT *pdt = (const TT *)a.dt + row * a.lddt + e, *pdy = (const TT *)a.dy + row * a.E + e;
+    const TT *pz = gated ? (const TT *)a.z + row * a.ldz + e : pdt;
+    const unsigned ldz = gated ? a.ldz : a.lddt;
+    struct Tile { Column<TT, K> dt, dy, z; } raw[2];
+    auto fetch = [&](int slot, int i) {                           // before the first tile: the first once more
+        const int t = max(i, 0) * T + q * K;
+        raw[slot].dt.load(pdt, a.lddt, t, tokens - 1), raw[slot].dy.load(pdy, a.E, t, tokens - 1), raw[slot].z.load(pz, ldz, t, tokens - 1);
+        pairs.fetch(slot, max(i, 0), tokens - 1);
     };
-    auto prepare = [&](const Tile &f, int i, int buf) {
-        pairs.park(buf);
+    auto prepare = [&](int slot, int i) {
+        pairs.park(slot);
+        const int n = tokens - i * T - q * K;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float d = f.dt.get(k) + bias, dv = f.dy.get(k);
-            if (a.softplus) d = softplus(d);
-            if (gated) dv *= f.z.get(k) * sigmoid(f.z.get(k));
-            const bool real = w.t0 + i * T + q * K + k < w.end;
-            in[buf][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(real ? d : 0.0f, real ? dv : 0.0f);
+            const float v = raw[slot].dt.get(k) + bias, sp = softplus(v), z = raw[slot].z.get(k), gate = z * sigmoid(z);
+            const float d = a.softplus ? sp : v, dv = raw[slot].dy.get(k) * (gated ? gate : 1.0f);
+            in[slot][(q * K + k) / 2][lane][(q * K + k) % 2] = make_float2(k < n ? d : 0.0f, k < n ? dv : 0.0f);
         }
     };
-    fetch(near);
-    fetch(far);
-    if (tiles > 0) prepare(near, tiles - 1, (tiles - 1) & 1);
-    __syncthreads();
-    for (int i = tiles - 1; i >= 0; --i) {
-        const int buf = i & 1;
-        near = far;
-        fetch(far);
-        if (i > 0) prepare(near, i - 1, buf ^ 1);
+    auto step = [&](auto parity, int i) {
+        constexpr int buf = decltype(parity)::value;
+        fetch(buf, i - 2);
 #pragma unroll
         for (int j = T - 1; j >= 0; --j) {
             const float2 v = in[buf][j / 2][lane][j % 2];
@@ -318,7 +308,21 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
 #pragma unroll
             for (int n = 0; n < P; ++n) g[n] = __builtin_amdgcn_exp2f(v.x * A[n]) * fmaf(p.C(n), v.y, g[n]);
         }
+        prepare(buf ^ 1, max(i - 1, 0));
         __syncthreads();
+    };
+    const int first = (tiles - 1) & 1;                            // the last tile's parity
+    if (tiles > 0) {
+        if (first == 0) fetch(0, tiles - 1), fetch(1, tiles - 2), prepare(0, tiles - 1);
+        else fetch(1, tiles - 1), fetch(0, tiles - 2), prepare(1, tiles - 1);
+    }
+    __syncthreads();
+    for (int i = tiles - 1; i >= 0; --i) {
+        if (i & 1) {
+            step(std::integral_constant<int, 1>{}, i);
+            --i;
+        }
+        step(std::integral_constant<int, 0>{}, i);
     }
     if (lane < w.channels) {
         __builtin_memcpy(a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), g, sizeof(g));
@@ -373,60 +377,57 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
     else if (a.dh1 != nullptr) __builtin_memcpy(g, a.dh1 + ((size_t)w.b * a.E + e) * a.S + n0, sizeof(g));
     const float bias = a.bias == nullptr ? 0.0f : a.bias[e], D = a.D == nullptr ? 0.0f : a.D[e];
     float dD = 0.0f, db = 0.0f;
-    const int tiles = w.end > w.t0 ? (w.end - w.t0 + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
-    Pairs<TT, NW, P> pairs(a, w, bc, last);
+    const int tokens = w.end - w.t0, tiles = tokens > 0 ? (tokens + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
+    Pairs<TT, NW, P> pairs(a, w, bc);
     const bool gated = a.z != nullptr;
-    const int mine = last + q * K;                                // this thread's first token of the last tile
-    const size_t row = (size_t)w.b * a.N + mine;
-    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e, *pz = (const TT *)a.z + row * a.ldz + e;
-    const TT *pdy = (const TT *)a.dy + row * a.E + e;
-    size_t dense = row * a.E + e;                                 // of dx, ddt and dz
+    const size_t row = (size_t)w.b * a.N + w.t0;
+    const TT *px = (const TT *)a.x + row * a.ldx + e, *pdt = (const TT *)a.dt + row * a.lddt + e, *pdy = (const TT *)a.dy + row * a.E + e;
+    const TT *pz = gated ? (const TT *)a.z + row * a.ldz + e : px;
+    const unsigned ldz = gated ? a.ldz : a.ldx;
+    size_t dense = (row + (tiles - 1) * T + q * K) * a.E + e;     // of dx, ddt and dz: this thread's first token of a tile
     const float *pk = a.keep + state_at<P>(a, w.b, a.tiles, last / T, n0, e);
     float *pbc = a.part_bc + (((size_t)w.block * a.B + w.b) * a.N + last) * (2 * NW * P) + n0;
-    struct Tile { Column<TT, K> x, dt, z, dy; } far, near;        // tiles i - 2 and i - 1
-    struct Ready { float d[K], slope[K], gate[K], x[K], z[K], dy[K]; } soon, cur;     // tiles i - 1 and i
-    int there = w.end - mine, left = tiles;
-    auto fetch = [&](Tile &f) {                                   // the tiles from the last on
-        const int n = left > 0 ? there : 0;
-        f.x.load(px, a.ldx, n), f.dt.load(pdt, a.lddt, n), f.dy.load(pdy, a.E, n);
-        if (gated) f.z.load(pz, a.ldz, n);
-        pairs.fetch(left > 0 ? there + q * K : 0, -1);
-        px -= T * a.ldx, pdt -= T * a.lddt, pz -= T * a.ldz, pdy -= (long)T * a.E, there += T, --left;
+    // by the tile's parity: elements two tiles ahead, what the finish of a tile needs, one tile ahead
+    struct Tile { Column<TT, K> x, dt, z, dy; } raw[2];
+    struct Ready { float d[K], slope[K], x[K], dv[K], dgate[K]; } ready[2];
+    float start[2][P] = {};                                       // the kept states before the tiles
+    auto fetch = [&](int slot, int i) {                           // before the first tile: the first once more
+        const int t = max(i, 0) * T + q * K;
+        raw[slot].x.load(px, a.ldx, t, tokens - 1), raw[slot].dt.load(pdt, a.lddt, t, tokens - 1);
+        raw[slot].dy.load(pdy, a.E, t, tokens - 1), raw[slot].z.load(pz, ldz, t, tokens - 1);
+        pairs.fetch(slot, max(i, 0), tokens - 1);
     };
-    auto prepare = [&](const Tile &f, Ready &r, int i, int buf) {
-        pairs.park(buf);
+    auto prepare = [&](int slot, int i) {
+        pairs.park(slot);
+        __builtin_memcpy(start[slot], pk, sizeof(start[slot]));
+        if (i > 0) pk -= (size_t)a.E * (NW * P);
+        Ready &r = ready[slot];
+        const int n = live ? tokens - i * T - q * K : 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             // behind the sequence and in lanes without a channel: a step of zero, and nothing for any sum
-            const bool real = live && w.t0 + i * T + q * K + k < w.end;
-            const float raw = f.dt.get(k) + bias;
-            r.d[k] = real ? (a.softplus ? softplus(raw) : raw) : 0.0f;
-            r.slope[k] = real ? (a.softplus ? sigmoid(raw) : 1.0f) : 0.0f;
-            r.x[k] = real ? f.x.get(k) : 0.0f, r.dy[k] = real ? f.dy.get(k) : 0.0f;
-            r.z[k] = gated ? f.z.get(k) : 0.0f, r.gate[k] = sigmoid(r.z[k]);
+            const bool real = k < n;
+            const float raw_d = real ? raw[slot].dt.get(k) + bias : 0.0f, dy = real ? raw[slot].dy.get(k) : 0.0f;
+            // softplus and its slope, the sigmoid, from one exponential
+            const float ex = __expf(-fabsf(raw_d)), inv = __builtin_amdgcn_rcpf(1.0f + ex), sp = fmaxf(raw_d, 0.0f) + log1p_small(ex);
+            const float slope = raw_d >= 0.0f ? inv : ex * inv;
+            r.d[k] = real ? (a.softplus ? sp : raw_d) : 0.0f;
+            r.slope[k] = a.softplus ? slope : 1.0f;
+            r.x[k] = real ? raw[slot].x.get(k) : 0.0f;
+            const float z = real ? raw[slot].z.get(k) : 0.0f, gate = sigmoid(z);
+            r.dv[k] = dy * (gated ? z * gate : 1.0f);
+            r.dgate[k] = dy * gate * fmaf(z, 1.0f - gate, 1.0f);
             const int t = q * K + k;
-            in[buf][t / 2][lane][t % 2] = make_float2(r.d[k], r.d[k] * r.x[k]);
-            in_v[buf][t / 2][lane][t % 2] = gated ? r.dy[k] * r.z[k] * r.gate[k] : r.dy[k];
+            in[slot][t / 2][lane][t % 2] = make_float2(r.d[k], r.d[k] * r.x[k]);
+            in_v[slot][t / 2][lane][t % 2] = r.dv[k];
         }
     };
-    fetch(near);
-    fetch(far);
-    float start[P] = {};                                          // the kept state before the next tile
-    if (tiles > 0) {
-        __builtin_memcpy(start, pk, sizeof(start));
-        prepare(near, soon, tiles - 1, (tiles - 1) & 1);
-    }
-    __syncthreads();
-    for (int i = tiles - 1; i >= 0; --i) {
-        const int t = w.t0 + i * T, buf = i & 1;
-        cur = soon, near = far;
-        fetch(far);
+    auto step = [&](auto parity, int i) {
+        constexpr int buf = decltype(parity)::value;
         float h[T + 1][P], dec[T][P];
 #pragma unroll
-        for (int n = 0; n < P; ++n) h[0][n] = start[n];
-        pk -= (size_t)a.E * (NW * P);
-        if (i > 0) __builtin_memcpy(start, pk, sizeof(start));
-        if (i > 0) prepare(near, soon, i - 1, buf ^ 1);
+        for (int n = 0; n < P; ++n) h[0][n] = start[buf][n];
+        fetch(buf, i - 2);
 #pragma unroll
         for (int j = 0; j < T; ++j) {
             const float2 v = in[buf][j / 2][lane][j % 2];
@@ -437,6 +438,7 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
                 h[j + 1][n] = fmaf(dec[j][n], h[j][n], v.y * p.B(n));
             }
         }
+        prepare(buf ^ 1, max(i - 1, 0));
         constexpr int kHeld = P / 2;                              // registers a token's folded products take
         float acc[kHeld * T], sum[3][K];
 #pragma unroll
@@ -444,24 +446,23 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
             const float2 v = in[buf][j / 2][lane][j % 2];
             const float dv = in_v[buf][j / 2][lane][j % 2];
             const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
-            float gB = 0.0f, gA = 0.0f, y = 0.0f, prod[2 * P];
+            float gB, gA, y, prod[2 * P];
 #pragma unroll
             for (int n = 0; n < P; ++n) {
-                y = fmaf(p.C(n), h[j + 1][n], y);
+                y = n == 0 ? p.C(n) * h[j + 1][n] : fmaf(p.C(n), h[j + 1][n], y);
                 g[n] = fmaf(p.C(n), dv, g[n]);
-                gB = fmaf(p.B(n), g[n], gB);
+                gB = n == 0 ? p.B(n) * g[n] : fmaf(p.B(n), g[n], gB);
                 prod[n] = g[n] * v.y;
                 prod[P + n] = h[j + 1][n] * dv;
                 g[n] *= dec[j][n];                                // now the gradient for h_{t-1}
                 const float through = g[n] * h[j][n];
-                gA = fmaf(through, A[n], gA);
+                gA = n == 0 ? through * A[n] : fmaf(through, A[n], gA);
                 dA[n] = fmaf(through, v.x, dA[n]);
             }
             sum[0][j % K] = gB, sum[1][j % K] = gA, sum[2][j % K] = y;
             if (j % K == 0) {
 #pragma unroll
-                for (int r = 0; r < 3; ++r)
-                    if (r < 2 || gated) __builtin_memcpy(__builtin_assume_aligned(out[r][q][j / K][lane], 4 * K), sum[r], sizeof(sum[r]));
+                for (int r = 0; r < 3; ++r) __builtin_memcpy(__builtin_assume_aligned(out[r][q][j / K][lane], 4 * K), sum[r], sizeof(sum[r]));
             }
             fold32<P>(prod);
             fold16<P / 2>(prod);
@@ -479,38 +480,51 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
             const int low = ((lane & 1) << 2) + (lane & 2) + ((lane & 4) >> 2);
             const int j = P == 4 ? k * 8 + low : 2 * low + ((lane & 8) >> 3);
             const int value = (P == 4 ? (lane & 8) >> 1 : 0) + ((lane & 16) >> 3) + ((lane & 32) >> 5);
-            if (t + j < w.end) pbc[(2 * j + value / P) * (NW * P) + value % P] = acc[k];
+            if (i * T + j < tokens) pbc[(2 * j + value / P) * (NW * P) + value % P] = acc[k];
         }
         pbc -= T * 2 * NW * P;
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < K; ++k) sum[0][k] = sum[1][k] = sum[2][k] = 0.0f;
+        for (int r = 0; r < 3; ++r) {
 #pragma unroll
-        for (int m = 0; m < NW; ++m) {
+            for (int k = 0; k < K; ++k) sum[r][k] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 3; ++r) {
-                if (r == 2 && !gated) break;
+            for (int m = 0; m < NW; ++m) {
                 float part[K];
-                __builtin_memcpy(part, out[r][m][q][lane], sizeof(part));
+                __builtin_memcpy(part, __builtin_assume_aligned(out[r][m][q][lane], 4 * K), sizeof(part));
 #pragma unroll
                 for (int k = 0; k < K; ++k) sum[r][k] += part[k];
             }
         }
         __syncthreads();
+        const Ready &r = ready[buf];
+        const int n = live ? tokens - i * T - q * K : 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const float gB = sum[0][k], gA = sum[1][k] * (1.0f / kLog2e), y = fmaf(D, cur.x[k], sum[2][k]);
-            const float dv = gated ? cur.dy[k] * cur.z[k] * cur.gate[k] : cur.dy[k];
-            const float ddt = fmaf(cur.x[k], gB, gA) * cur.slope[k];
-            dD = fmaf(dv, cur.x[k], dD), db += ddt;
-            if (live && t + q * K + k < w.end) {
+            const float gB = sum[0][k], gA = sum[1][k] * (1.0f / kLog2e), y = fmaf(D, r.x[k], sum[2][k]);
+            const float ddt = k < n ? fmaf(r.x[k], gB, gA) * r.slope[k] : 0.0f;
+            dD = fmaf(r.dv[k], r.x[k], dD), db += ddt;
+            if (k < n) {
                 const size_t at = dense + (size_t)k * a.E;
-                store_elem<false>((TT *)a.dx + at, fmaf(cur.d[k], gB, D * dv));
+                store_elem<false>((TT *)a.dx + at, fmaf(r.d[k], gB, D * r.dv[k]));
                 store_elem<false>((TT *)a.ddt + at, ddt);
-                if (gated) store_elem<false>((TT *)a.dz + at, cur.dy[k] * y * cur.gate[k] * fmaf(cur.z[k], 1.0f - cur.gate[k], 1.0f));
+                if (gated) store_elem<false>((TT *)a.dz + at, r.dgate[k] * y);
             }
         }
         dense -= (size_t)T * a.E;
+    };
+    const int first = (tiles - 1) & 1;                            // the last tile's parity
+    if (tiles > 0) {
+        if (first == 0) fetch(0, tiles - 1), fetch(1, tiles - 2), prepare(0, tiles - 1);
+        else fetch(1, tiles - 1), fetch(0, tiles - 2), prepare(1, tiles - 1);
+    }
+    __syncthreads();
+    for (int i = tiles - 1; i >= 0; --i) {
+        if (i & 1) {
+            step(std::integral_constant<int, 1>{}, i);
+            --i;
+        }
+        step(std::integral_constant<int, 0>{}, i);
     }
     if (live) {                                                   // rows behind the sequence
         for (int t = max(w.end, w.t0) + q; t < w.t1; t += NW) {
@@ -537,19 +551,32 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
     }
 }
 
-// dB and dC of every token and group: sums over the channel blocks of the group; zero behind the sequence
+// dB and dC of every token and group: sums over the channel blocks of the group, in their order; zero behind the sequence.
+// A thread has 4 of a token's 2 S sums.
 template <typename TT> __global__ __launch_bounds__(256) void scan_sum_bc_kernel(const ScanArgs a) {
-    const int per = a.E / a.G, nb = (per + kLanes - 1) / kLanes;
-    const long row = (long)a.B * a.N, all = row * 2 * a.S * a.G;
+    constexpr int kAhead = 8;                                     // blocks on their way at a time
+    const int per = a.E / a.G, nb = (per + kLanes - 1) / kLanes, quads = a.S / 2;
+    const long tokens = (long)a.B * a.N, all = tokens * quads * a.G;
+    const size_t block = (size_t)tokens * 2 * a.S;
     for (long id = (long)blockIdx.x * 256 + threadIdx.x; id < all; id += (long)gridDim.x * 256) {
-        const long rows = id / (2 * a.S * a.G);
-        const int in_row = (int)(id - rows * (2 * a.S * a.G)), g = in_row / (2 * a.S), c = in_row % (2 * a.S);
-        const int b = (int)(rows / a.N), t = (int)(rows - (long)b * a.N);
-        float v = 0.0f;
-        if (t < length_of(a.lengths, b, a.N))
-            for (int k = 0; k < nb; ++k) v += a.part_bc[(((size_t)(g * nb + k)) * row + rows) * 2 * a.S + c];
-        TT *o = (TT *)(c < a.S ? a.dB : a.dC);
-        store_elem<false>(o + ((size_t)rows * a.G + g) * a.S + c % a.S, v);
+        const long token = id / (quads * a.G);
+        const int in_token = (int)(id - token * (quads * a.G)), g = in_token / quads, c = in_token % quads * 4;
+        const int b = (int)(token / a.N), t = (int)(token - (long)b * a.N);
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (t < length_of(a.lengths, b, a.N)) {
+            const float *from = a.part_bc + (size_t)g * nb * block + (size_t)token * 2 * a.S + c;
+            for (int k0 = 0; k0 < nb; k0 += kAhead) {
+                f32x4 part[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) part[k] = *reinterpret_cast<const f32x4 *>(from + (size_t)min(k0 + k, nb - 1) * block);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (k0 + k < nb) v += part[k];
+            }
+        }
+        TT *o = (TT *)(c < a.S ? a.dB : a.dC) + ((size_t)token * a.G + g) * a.S + c % a.S;
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        store_row<TT, 4>(o, 4, f);
     }
 }
 
@@ -603,27 +630,58 @@ template <typename TT, int S> __global__ __launch_bounds__(256) void scan_step_k
 
 unsigned blocks_for(long n) { return (unsigned)((n + 255) / 256 < (1 << 20) ? (n + 255) / 256 : 1 << 20); }
 
+// ---- cutting sequences into pieces ------------------------------------------------------------------
+// Microseconds a tile of 16 tokens takes while every compute unit has 1, 2, .. `most` workgroups (its LDS holds no more),
+// and what each 256 workgroups of the kernel that only forms the pieces' states add; measured with 2048 channels, bf16.
+struct TileCost {
+    int most;
+    double us[3], local;
+};
+constexpr int kUnits = 256;
+// Sixteen states: eight waves of two states while a compute unit has one workgroup, else four waves of four (1.95 us
+// alone, but up to three fit: 3.6 us for the three, and 4.4 for three of the others, one after the other).
+TileCost fwd_cost(int S) {
+    return S == 8 ? TileCost{3, {1.53, 2.0, 2.6}, 0.6} : S == 16 ? TileCost{3, {1.47, 2.7, 3.6}, 0.9} : TileCost{1, {2.5}, 1.6};
+}
+TileCost bwd_cost(int S) {
+    return S == 8 ? TileCost{2, {3.3, 4.8}, 0.6} : S == 16 ? TileCost{1, {3.85}, 0.9} : TileCost{1, {6.5}, 1.75};
+}
+double tile_us(const TileCost &c, long workgroups) {
+    const long full = workgroups / (kUnits * c.most), rest = workgroups % (kUnits * c.most);
+    return full * c.us[c.most - 1] + (rest > 0 ? c.us[(rest - 1) / kUnits] : 0.0);
+}
+
 }  // namespace
 
 int scan_blocks(int E, int G) { return G * ((E / G + kLanes - 1) / kLanes); }
 
-void scan_cut(ScanArgs &a) {
+// The number of pieces with the least time: all of a sequence's tiles one after the other, or pieces of at least 4 tiles side by
+// side after the kernel that forms their states (one piece fewer), a scan over the pieces and two more launches.
+void scan_cut(ScanArgs &a, bool backward) {
     a.tiles = (a.N + T - 1) / T;
     const long whole = (long)a.B * scan_blocks(a.E, a.G);
-    long pieces = 1;
-    if (whole < 160) pieces = (1024 + whole - 1) / whole;
-    const long most = a.tiles / 4 > 1 ? a.tiles / 4 : 1;          // no piece shorter than 64 tokens
-    if (pieces > most) pieces = most;
-    a.piece_tiles = (int)((a.tiles + pieces - 1) / pieces);
-    a.pieces = (a.tiles + a.piece_tiles - 1) / a.piece_tiles;
+    const TileCost c = backward ? bwd_cost(a.S) : fwd_cost(a.S);
+    double best = tile_us(c, whole) * a.tiles;
+    a.pieces = 1, a.piece_tiles = a.tiles;
+    for (int pieces = 2; pieces <= a.tiles / 4 && whole * pieces <= kUnits * c.most + whole; ++pieces) {
+        const int tiles = (a.tiles + pieces - 1) / pieces;
+        if ((a.tiles + tiles - 1) / tiles != pieces) continue;
+        const double us = tiles * (tile_us(c, whole * pieces) + c.local * ((whole * (pieces - 1) + kUnits - 1) / kUnits)) + 10.0 + 0.25 * pieces;
+        if (us < best) best = us, a.pieces = pieces, a.piece_tiles = tiles;
+    }
 }
 
 hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s) {
-    const unsigned grid = (unsigned)((long)a.B * a.pieces * scan_blocks(a.E, a.G));
+    const long workgroups = (long)a.B * a.pieces * scan_blocks(a.E, a.G);
+    const unsigned grid = (unsigned)workgroups;
     LA_SCAN_DISPATCH(a.S, dtype, {
         if (a.pieces > 1) {
             scan_fwd_kernel<TT, NW, P, true><<<grid, 64 * NW, 0, s>>>(a);
             scan_pieces_kernel<false><<<blocks_for((long)a.B * a.E * a.S), 256, 0, s>>>(a);
+        }
+        if (a.S == 16 && workgroups > kUnits) {
+            scan_fwd_kernel<TT, 4, 4, false><<<grid, 256, 0, s>>>(a);
+            return hipGetLastError();
         }
         scan_fwd_kernel<TT, NW, P, false><<<grid, 64 * NW, 0, s>>>(a);
     });
@@ -639,7 +697,7 @@ hipError_t launch_scan_bwd(const ScanArgs &a, int dtype, hipStream_t s) {
         }
         scan_bwd_kernel<TT, NW, P><<<grid, 64 * NW, 0, s>>>(a);
     });
-    LA_SCAN_T(dtype, scan_sum_bc_kernel<TT><<<blocks_for((long)a.B * a.N * a.G * 2 * a.S), 256, 0, s>>>(a));
+    LA_SCAN_T(dtype, scan_sum_bc_kernel<TT><<<blocks_for((long)a.B * a.N * a.G * a.S / 2), 256, 0, s>>>(a));
     return hipGetLastError();
 }
 
