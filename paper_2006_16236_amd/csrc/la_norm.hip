@@ -3,16 +3,17 @@
 // Bound by memory: forward 2 tensors (4 with a residual and its sum), backward 3 (4).  A row lives in the
 // registers of the lanes that share it, so that each element is read once: mean, then the sum of squares around it
 // (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  64 lanes share rows
-// up to 1024 elements, 256 up to 4096, 1024 up to 16384: 16 elements a lane at most, which leaves room for
-// the backward's two sums per column.
+// up to 1024 elements (backward 2048, whose sums per column then need no barrier), 256 up to 8192, 1024 (backward 512) up to 16384.
 #include "la_layer.h"
 
 namespace la {
 namespace {
 
 constexpr int kSumSlices = 16;
-constexpr int kBwdThreads = 512, kBwdGroups = 512;
-constexpr long kMaxGrid = 1 << 20;       // workgroups of a launch; more rows go round again
+constexpr int kBwdThreads = 512;
+// Workgroups of a launch; more rows go round again.  A workgroup of 1024 lanes that keeps its weights for several rows is 6 %
+// faster than one a row, one of 256 is 5 % slower.
+constexpr long kMaxGrid = 1 << 20, kWideGrid = 2048;
 
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ part, long rows, const SumTargets out) {
     __shared__ float red[kSumSlices][kWave];
@@ -61,6 +62,13 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? 
     constexpr int V = 16 / sizeof(T), kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
     __shared__ float red[kThreads / kWave];
     const int E = a.E, l = threadIdx.x % TPR;
+    float g[NV][V], b[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (j * TPR + l) * V;
+        load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, g[j], 1.0f);
+        load_params<V>(a.beta == nullptr ? nullptr : a.beta + e, E - e, b[j]);
+    }
     for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
     const long row = first + threadIdx.x / TPR;
     const bool live = row < a.rows;          // whole waves; all of a workgroup's waves meet in row_sum
@@ -101,12 +109,10 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? 
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int e = (j * TPR + l) * V;
-        float g[V], b[V];
-        load_params<V>(a.gamma == nullptr ? nullptr : a.gamma + e, E - e, g, 1.0f);
-        load_params<V>(a.beta == nullptr ? nullptr : a.beta + e, E - e, b);
+        float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) g[i] = fmaf(f[j][i] * rstd, g[i], b[i]);
-        store_row<T, V>((T *)a.y + (size_t)row * E + e, live ? E - e : 0, g);
+        for (int i = 0; i < V; ++i) o[i] = fmaf(f[j][i] * rstd, g[j][i], b[j][i]);
+        store_row<T, V>((T *)a.y + (size_t)row * E + e, live ? E - e : 0, o);
     }
     }
 }
@@ -200,7 +206,7 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads)
     }
 }
 
-int lanes_of(int E) { return E <= 1024 ? 64 : E <= 4096 ? 256 : 1024; }
+int lanes_of(int E) { return E <= 1024 ? 64 : 256; }     // up to 8192
 int lanes_of_bwd(int E) { return E <= 2048 ? 64 : E <= 8192 ? 256 : 512; }
 
 }  // namespace
@@ -211,66 +217,69 @@ hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, 
     return hipGetLastError();
 }
 
+// Two workgroups a compute unit, or one where more than 16 elements a lane leave room for no more (16384 x 2048 bf16: 62 us
+// with 512 workgroups, 55 with 256; 16384 x 4096: 113 and 140).
 int norm_groups(int rows, int E) {
-    const int per = kBwdThreads / lanes_of_bwd(E);
-    const long sets = ((long)rows + per - 1) / per, turns = (sets + kBwdGroups - 1) / kBwdGroups;      // equal shares
+    const int tpr = lanes_of_bwd(E), per = kBwdThreads / tpr, most = E > 16 * tpr ? 256 : 512;
+    const long sets = ((long)rows + per - 1) / per, turns = (sets + most - 1) / most;      // equal shares
     return (int)((sets + turns - 1) / turns);
 }
 
-// pieces per lane: 1, 2 or 4 (fp32: 16 elements are four pieces; bf16: two)
-#define LA_NORM_DISPATCH(KERNEL)                                                                         \
-    do {                                                                                                 \
-        const int tpr = lanes_of(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);     \
-        if (dtype == 0) {                                                                                \
-            if (tpr == 64) { if (nv <= 1) KERNEL(float, 64, 1); else if (nv == 2) KERNEL(float, 64, 2); else KERNEL(float, 64, 4); }   \
-            else if (tpr == 256) { if (nv == 2) KERNEL(float, 256, 2); else KERNEL(float, 256, 4); }     \
-            else { if (nv == 2) KERNEL(float, 1024, 2); else KERNEL(float, 1024, 4); }                   \
-        } else {                                                                                         \
-            if (tpr == 64) { if (nv <= 1) KERNEL(bf16_t, 64, 1); else KERNEL(bf16_t, 64, 2); }           \
-            else if (tpr == 256) { if (nv <= 1) KERNEL(bf16_t, 256, 1); else KERNEL(bf16_t, 256, 2); }   \
-            else { if (nv <= 1) KERNEL(bf16_t, 1024, 1); else KERNEL(bf16_t, 1024, 2); }                 \
-        }                                                                                                \
+// Kernels by lanes per row and pieces per lane: 16 elements are four pieces of fp32, two of bf16.
+#define LA_NORM_DISPATCH(TPR_OF, LA_KERNEL)                                                                  \
+    do {                                                                                                     \
+        const int tpr = TPR_OF(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);           \
+        if (dtype == 0) {                                                                                    \
+            if (tpr == 64) {                                                                                 \
+                if (nv <= 1) LA_KERNEL(float, 64, 1);                                                        \
+                else if (nv == 2) LA_KERNEL(float, 64, 2);                                                   \
+                else if (nv <= 4) LA_KERNEL(float, 64, 4);                                                   \
+                else LA_KERNEL(float, 64, 8);                                                                \
+            } else if (tpr == 256) {                                                                         \
+                if (nv <= 2) LA_KERNEL(float, 256, 2);                                                       \
+                else if (nv <= 4) LA_KERNEL(float, 256, 4);                                                  \
+                else LA_KERNEL(float, 256, 8);                                                               \
+            } else {                                                                                         \
+                LA_KERNEL(float, 512, 8);                                                                    \
+            }                                                                                                \
+        } else {                                                                                             \
+            if (tpr == 64) {                                                                                 \
+                if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);                                                       \
+                else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);                                                  \
+                else LA_KERNEL(bf16_t, 64, 4);                                                               \
+            } else if (tpr == 256) {                                                                         \
+                if (nv <= 1) LA_KERNEL(bf16_t, 256, 1);                                                      \
+                else if (nv == 2) LA_KERNEL(bf16_t, 256, 2);                                                 \
+                else LA_KERNEL(bf16_t, 256, 4);                                                              \
+            } else {                                                                                         \
+                LA_KERNEL(bf16_t, 512, 4);                                                                   \
+            }                                                                                                \
+        }                                                                                                    \
     } while (0)
 
 hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
 #define LA_KERNEL(T, TPR, NV)                                                                                        \
     do {                                                                                                             \
         constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR;                                          \
+        constexpr long most = TPR > 256 ? kWideGrid : kMaxGrid;                                                      \
         const long sets = ((long)a.rows + per - 1) / per;                                                            \
-        norm_fwd_kernel<T, TPR, NV><<<(unsigned)(sets < kMaxGrid ? sets : kMaxGrid), threads, 0, s>>>(a);            \
+        norm_fwd_kernel<T, TPR, NV><<<(unsigned)(sets < most ? sets : most), threads, 0, s>>>(a);                    \
     } while (0)
-    LA_NORM_DISPATCH(LA_KERNEL);
+    // 16 elements a lane again (4096 x 16384 bf16: 512 lanes of 32 take 137 us, these 106)
+    if (a.E > 8192) {
+        if (dtype == 0) LA_KERNEL(float, 1024, 4);
+        else LA_KERNEL(bf16_t, 1024, 2);
+    } else {
+        LA_NORM_DISPATCH(lanes_of, LA_KERNEL);
+    }
 #undef LA_KERNEL
     return hipGetLastError();
 }
 
 hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
-    const int groups = norm_groups(a.rows, a.E), tpr = lanes_of_bwd(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);
+    const int groups = norm_groups(a.rows, a.E);
 #define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, kBwdThreads, 0, s>>>(a)
-    if (dtype == 0) {
-        if (tpr == 64) {
-            if (nv <= 1) LA_KERNEL(float, 64, 1);
-            else if (nv == 2) LA_KERNEL(float, 64, 2);
-            else if (nv <= 4) LA_KERNEL(float, 64, 4);
-            else LA_KERNEL(float, 64, 8);
-        } else if (tpr == 256) {
-            if (nv <= 4) LA_KERNEL(float, 256, 4);
-            else LA_KERNEL(float, 256, 8);
-        } else {
-            LA_KERNEL(float, 512, 8);
-        }
-    } else {
-        if (tpr == 64) {
-            if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
-            else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);
-            else LA_KERNEL(bf16_t, 64, 4);
-        } else if (tpr == 256) {
-            if (nv <= 2) LA_KERNEL(bf16_t, 256, 2);
-            else LA_KERNEL(bf16_t, 256, 4);
-        } else {
-            LA_KERNEL(bf16_t, 512, 4);
-        }
-    }
+    LA_NORM_DISPATCH(lanes_of_bwd, LA_KERNEL);
 #undef LA_KERNEL
     return hipGetLastError();
 }
