@@ -206,7 +206,8 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads)
     }
 }
 
-int lanes_of(int E) { return E <= 1024 ? 64 : 256; }     // up to 8192
+// forward: beyond 8192 elements 16 a lane again (4096 x 16384 bf16: 512 lanes of 32 take 137 us, 1024 of 16 take 106)
+int lanes_of(int E) { return E <= 1024 ? 64 : E <= 8192 ? 256 : 1024; }
 int lanes_of_bwd(int E) { return E <= 2048 ? 64 : E <= 8192 ? 256 : 512; }
 
 }  // namespace
@@ -225,37 +226,11 @@ int norm_groups(int rows, int E) {
     return (int)((sets + turns - 1) / turns);
 }
 
-// Kernels by lanes per row and pieces per lane: 16 elements are four pieces of fp32, two of bf16.
-#define LA_NORM_DISPATCH(TPR_OF, LA_KERNEL)                                                                  \
-    do {                                                                                                     \
-        const int tpr = TPR_OF(a.E), v = dtype == 0 ? 4 : 8, nv = (a.E + tpr * v - 1) / (tpr * v);           \
-        if (dtype == 0) {                                                                                    \
-            if (tpr == 64) {                                                                                 \
-                if (nv <= 1) LA_KERNEL(float, 64, 1);                                                        \
-                else if (nv == 2) LA_KERNEL(float, 64, 2);                                                   \
-                else if (nv <= 4) LA_KERNEL(float, 64, 4);                                                   \
-                else LA_KERNEL(float, 64, 8);                                                                \
-            } else if (tpr == 256) {                                                                         \
-                if (nv <= 2) LA_KERNEL(float, 256, 2);                                                       \
-                else if (nv <= 4) LA_KERNEL(float, 256, 4);                                                  \
-                else LA_KERNEL(float, 256, 8);                                                               \
-            } else {                                                                                         \
-                LA_KERNEL(float, 512, 8);                                                                    \
-            }                                                                                                \
-        } else {                                                                                             \
-            if (tpr == 64) {                                                                                 \
-                if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);                                                       \
-                else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);                                                  \
-                else LA_KERNEL(bf16_t, 64, 4);                                                               \
-            } else if (tpr == 256) {                                                                         \
-                if (nv <= 1) LA_KERNEL(bf16_t, 256, 1);                                                      \
-                else if (nv == 2) LA_KERNEL(bf16_t, 256, 2);                                                 \
-                else LA_KERNEL(bf16_t, 256, 4);                                                              \
-            } else {                                                                                         \
-                LA_KERNEL(bf16_t, 512, 4);                                                                   \
-            }                                                                                                \
-        }                                                                                                    \
-    } while (0)
+// pieces of 16 bytes a lane has of a row that `tpr` lanes share
+static int pieces_of(int E, int tpr, int dtype) {
+    const int v = tpr * (dtype == 0 ? 4 : 8);
+    return (E + v - 1) / v;
+}
 
 hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
 #define LA_KERNEL(T, TPR, NV)                                                                                        \
@@ -265,21 +240,62 @@ hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
         const long sets = ((long)a.rows + per - 1) / per;                                                            \
         norm_fwd_kernel<T, TPR, NV><<<(unsigned)(sets < most ? sets : most), threads, 0, s>>>(a);                    \
     } while (0)
-    // 16 elements a lane again (4096 x 16384 bf16: 512 lanes of 32 take 137 us, these 106)
-    if (a.E > 8192) {
-        if (dtype == 0) LA_KERNEL(float, 1024, 4);
-        else LA_KERNEL(bf16_t, 1024, 2);
+    const int tpr = lanes_of(a.E), nv = pieces_of(a.E, tpr, dtype);
+    if (dtype == 0) {
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(float, 64, 1);
+            else if (nv == 2) LA_KERNEL(float, 64, 2);
+            else LA_KERNEL(float, 64, 4);
+        } else if (tpr == 256) {
+            if (nv <= 2) LA_KERNEL(float, 256, 2);
+            else if (nv <= 4) LA_KERNEL(float, 256, 4);
+            else LA_KERNEL(float, 256, 8);
+        } else {
+            LA_KERNEL(float, 1024, 4);
+        }
     } else {
-        LA_NORM_DISPATCH(lanes_of, LA_KERNEL);
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
+            else LA_KERNEL(bf16_t, 64, 2);
+        } else if (tpr == 256) {
+            if (nv <= 1) LA_KERNEL(bf16_t, 256, 1);
+            else if (nv == 2) LA_KERNEL(bf16_t, 256, 2);
+            else LA_KERNEL(bf16_t, 256, 4);
+        } else {
+            LA_KERNEL(bf16_t, 1024, 2);
+        }
     }
 #undef LA_KERNEL
     return hipGetLastError();
 }
 
 hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
-    const int groups = norm_groups(a.rows, a.E);
 #define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, kBwdThreads, 0, s>>>(a)
-    LA_NORM_DISPATCH(lanes_of_bwd, LA_KERNEL);
+    const int groups = norm_groups(a.rows, a.E), tpr = lanes_of_bwd(a.E), nv = pieces_of(a.E, tpr, dtype);
+    if (dtype == 0) {
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(float, 64, 1);
+            else if (nv == 2) LA_KERNEL(float, 64, 2);
+            else if (nv <= 4) LA_KERNEL(float, 64, 4);
+            else LA_KERNEL(float, 64, 8);
+        } else if (tpr == 256) {
+            if (nv <= 4) LA_KERNEL(float, 256, 4);
+            else LA_KERNEL(float, 256, 8);
+        } else {
+            LA_KERNEL(float, 512, 8);
+        }
+    } else {
+        if (tpr == 64) {
+            if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
+            else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);
+            else LA_KERNEL(bf16_t, 64, 4);
+        } else if (tpr == 256) {
+            if (nv == 2) LA_KERNEL(bf16_t, 256, 2);
+            else LA_KERNEL(bf16_t, 256, 4);
+        } else {
+            LA_KERNEL(bf16_t, 512, 4);
+        }
+    }
 #undef LA_KERNEL
     return hipGetLastError();
 }

@@ -26,7 +26,8 @@ def _abs(mag):
 
 
 def sigmoid(v):
-    return 0.5 * (1.0 + np.tanh(0.5 * v))
+    e = np.exp(-np.abs(v))                         # both branches without cancellation
+    return np.where(v >= 0, 1.0, e) / (1.0 + e)
 
 
 def to_bf16(a):
