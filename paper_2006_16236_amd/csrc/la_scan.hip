@@ -440,7 +440,7 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
         }
         prepare(buf ^ 1, max(i - 1, 0));
         constexpr int kHeld = P / 2;                              // registers a token's folded products take
-        float acc[kHeld * T], sum[3][K];
+        float acc[kHeld * T], sum[3][K], dA_tile[P] = {};         // (a sum of thousands of terms, in two levels)
 #pragma unroll
         for (int j = T - 1; j >= 0; --j) {
             const float2 v = in[buf][j / 2][lane][j % 2];
@@ -457,7 +457,7 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
                 g[n] *= dec[j][n];                                // now the gradient for h_{t-1}
                 const float through = g[n] * h[j][n];
                 gA = n == 0 ? through * A[n] : fmaf(through, A[n], gA);
-                dA[n] = fmaf(through, v.x, dA[n]);
+                dA_tile[n] = fmaf(through, v.x, dA_tile[n]);
             }
             sum[0][j % K] = gB, sum[1][j % K] = gA, sum[2][j % K] = y;
             if (j % K == 0) {
@@ -469,6 +469,8 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) acc[kHeld * j + r] = prod[r];
         }
+#pragma unroll
+        for (int n = 0; n < P; ++n) dA[n] += dA_tile[n];
         // Lanes that differ in bits 5 and 4 now hold different products: value 4 r + 2 bit4 + bit5 of a token's 2 P.  The
         // folds within 16 lanes choose between the two halves r (P = 4) by bit 3, and between tokens by the rest.
         fold_row<P * T / 4, 0x128>(acc, lane & 8);
