@@ -41,29 +41,60 @@ template <int W, int V> struct Filter {
     }
 };
 
-// row t of the sequence, t >= -(W - 1): x0 (zeros without it) before token 0, nothing from `end` on.  kInside: the caller
-// knows that all of the rows it asks for are tokens of the sequence, and all V channels there.
-template <typename T, int W, int V> struct Rows {
+// A thread's V channels from e on: the last ones of a row begin at E - V, and share channels (and results) with the thread
+// before.  kNarrow: E < V, `valid` = E of the V are there.
+template <bool kNarrow, int V> __device__ __forceinline__ int first_channel(int piece, int E) { return kNarrow ? 0 : min(piece * V, E - V); }
+template <bool kNarrow, typename T, int V> __device__ __forceinline__ Piece<T, V> load_row(const T *p, int E) {
+    return load_piece<T, V>(p, kNarrow ? E : V);
+}
+template <bool kNarrow, typename T, int V> __device__ __forceinline__ void store_to(T *p, int E, const float (&f)[V]) {
+    store_row<T, V>(p, kNarrow ? E : V, f);
+}
+template <typename T, int V> __device__ __forceinline__ void keep_if(bool there, Piece<T, V> &p) {
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) p.w[i] = there ? p.w[i] : 0;
+}
+// Row t of the sequence, t >= -(W - 1): x0 (zeros without it) before token 0, zeros from `end` on.  The address is that of a
+// row that is there in any case, and the value is masked: a branch around the load would be waited for.  kInside: the
+// caller knows that all rows it asks for are tokens of the sequence.
+template <typename T, int W, int V, bool kNarrow> struct Rows {
     const T *x, *x0;                 // at this sequence and channel; x0: its first row
     long ldx;
-    int E, valid, end;
+    int E, end;
     template <bool kInside = false> __device__ __forceinline__ Piece<T, V> at(int t) const {
-        if constexpr (kInside) return load_piece<T, V>(x + (size_t)t * ldx, V);
-        if (t >= 0) return load_piece<T, V>(x + (size_t)t * ldx, t < end ? valid : 0);
-        return load_piece<T, V>(x0 + (size_t)(t + W - 1) * E, x0 == nullptr ? 0 : valid);
+        if constexpr (kInside) return load_row<kNarrow, T, V>(x + (size_t)t * ldx, E);
+        const bool before = t < 0;
+        const T *p = before && x0 != nullptr ? x0 + (size_t)(t + W - 1) * E : x + (size_t)max(min(t, end - 1), 0) * ldx;
+        Piece<T, V> r = load_row<kNarrow, T, V>(p, E);
+        keep_if(before ? x0 != nullptr : t < end, r);
+        return r;
     }
 };
 
-template <typename T, int W, bool kInside>
-__device__ __forceinline__ void conv_fwd_run(const Rows<T, W, kV<T>> &row, const Filter<W, kV<T>> &f, T *y, int E, int t0, int t1, bool silu) {
+template <typename T, int W, bool kNarrow> __global__ __launch_bounds__(256) void conv_fwd_kernel(const ConvArgs a) {
     constexpr int V = kV<T>;
+    const int pieces = (a.E + V - 1) / V, E = a.E;
+    const long id = (long)blockIdx.x * 256 + threadIdx.x;
+    const long cut = id / pieces;
+    if (cut >= (long)a.B * a.runs) return;
+    const int e = first_channel<kNarrow, V>((int)(id - cut * pieces), E), b = (int)(cut / a.runs);
+    const int t0 = (int)(cut - (long)b * a.runs) * a.run, t1 = min(t0 + a.run, a.N), len = length_of(a.lengths, b, a.N);
+    const Rows<T, W, V, kNarrow> row{(const T *)a.x + (size_t)b * a.N * a.ldx + e,
+                                     a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * E + e, a.ldx, E, len};
+    const Filter<W, V> f(a.w, a.bias, e, kNarrow ? E : V);
     Piece<T, V> win[W - 1];
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) win[k] = row.template at<kInside>(t0 - (W - 1) + k);
+    for (int k = 0; k < W - 1; ++k) win[k] = row.at(t0 - (W - 1) + k);
+    if (a.x1 != nullptr && t0 == 0) {        // the last W - 1 rows of the sequence, rows of x0 among them if it is short
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+            store_piece<T, V>((T *)a.x1 + ((size_t)b * (W - 1) + k) * E + e, kNarrow ? E : V, row.at(len - (W - 1) + k));
+    }
+    T *y = (T *)a.y + ((size_t)b * a.N + t0) * E + e;
     for (int t = t0; t < t1; t += kAhead) {
         Piece<T, V> next[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) next[j] = row.template at<kInside>(t + j);
+        for (int j = 0; j < kAhead; ++j) next[j] = row.at(t + j);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             float o[V];
@@ -75,47 +106,25 @@ __device__ __forceinline__ void conv_fwd_run(const Rows<T, W, kV<T>> &row, const
                     const int at = j + k - (W - 1);      // row of the tap among `win`, `next`
                     p = fmaf(f.w[k][i], at < 0 ? win[at + W - 1].get(i) : next[at].get(i), p);
                 }
-                o[i] = silu ? p * sigmoid(p) : p;
-                if (!kInside && t + j >= row.end) o[i] = 0.0f;
+                const float gate = sigmoid(p);
+                o[i] = t + j < len ? (a.silu ? p * gate : p) : 0.0f;
             }
-            if constexpr (kInside) store_row<T, V>(y + (size_t)(t + j) * E, V, o);
-            else if (t + j < t1) store_row<T, V>(y + (size_t)(t + j) * E, row.valid, o);
+            if (t + j < t1) store_to<kNarrow>(y, E, o);
+            y += E;
         }
 #pragma unroll
         for (int k = 0; k < W - 1; ++k) win[k] = next[kAhead - (W - 1) + k];
     }
 }
 
-template <typename T, int W> __global__ __launch_bounds__(256) void conv_fwd_kernel(const ConvArgs a) {
-    constexpr int V = kV<T>;
-    const int pieces = (a.E + V - 1) / V;
-    const long id = (long)blockIdx.x * 256 + threadIdx.x;
-    const long cut = id / pieces;
-    if (cut >= (long)a.B * a.runs) return;
-    const int e = (int)(id - cut * pieces) * V, b = (int)(cut / a.runs), t0 = (int)(cut - (long)b * a.runs) * a.run;
-    const int valid = a.E - e, t1 = min(t0 + a.run, a.N), len = length_of(a.lengths, b, a.N);
-    const Rows<T, W, V> row{(const T *)a.x + (size_t)b * a.N * a.ldx + e,
-                            a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * a.E + e, a.ldx, a.E, valid, len};
-    T *y = (T *)a.y + (size_t)b * a.N * a.E + e;
-    if (a.x1 != nullptr && t0 == 0) {        // the last W - 1 rows of the sequence, rows of x0 among them if it is short
-#pragma unroll
-        for (int k = 0; k < W - 1; ++k)
-            store_piece<T, V>((T *)a.x1 + ((size_t)b * (W - 1) + k) * a.E + e, valid, row.at(len - (W - 1) + k));
-    }
-    const Filter<W, V> f(a.w, a.bias, e, valid);
-    // runs are multiples of kAhead: a whole one that begins behind the first W - 1 tokens needs no masks
-    if (valid >= V && t0 >= W - 1 && t0 + a.run <= len) conv_fwd_run<T, W, true>(row, f, y, a.E, t0, t1, a.silu);
-    else conv_fwd_run<T, W, false>(row, f, y, a.E, t0, t1, a.silu);
-}
-
 // A run [t0, t1) of the gradient: dp_t = dy_t slope(p_t) for t0 <= t < t1 + W - 1 (the last W - 1 belong to the next run
 // and are formed again here), dx_t = sum_k w[k] dp_{t+W-1-k}, dw[k] = sum_t dp_t x_{t-W+1+k}, db = sum_t dp_t.
-// kInside: all of these tokens are there, and none of them is the first or last W - 1 of its sequence.
-template <typename T, int W, bool kInside>
-__device__ __forceinline__ void conv_bwd_run(const ConvArgs &a, const Rows<T, W, kVBwd> &row, const Filter<W, kVBwd> &f, const T *dy, T *dx,
-                                             size_t state, int t0, int t1, float (&dw)[W + 1][kVBwd]) {
+// kInside: all of these tokens are there, and none of them is among the first or last W - 1 of its sequence.
+template <typename T, int W, bool kNarrow, bool kInside>
+__device__ __forceinline__ void conv_bwd_run(const ConvArgs &a, const Rows<T, W, kVBwd, kNarrow> &row, const Rows<T, W, kVBwd, kNarrow> &grad,
+                                             const Filter<W, kVBwd> &f, T *dx, size_t state, int t0, int t1, float (&dw)[W + 1][kVBwd]) {
     constexpr int V = kVBwd;
-    const int valid = kInside ? V : row.valid, len = row.end;
+    const int E = a.E, len = row.end;
     float win[W - 1][V], dp[W][V] = {};      // x_{t-W+1} .. x_{t-1}; dp_{t-W+1} .. dp_t
 #pragma unroll
     for (int k = 0; k < W - 1; ++k) {
@@ -126,11 +135,7 @@ __device__ __forceinline__ void conv_bwd_run(const ConvArgs &a, const Rows<T, W,
     for (int t = t0; t < t1 + W - 1; t += kAhead) {
         Piece<T, V> nx[kAhead], nd[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int there = kInside || (t + j < t1 + W - 1 && t + j < len) ? valid : 0;
-            nx[j] = load_piece<T, V>(row.x + (size_t)(t + j) * a.ldx, there);
-            nd[j] = load_piece<T, V>(dy + (size_t)(t + j) * a.E, there);
-        }
+        for (int j = 0; j < kAhead; ++j) nx[j] = row.template at<kInside>(t + j), nd[j] = grad.template at<kInside>(t + j);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int now = t + j, out = now - (W - 1);
@@ -141,13 +146,12 @@ __device__ __forceinline__ void conv_bwd_run(const ConvArgs &a, const Rows<T, W,
                 float p = fmaf(f.w[W - 1][i], x, f.bias[i]);
 #pragma unroll
                 for (int k = 0; k < W - 1; ++k) p = fmaf(f.w[k][i], win[k][i], p);
-                float d = nd[j].get(i);
-                if (a.silu) d *= silu_slope(p, sigmoid(p));
-                if (!kInside && now >= len) d = 0.0f;
+                const float slope = silu_slope(p, sigmoid(p)), dy = nd[j].get(i);
+                // behind the sequence dy is zero, and so is whatever the taps make of its rows
+                const float d = a.silu ? dy * slope : dy, mine = now < t1 ? d : 0.0f;
 #pragma unroll
                 for (int k = 0; k < W - 1; ++k) dp[k][i] = dp[k + 1][i];
                 dp[W - 1][i] = d;
-                const float mine = now < t1 ? d : 0.0f;
 #pragma unroll
                 for (int k = 0; k < W - 1; ++k) dw[k][i] = fmaf(mine, win[k][i], dw[k][i]);
                 dw[W - 1][i] = fmaf(mine, x, dw[W - 1][i]);
@@ -159,43 +163,46 @@ __device__ __forceinline__ void conv_bwd_run(const ConvArgs &a, const Rows<T, W,
 #pragma unroll
                 for (int k = 0; k < W; ++k) o[i] = fmaf(f.w[k][i], dp[W - 1 - k][i], o[i]);
             }
-            if constexpr (kInside) {
-                if (out >= t0) store_row<T, V>(dx + (size_t)out * a.E, V, o);
-                continue;
-            }
-            // gradient that arrives at the rows handed on: x1 holds rows len - W + 1 .. len - 1
-            if (a.dx1 != nullptr && out >= len - (W - 1) && out < len) {
-                const Piece<T, V> g = load_piece<T, V>((const T *)a.dx1 + state + (size_t)(out - (len - (W - 1))) * a.E, valid);
+            T *to = dx + (long)out * E;
+            bool store = out >= t0 && out < t1;
+            if constexpr (!kInside) {
+                // gradient that arrives at the rows handed on: x1 holds rows len - W + 1 .. len - 1
+                if (a.dx1 != nullptr && out >= len - (W - 1) && out < len) {
+                    const Piece<T, V> g = load_row<kNarrow, T, V>((const T *)a.dx1 + state + (size_t)(out - (len - (W - 1))) * E, E);
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] += g.get(i);
+                    for (int i = 0; i < V; ++i) o[i] += g.get(i);
+                }
+                if (t0 == 0 && out < 0) to = (T *)a.dx0 + state + (size_t)(out + W - 1) * E, store = a.dx0 != nullptr;
             }
-            if (out >= t0 && out < t1) store_row<T, V>(dx + (size_t)out * a.E, valid, o);
-            else if (out < 0 && a.dx0 != nullptr && t0 == 0) store_row<T, V>((T *)a.dx0 + state + (size_t)(out + W - 1) * a.E, valid, o);
+            if (store) store_to<kNarrow>(to, E, o);
         }
     }
 }
 
 // lpr lanes take the pieces of a row side by side, 256 / lpr runs at once; their dw and db are added up in LDS.
-template <typename T, int W> __global__ __launch_bounds__(256) void conv_bwd_kernel(const ConvArgs a) {
+template <typename T, int W, bool kNarrow> __global__ __launch_bounds__(256) void conv_bwd_kernel(const ConvArgs a) {
     constexpr int V = kVBwd;
     __shared__ float red[256][V];
-    const int lane = threadIdx.x % a.lpr, slot = threadIdx.x / a.lpr, slots = 256 / a.lpr;
-    const int group = (int)(blockIdx.x % a.groups);
+    const int E = a.E, lane = threadIdx.x % a.lpr, slot = threadIdx.x / a.lpr, slots = 256 / a.lpr;
+    const int piece = (int)(blockIdx.x % a.groups) * a.lpr + lane, pieces = (E + V - 1) / V;
     const long set = blockIdx.x / a.groups, cut = set * slots + slot;
-    const int e = (group * a.lpr + lane) * V, valid = a.E - e;
+    const int e = first_channel<kNarrow, V>(piece, E);
     float dw[W + 1][V] = {};                 // dw[W]: db
-    if (cut < (long)a.B * a.runs && valid > 0) {
+    if (cut < (long)a.B * a.runs && piece < pieces) {
         const int b = (int)(cut / a.runs), t0 = (int)(cut - (long)b * a.runs) * a.run, t1 = min(t0 + a.run, a.N);
         const int len = length_of(a.lengths, b, a.N);
-        const Rows<T, W, V> row{(const T *)a.x + (size_t)b * a.N * a.ldx + e,
-                                a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * a.E + e, a.ldx, a.E, valid, len};
-        const T *dy = (const T *)a.dy + (size_t)b * a.N * a.E + e;
-        T *dx = (T *)a.dx + (size_t)b * a.N * a.E + e;
-        const size_t state = (size_t)b * (W - 1) * a.E + e;
-        const Filter<W, V> f(a.w, a.bias, e, valid);
-        // run + W - 1 is a multiple of kAhead: a whole run reads tokens up to t0 + run + W - 2, none masked
-        if (valid >= V && t0 >= W - 1 && t0 + a.run + W - 1 <= len) conv_bwd_run<T, W, true>(a, row, f, dy, dx, state, t0, t1, dw);
-        else conv_bwd_run<T, W, false>(a, row, f, dy, dx, state, t0, t1, dw);
+        const Rows<T, W, V, kNarrow> row{(const T *)a.x + (size_t)b * a.N * a.ldx + e,
+                                         a.x0 == nullptr ? nullptr : (const T *)a.x0 + (size_t)b * (W - 1) * E + e, a.ldx, E, len};
+        const Rows<T, W, V, kNarrow> grad{(const T *)a.dy + (size_t)b * a.N * E + e, nullptr, E, E, min(len, t1 + W - 1)};
+        T *dx = (T *)a.dx + (size_t)b * a.N * E + e;
+        const size_t state = (size_t)b * (W - 1) * E + e;
+        const Filter<W, V> f(a.w, a.bias, e, kNarrow ? E : V);
+        // run + W - 1 is a multiple of kAhead: a whole run reads tokens up to t0 + run + W - 2.  One path for all lanes of a wave:
+        // where it is cold, fetching the instructions of both takes longer than running one (2 x 133 x 72 bf16: 24 us, not 10),
+        // and the masked one alone is 11 % slower where few runs need it (8 x 2048 x 4096 bf16: 106 us, not 95).
+        const bool inside = t0 >= W - 1 && t0 + a.run + W - 1 <= len;
+        if (__all(inside)) conv_bwd_run<T, W, kNarrow, true>(a, row, grad, f, dx, state, t0, t1, dw);
+        else conv_bwd_run<T, W, kNarrow, false>(a, row, grad, f, dx, state, t0, t1, dw);
     }
     if (a.part == nullptr) return;
     for (int k = 0; k <= W; ++k) {
@@ -209,12 +216,13 @@ template <typename T, int W> __global__ __launch_bounds__(256) void conv_bwd_ker
         }
         __syncthreads();
         for (int c = threadIdx.x; c < a.lpr * V; c += 256) {
-            const int at = group * a.lpr * V + c;
-            if (at >= a.E) continue;
+            const int its = (int)(blockIdx.x % a.groups) * a.lpr + c / V, from = first_channel<kNarrow, V>(its, E), at = from + c % V;
+            // channels of the row's last piece that are the piece before's as well are left to that
+            if (its >= pieces || at >= E || at < its * V) continue;
             float v = 0.0f;
             for (int r = 0; r < slots; ++r) v += red[r * a.lpr + c / V][c % V];
             // [E][W] of the taps, then [E] of the bias, as the sums of all workgroups are handed out
-            a.part[(size_t)set * a.E * (W + 1) + (k < W ? (size_t)at * W + k : (size_t)a.E * W + at)] = v;
+            a.part[(size_t)set * E * (W + 1) + (k < W ? (size_t)at * W + k : (size_t)E * W + at)] = v;
         }
     }
 }
@@ -272,7 +280,11 @@ hipError_t launch_conv_fwd(ConvArgs a, int dtype, hipStream_t s) {
     while (a.run > 4 && a.B * pieces * ((a.N + a.run - 1) / a.run) < 256 * 1024) a.run /= 2;
     a.runs = (a.N + a.run - 1) / a.run;
     const long threads = (long)a.B * a.runs * pieces;
-    LA_CONV_DISPATCH(a.W, dtype, conv_fwd_kernel<TT, kW><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a));
+    const unsigned grid = (unsigned)((threads + 255) / 256);
+    LA_CONV_DISPATCH(a.W, dtype, {
+        if (a.E < kV<TT>) conv_fwd_kernel<TT, kW, true><<<grid, 256, 0, s>>>(a);
+        else conv_fwd_kernel<TT, kW, false><<<grid, 256, 0, s>>>(a);
+    });
     return hipGetLastError();
 }
 
@@ -281,10 +293,12 @@ long conv_plan_bwd(ConvArgs &a, int) {
     a.lpr = 64;
     while (a.lpr / 2 >= pieces && a.lpr > 1) a.lpr /= 2;
     a.groups = (pieces + a.lpr - 1) / a.lpr;
-    // 32 steps a run, W - 1 of them on the next run's tokens (64: 107 instead of 95 us at 8 x 2048 x 4096 bf16); 16 where
-    // those are too few threads
+    // 32 steps a run, W - 1 of them on the next run's tokens (64: 107 instead of 95 us at 8 x 2048 x 4096 bf16); 16 or 8
+    // where those are too few threads (3 x 2531 x 1001 fp32: 16 take 29 us, 8 take 36; 2 x 133 x 72 bf16: 15 and 12)
     int steps = 32;
-    while (steps > 16 && (long)a.B * pieces * ((a.N + steps - a.W) / (steps - a.W + 1)) < 192 * 1024) steps /= 2;
+    const auto threads = [&] { return (long)a.B * pieces * ((a.N + steps - a.W) / (steps - a.W + 1)); };
+    if (threads() < 192 * 1024) steps = 16;
+    if (threads() < 16 * 1024) steps = 8;
     a.run = steps - (a.W - 1);
     a.runs = (a.N + a.run - 1) / a.run;
     const long cuts = (long)a.B * a.runs, slots = 256 / a.lpr;
@@ -294,7 +308,11 @@ long conv_plan_bwd(ConvArgs &a, int) {
 hipError_t launch_conv_bwd(const ConvArgs &a, int dtype, hipStream_t s) {
     ConvArgs p = a;
     const long sets = conv_plan_bwd(p, dtype);
-    LA_CONV_DISPATCH(a.W, dtype, conv_bwd_kernel<TT, kW><<<(unsigned)(sets * p.groups), 256, 0, s>>>(p));
+    const unsigned grid = (unsigned)(sets * p.groups);
+    LA_CONV_DISPATCH(a.W, dtype, {
+        if (a.E < kVBwd) conv_bwd_kernel<TT, kW, true><<<grid, 256, 0, s>>>(p);
+        else conv_bwd_kernel<TT, kW, false><<<grid, 256, 0, s>>>(p);
+    });
     return hipGetLastError();
 }
 

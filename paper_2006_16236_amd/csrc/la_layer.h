@@ -121,11 +121,12 @@ struct NormArgs {
     const void *dy;
     const float *gamma, *beta, *mean_in, *rstd_in;
     void *y, *s;                     // forward: result, the sum or NULL; backward: dx
-    float *mean, *rstd, *part;       // part: [groups][2][E]
+    float *mean, *rstd, *part;       // part: [groups][2][E], or with one group straight to
+    float *dgamma, *dbeta;
     int rows, E;
     float eps;
 };
-int norm_groups(int rows, int E);    // workgroups of the backward, one partial sum of the weights' gradients each
+int norm_groups(int rows, int E, int dtype);    // workgroups of the backward, one partial sum of the weights' gradients each
 hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s);
 

@@ -24,7 +24,7 @@ int norm_sizes(int rows, int E, la_dtype t) {
     if (E > kMaxNorm) return LA_ERR_UNSUPPORTED;
     return LA_OK;
 }
-size_t norm_bytes(int rows, int E) { return align256((size_t)la::norm_groups(rows, E) * 2 * E * sizeof(float)); }
+size_t norm_bytes(int rows, int E, la_dtype t) { return align256((size_t)la::norm_groups(rows, E, t) * 2 * E * sizeof(float)); }
 
 // ---- convolution --------------------------------------------------------------------------------
 int conv_sizes(int B, int N, int E, int W, la_dtype t) {
@@ -104,7 +104,7 @@ int la_norm_fwd(const void *x, const void *r, const float *gamma, const float *b
     return hip_status(la::launch_norm_fwd(a, t, static_cast<hipStream_t>(stream)));
 }
 
-size_t la_norm_bwd_workspace(int rows, int E, la_dtype t) { return norm_sizes(rows, E, t) == LA_OK ? norm_bytes(rows, E) : 0; }
+size_t la_norm_bwd_workspace(int rows, int E, la_dtype t) { return norm_sizes(rows, E, t) == LA_OK ? norm_bytes(rows, E, t) : 0; }
 
 int la_norm_bwd(const void *s, const float *gamma, const float *mean, const float *rstd, const void *dy, const void *ds, void *dx,
                 float *dgamma, float *dbeta, int rows, int E, la_dtype t, void *ws, size_t ws_bytes, void *stream) {
@@ -113,7 +113,7 @@ int la_norm_bwd(const void *s, const float *gamma, const float *mean, const floa
     if (st != LA_OK) return st;
     if (any_misaligned(s, gamma, mean, rstd, dy, ds, dx, dgamma, dbeta, ws)) return LA_ERR_ALIGN;
     const bool sums = dgamma != nullptr || dbeta != nullptr;
-    const size_t need = sums ? norm_bytes(rows, E) : 0;
+    const size_t need = sums ? norm_bytes(rows, E, t) : 0;
     if (need > 0 && (ws == nullptr || ws_bytes < need)) return LA_ERR_WORKSPACE;
     const size_t n = (size_t)rows * E * esize_of(t), col = (size_t)E * 4, per = (size_t)rows * 4;
     const Span outs[] = {{dx, n}, {dgamma, span_of(dgamma, col)}, {dbeta, span_of(dbeta, col)}, {ws, need}};
@@ -121,12 +121,13 @@ int la_norm_bwd(const void *s, const float *gamma, const float *mean, const floa
     if (aliased(outs, ins)) return LA_ERR_ALIAS;
     la::NormArgs a{};
     a.x = s, a.r = ds, a.dy = dy, a.gamma = gamma, a.mean_in = mean, a.rstd_in = rstd, a.y = dx;
-    a.part = sums ? static_cast<float *>(ws) : nullptr;
+    a.part = sums ? static_cast<float *>(ws) : nullptr, a.dgamma = dgamma, a.dbeta = dbeta;
     a.rows = rows, a.E = E;
     hipStream_t q = static_cast<hipStream_t>(stream);
     const int launched = hip_status(la::launch_norm_bwd(a, t, q));
-    if (launched != LA_OK || !sums) return launched;
-    return hip_status(la::launch_sum_rows(a.part, la::norm_groups(rows, E), {{dgamma, dbeta, nullptr}, {E, E, 0}}, q));
+    const int groups = la::norm_groups(rows, E, t);
+    if (launched != LA_OK || !sums || groups == 1) return launched;
+    return hip_status(la::launch_sum_rows(a.part, groups, {{dgamma, dbeta, nullptr}, {E, E, 0}}, q));
 }
 
 int la_conv_fwd(const void *x, int ldx, const float *w, const float *bias, const void *x0, const int *lengths, void *y, void *x1,

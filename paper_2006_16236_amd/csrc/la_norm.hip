@@ -2,8 +2,9 @@
 //
 // Bound by memory: forward 2 tensors (4 with a residual and its sum), backward 3 (4).  A row lives in the
 // registers of the lanes that share it, so that each element is read once: mean, then the sum of squares around it
-// (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  64 lanes share rows
-// up to 1024 elements (backward 2048, whose sums per column then need no barrier), 256 up to 8192, 1024 (backward 512) up to 16384.
+// (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  16 or 32 lanes share a row
+// of as many 16-byte pieces, 64 one of up to 1024 elements (backward 2048, whose sums per column then need no barrier), 256 up to
+// 8192, 1024 (backward 512) up to 16384.
 #include "la_layer.h"
 
 namespace la {
@@ -43,8 +44,13 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict_
 }
 
 // sum over the TPR lanes that share a row; `red`: one slot per wave of the workgroup
+template <int TPR> __device__ __forceinline__ float lanes_sum(float v) {        // within a wave
+    if constexpr (TPR == 16) return row_sum16(v);
+    else if constexpr (TPR == 32) return add_rows(row_sum16(v));
+    else return wave_sum(v);
+}
 template <int TPR> __device__ __forceinline__ float row_sum(float v, float *red) {
-    v = wave_sum(v);
+    v = lanes_sum<TPR>(v);
     if constexpr (TPR > kWave) {
         const int wave = threadIdx.x / kWave, first = wave / (TPR / kWave) * (TPR / kWave);
         __syncthreads();
@@ -71,7 +77,7 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? 
     }
     for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
     const long row = first + threadIdx.x / TPR;
-    const bool live = row < a.rows;          // whole waves; all of a workgroup's waves meet in row_sum
+    const bool live = row < a.rows;          // all lanes meet in row_sum
     float f[NV][V];
     float sum = 0.0f;
 #pragma unroll
@@ -151,7 +157,7 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads)
                 db[j][i] += dy;
             }
         }
-        s1 = wave_sum(s1), s2 = wave_sum(s2);
+        s1 = lanes_sum<TPR>(s1), s2 = lanes_sum<TPR>(s2);
         if constexpr (TPR > kWave) {
             const int wave = threadIdx.x / kWave, w0 = wave / (TPR / kWave) * (TPR / kWave);
             __syncthreads();
@@ -198,17 +204,25 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads)
     gather(dg);
     gather(db);
     if (slot != 0) return;
+    float *pg = a.part + (size_t)blockIdx.x * 2 * E, *pb = pg + E;
+    if (gridDim.x == 1) pg = a.dgamma, pb = a.dbeta;                     // a part that is the whole
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int e = (j * TPR + l) * V;
-        store_row<float, V>(a.part + (size_t)blockIdx.x * 2 * E + e, E - e, dg[j]);
-        store_row<float, V>(a.part + (size_t)blockIdx.x * 2 * E + E + e, E - e, db[j]);
+        if (pg != nullptr) store_row<float, V>(pg + e, E - e, dg[j]);
+        if (pb != nullptr) store_row<float, V>(pb + e, E - e, db[j]);
     }
 }
 
 // forward: beyond 8192 elements 16 a lane again (4096 x 16384 bf16: 512 lanes of 32 take 137 us, 1024 of 16 take 106)
-int lanes_of(int E) { return E <= 1024 ? 64 : E <= 8192 ? 256 : 1024; }
-int lanes_of_bwd(int E) { return E <= 2048 ? 64 : E <= 8192 ? 256 : 512; }
+int lanes_of(int E, int dtype) {
+    const int pieces = dtype == 0 ? (E + 3) / 4 : (E + 7) / 8;
+    return pieces <= 16 ? 16 : pieces <= 32 ? 32 : E <= 1024 ? 64 : E <= 8192 ? 256 : 1024;
+}
+int lanes_of_bwd(int E, int dtype) {
+    const int pieces = dtype == 0 ? (E + 3) / 4 : (E + 7) / 8;
+    return pieces <= 16 ? 16 : pieces <= 32 ? 32 : E <= 2048 ? 64 : E <= 8192 ? 256 : 512;
+}
 
 }  // namespace
 
@@ -220,8 +234,8 @@ hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, 
 
 // Two workgroups a compute unit, or one where more than 16 elements a lane leave room for no more (16384 x 2048 bf16: 62 us
 // with 512 workgroups, 55 with 256; 16384 x 4096: 113 and 140).
-int norm_groups(int rows, int E) {
-    const int tpr = lanes_of_bwd(E), per = kBwdThreads / tpr, most = E > 16 * tpr ? 256 : 512;
+int norm_groups(int rows, int E, int dtype) {
+    const int tpr = lanes_of_bwd(E, dtype), per = kBwdThreads / tpr, most = E > 16 * tpr ? 256 : 512;
     const long sets = ((long)rows + per - 1) / per, turns = (sets + most - 1) / most;      // equal shares
     return (int)((sets + turns - 1) / turns);
 }
@@ -240,9 +254,13 @@ hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
         const long sets = ((long)a.rows + per - 1) / per;                                                            \
         norm_fwd_kernel<T, TPR, NV><<<(unsigned)(sets < most ? sets : most), threads, 0, s>>>(a);                    \
     } while (0)
-    const int tpr = lanes_of(a.E), nv = pieces_of(a.E, tpr, dtype);
+    const int tpr = lanes_of(a.E, dtype), nv = pieces_of(a.E, tpr, dtype);
     if (dtype == 0) {
-        if (tpr == 64) {
+        if (tpr == 16) {
+            LA_KERNEL(float, 16, 1);
+        } else if (tpr == 32) {
+            LA_KERNEL(float, 32, 1);
+        } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(float, 64, 1);
             else if (nv == 2) LA_KERNEL(float, 64, 2);
             else LA_KERNEL(float, 64, 4);
@@ -254,7 +272,11 @@ hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
             LA_KERNEL(float, 1024, 4);
         }
     } else {
-        if (tpr == 64) {
+        if (tpr == 16) {
+            LA_KERNEL(bf16_t, 16, 1);
+        } else if (tpr == 32) {
+            LA_KERNEL(bf16_t, 32, 1);
+        } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
             else LA_KERNEL(bf16_t, 64, 2);
         } else if (tpr == 256) {
@@ -271,9 +293,13 @@ hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
 
 hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
 #define LA_KERNEL(T, TPR, NV) norm_bwd_kernel<T, TPR, NV><<<groups, kBwdThreads, 0, s>>>(a)
-    const int groups = norm_groups(a.rows, a.E), tpr = lanes_of_bwd(a.E), nv = pieces_of(a.E, tpr, dtype);
+    const int groups = norm_groups(a.rows, a.E, dtype), tpr = lanes_of_bwd(a.E, dtype), nv = pieces_of(a.E, tpr, dtype);
     if (dtype == 0) {
-        if (tpr == 64) {
+        if (tpr == 16) {
+            LA_KERNEL(float, 16, 1);
+        } else if (tpr == 32) {
+            LA_KERNEL(float, 32, 1);
+        } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(float, 64, 1);
             else if (nv == 2) LA_KERNEL(float, 64, 2);
             else if (nv <= 4) LA_KERNEL(float, 64, 4);
@@ -285,7 +311,11 @@ hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
             LA_KERNEL(float, 512, 8);
         }
     } else {
-        if (tpr == 64) {
+        if (tpr == 16) {
+            LA_KERNEL(bf16_t, 16, 1);
+        } else if (tpr == 32) {
+            LA_KERNEL(bf16_t, 32, 1);
+        } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
             else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);
             else LA_KERNEL(bf16_t, 64, 4);
