@@ -361,7 +361,8 @@ int la_recurrent_steps(const void *q, const void *k, const void *v, float *S, fl
  *              the outputs (and of the gradients) are zero, and the state handed out is that behind the
  *              last real token.  0 is a sequence without tokens; values outside 0 .. N are taken as
  *              the nearest of these.
- *   LA_ERR_SHAPE also for sizes whose launch would not fit a grid: B * N * E from 2^36 on, and as said below.
+ *   LA_ERR_SHAPE also for sizes whose launch would not fit a grid: B * N * E from 2^36 on, N (of a convolution also E)
+ *              beyond 2^30, and as said below.
  *   Non-finite inputs are outside the contract, but for causality: outputs before token t do not
  *              depend on what the tensors hold from token t on, and rows behind lengths[b] may hold anything.
  */

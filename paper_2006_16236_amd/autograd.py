@@ -9,6 +9,7 @@ per-position state is stored (the constant-memory backward of section 3.3.1).
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as _b
 from . import layer as _l
@@ -127,6 +128,7 @@ class _LayerNorm(torch.autograd.Function):
         return y if s is None else (y, s)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, ds=None):
         s, gamma, mean, rstd = ctx.saved_tensors
         has_gamma, has_beta, has_residual = ctx.has
@@ -160,6 +162,7 @@ class _CausalConv(torch.autograd.Function):
         return y, x1
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dx1):
         x, w, bias, state, lengths = ctx.saved_tensors
         if dy is None and dx1 is None:
@@ -194,6 +197,7 @@ class _SelectiveScan(torch.autograd.Function):
         return y, h1
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh1):
         x, dt, A, Bt, Ct, D, z, dt_bias, state, lengths, ws = ctx.saved_tensors
         if dy is None and dh1 is None:

@@ -15,6 +15,9 @@ size_t span_of(const void *p, size_t bytes) { return p == nullptr ? 0 : bytes; }
 template <typename... Ps> bool any_misaligned(Ps... p) { return (misaligned(p) || ...); }
 template <typename... Ps> bool any_null(Ps... p) { return ((p == nullptr) || ...); }
 
+// Tokens are counted in int, a run, a tile or two tiles ahead of the last one, and channels rounded up to a piece.
+constexpr int kMostInt = 1 << 30;
+
 // ---- layer norm ---------------------------------------------------------------------------------
 constexpr int kMaxNorm = 16384;
 
@@ -30,7 +33,7 @@ size_t norm_bytes(int rows, int E, la_dtype t) { return align256((size_t)la::nor
 int conv_sizes(int B, int N, int E, int W, la_dtype t) {
     if (!known(t)) return LA_ERR_UNSUPPORTED;
     if (W < 2 || W > 4) return LA_ERR_UNSUPPORTED;
-    if (B < 1 || N < 1 || E < 1) return LA_ERR_SHAPE;
+    if (B < 1 || N < 1 || E < 1 || N > kMostInt || E > kMostInt) return LA_ERR_SHAPE;
     if ((double)B * N * E >= 68719476736.0) return LA_ERR_SHAPE;                                    // 2^36
     if ((double)B * ((double)(N - 1) / 8 + 1) * (E / 4 + 1.0) >= 2147483648.0) return LA_ERR_SHAPE;  // threads of a launch
     return LA_OK;
@@ -44,7 +47,7 @@ size_t conv_bytes(int B, int N, int E, int W, la_dtype t) {
 // ---- scan ---------------------------------------------------------------------------------------
 int scan_sizes(int B, int N, int E, int G, int S, la_dtype t, int flags) {
     if (!known(t) || !(S == 8 || S == 16 || S == 32) || (flags & ~(LA_SCAN_SOFTPLUS | LA_SCAN_KEEP)) != 0) return LA_ERR_UNSUPPORTED;
-    if (B < 1 || N < 1 || E < 1 || G < 1 || E % G != 0) return LA_ERR_SHAPE;
+    if (B < 1 || N < 1 || E < 1 || G < 1 || E % G != 0 || N > kMostInt) return LA_ERR_SHAPE;
     if ((double)B * N * E >= 68719476736.0 || (double)B * E >= 268435456.0) return LA_ERR_SHAPE;     // 2^36, 2^28
     if ((double)B * la::scan_blocks(E, G) >= 8388608.0) return LA_ERR_SHAPE;                         // 2^23 workgroups
     if ((double)B * N * G * S >= 68719476736.0 || (double)G * S >= 2147483648.0) return LA_ERR_SHAPE;

@@ -274,7 +274,7 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
 #pragma unroll
     for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, g[n] = 0.0f;
     const float bias = a.bias == nullptr ? 0.0f : a.bias[e];
-    const int tokens = w.end - w.t0, tiles = tokens > 0 ? (tokens + T - 1) / T : 0, last = w.t0 + (tiles - 1) * T;
+    const int tokens = w.end - w.t0, tiles = tokens > 0 ? (tokens + T - 1) / T : 0;
     Pairs<TT, NW, P> pairs(a, w, bc);
     const size_t row = (size_t)w.b * a.N + w.t0;
     const bool gated = a.z != nullptr;
@@ -590,7 +590,7 @@ template <typename TT, int S> __global__ __launch_bounds__(256) void scan_step_k
     const int e = (blockIdx.x - b * wide) * (256 / L) + threadIdx.x / L, q = threadIdx.x % L;
     if (e >= a.E) return;
     const size_t at = (size_t)b * a.E + e, g = (size_t)b * a.G + e / (a.E / a.G);
-    float s[4], A[4], B[4], C[4];
+    float s[4], A[4];
     __builtin_memcpy(s, h + at * S + q * 4, sizeof(s));
     __builtin_memcpy(A, a.A + (size_t)e * S + q * 4, sizeof(A));
     const Piece<TT, 4> pb = load_piece<TT, 4>((const TT *)a.Bt + g * S + q * 4, 4), pc = load_piece<TT, 4>((const TT *)a.Ct + g * S + q * 4, 4);

@@ -31,7 +31,15 @@ def _code(name, t):
 def _dims(name, t, n):
     if t.dim() != n:
         raise ValueError(f"{name} must have {n} dimensions, not {t.dim()}")
-    return tuple(t.shape)
+    return _ints(f"a size of {name}", *t.shape)
+
+
+def _ints(what, *sizes):
+    """The sizes, each one that the C ABI's int holds (ctypes would cut off the rest)."""
+    for n in sizes:
+        if n > 0x7FFFFFFF:
+            raise ValueError(f"{what} is {n}, at most {0x7FFFFFFF} is possible")
+    return sizes
 
 
 def _rows(name, t, shape, dtype, device, optional=False):
@@ -57,7 +65,7 @@ def _rows(name, t, shape, dtype, device, optional=False):
     ld = stride[1] if N > 1 else stride[0] if B > 1 else width
     if ld < width or (B > 1 and stride[0] != N * ld):
         raise ValueError(f"{name}: the tokens of all sequences must lie at one distance")
-    return ld
+    return _ints(f"{name}: the distance between tokens", ld)[0]
 
 
 def _run(where, device, stream, call):
@@ -78,10 +86,16 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(ws, need, device):
-    """The caller's workspace, or a new one."""
+def _workspace(ws, need, device, stream):
+    """The caller's workspace, or a new one of the memory of the stream that uses it."""
     if ws is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        if stream is None or device.type != "cuda":
+            return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = int(getattr(stream, "cuda_stream", stream))
+            stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
+            return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
     _bytes("ws", ws, device)
     return ws
 
@@ -106,6 +120,7 @@ def la_norm_fwd(x, gamma, beta, y, mean=None, rstd=None, r=None, s=None, eps=1e-
     if len(shape) < 1:
         raise ValueError("x must have at least one dimension")
     E, lead = shape[-1], shape[:-1]
+    _ints("the number of rows or their width", lead.numel(), E)
     _like("x", x, shape, dt, dev)
     _like("y", y, shape, dt, dev)
     _like("r", r, shape, dt, dev, optional=True)
@@ -133,6 +148,7 @@ def la_norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ds=None, 
     if len(shape) < 1:
         raise ValueError("s must have at least one dimension")
     E, lead = shape[-1], shape[:-1]
+    _ints("the number of rows or their width", lead.numel(), E)
     for name, v in (("s", s), ("dy", dy), ("dx", dx)):
         _like(name, v, shape, dt, dev)
     _like("ds", ds, shape, dt, dev, optional=True)
@@ -144,7 +160,7 @@ def la_norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ds=None, 
         raise ValueError(f"s: shape {tuple(shape)} is empty")
     rows = lead.numel()
     if dgamma is not None or dbeta is not None:
-        ws = _workspace(ws, la_norm_bwd_workspace(rows, E, t), dev)
+        ws = _workspace(ws, la_norm_bwd_workspace(rows, E, t), dev, stream)
     _run("la_norm_bwd", dev, stream,
          lambda q: _lib.la_norm_bwd(_p(s), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(ds), _p(dx), _p(dgamma), _p(dbeta),
                                     rows, E, t, _p(ws), 0 if ws is None else _size(ws), q))
@@ -162,7 +178,7 @@ def _conv_checks(x, w, bias, n):
     shape = _dims("x", x, n)
     if not isinstance(w, torch.Tensor) or w.dim() != 2:
         raise ValueError("w must be a tensor [E, W]")
-    E, W = shape[-1], w.shape[1]
+    E, W = shape[-1], _dims("w", w, 2)[1]
     _like("w", w, (E, W), _F32, dev)
     _like("bias", bias, (E,), _F32, dev, optional=True)
     return t, dt, dev, shape, W
@@ -203,7 +219,7 @@ def la_conv_bwd(x, w, bias, dy, dx, dw=None, db=None, x0=None, dx1=None, dx0=Non
     _like("db", db, (E,), _F32, dev, optional=True)
     _like("lengths", lengths, (B,), torch.int32, dev, optional=True)
     if dw is not None or db is not None:
-        ws = _workspace(ws, la_conv_bwd_workspace(B, N, E, W, t), dev)
+        ws = _workspace(ws, la_conv_bwd_workspace(B, N, E, W, t), dev, stream)
     _run("la_conv_bwd", dev, stream,
          lambda q: _lib.la_conv_bwd(_p(x), ldx, _p(w), _p(bias), _p(x0), _p(lengths), _p(dy), _p(dx1), _p(dx), _p(dw), _p(db),
                                     _p(dx0), B, N, E, W, int(silu), t, _p(ws), 0 if ws is None else _size(ws), q))
@@ -242,7 +258,7 @@ class _Scan:
         self.B, self.N, self.E = B, N, E = _dims("x", x, 3)
         if not isinstance(Bt, torch.Tensor) or Bt.dim() != 4:
             raise ValueError("Bt must be a tensor [B, N, G, S]")
-        self.G, self.S = G, S = Bt.shape[2], Bt.shape[3]
+        self.G, self.S = G, S = _dims("Bt", Bt, 4)[2:]
         if G < 1 or E % G:
             raise ValueError(f"Bt: {G} groups do not divide {E} channels")
         rows, bc = (B, N, E), (B, N, G, S)
@@ -279,7 +295,7 @@ def la_scan_fwd(x, dt, A, Bt, Ct, y, D=None, z=None, dt_bias=None, h0=None, h1=N
     _like("y", y, k.rows, k.dtype, k.dev)
     k.states(h0=h0, h1=h1)
     flags = (LA_SCAN_SOFTPLUS if softplus else 0) | (LA_SCAN_KEEP if keep else 0)
-    ws = _workspace(ws, la_scan_fwd_workspace(*k.dims, k.t, flags), k.dev)
+    ws = _workspace(ws, la_scan_fwd_workspace(*k.dims, k.t, flags), k.dev, stream)
     _run("la_scan_fwd", k.dev, stream,
          lambda q: _lib.la_scan_fwd(*k.inputs(x, dt, z, Bt, Ct), _p(A), _p(D), _p(dt_bias), _p(h0), _p(lengths), _p(y), _p(h1),
                                     *k.dims, flags, k.t, _p(ws), _size(ws), q))
@@ -316,7 +332,7 @@ def la_scan_bwd(x, dt, A, Bt, Ct, dy, dx, ddt, dA, dB, dC, D=None, z=None, dt_bi
         need = la_scan_fwd_workspace(*k.dims, k.t, flags | kept)
         if _size(fwd_ws) < need:
             raise ValueError(f"fwd_ws: {_size(fwd_ws)} bytes, {need} expected: not a workspace of la_scan_fwd(keep=True) on these sizes")
-    ws = _workspace(ws, la_scan_bwd_workspace(*k.dims, k.t, flags | kept), k.dev)
+    ws = _workspace(ws, la_scan_bwd_workspace(*k.dims, k.t, flags | kept), k.dev, stream)
     _run("la_scan_bwd", k.dev, stream,
          lambda q: _lib.la_scan_bwd(*k.inputs(x, dt, z, Bt, Ct), _p(A), _p(D), _p(dt_bias), _p(h0), _p(lengths), _p(fwd_ws),
                                     _p(dy), _p(dh1), _p(dx), _p(ddt), _p(dz), _p(dB), _p(dC), _p(dA), _p(dD), _p(ddt_bias),
@@ -333,7 +349,7 @@ def la_scan_step(x, dt, A, Bt, Ct, h, y, D=None, z=None, dt_bias=None, softplus=
     B, E = _dims("x", x, 2)
     if not isinstance(Bt, torch.Tensor) or Bt.dim() != 3:
         raise ValueError("Bt must be a tensor [B, G, S]")
-    G, S = Bt.shape[1:]
+    G, S = _dims("Bt", Bt, 3)[1:]
     if G < 1 or E % G:
         raise ValueError(f"Bt: {G} groups do not divide {E} channels")
     for name, v in (("x", x), ("dt", dt), ("y", y)):

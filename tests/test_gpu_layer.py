@@ -378,6 +378,23 @@ def test_calls_run_on_the_current_and_on_a_given_stream():
     assert torch.equal(y, y2)
 
 
+def test_a_workspace_belongs_to_the_stream_that_uses_it():
+    """Allocated by the call for a given stream: once it is dropped, the current stream must not be handed its memory."""
+    d, a = scan_data(2, 150, 64, 1, 16, None, False, True, False, False, "f32")
+    t = {n: d.dev(v, f32=n in F32_NAMES) for n, v in a.items() if v is not None}
+    side, y, y2 = torch.cuda.Stream(), torch.empty_like(t["x"]), torch.empty_like(t["x"])
+    la.la_scan_fwd(t["x"], t["dt"], t["A"], t["Bt"], t["Ct"], y2)
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        ws = la.la_scan_fwd(t["x"], t["dt"], t["A"], t["Bt"], t["Ct"], y, keep=True, stream=stream)
+        at, size = ws.data_ptr(), ws.numel()
+        del ws
+        others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        assert at not in [o.data_ptr() for o in others]
+        side.synchronize()
+        assert torch.equal(y, y2)
+
+
 def test_a_captured_layer_replays():
     """norm, convolution, scan forward and backward in one graph, replayed on new inputs between eager calls."""
     B, N, E, S, W = 2, 140, 72, 16, 4

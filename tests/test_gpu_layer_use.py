@@ -171,6 +171,17 @@ def test_autograd_on_a_side_stream_and_twice_through_one_leaf():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_second_derivatives_are_refused():
+    """The gradient kernels have no gradient of their own: asking for one must not leave a term out in silence."""
+    x = torch.randn(2, 20, E, device=DEV, requires_grad=True)
+    w = torch.randn(E, W, device=DEV, requires_grad=True)
+    A, Bt = -torch.rand(E, S, device=DEV), torch.randn(2, 20, 1, S, device=DEV)
+    for y in (la.layer_norm(x), la.causal_conv(x, w)[0], la.selective_scan(x, x, A, Bt, Bt)[0]):
+        g, = torch.autograd.grad((y * x).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.sum().backward()
+
+
 # ---- edges --------------------------------------------------------------------------------------------------
 
 def test_what_follows_a_token_does_not_reach_it():

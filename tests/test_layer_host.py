@@ -181,3 +181,30 @@ def test_the_cut_covers_every_token_once(b):
                 if tiles < 8:
                     assert room == 0
                 assert room <= (tiles // 4) * (E * S * 4 + E * 4) + 512
+
+
+def test_sizes_beyond_int_are_refused(b):
+    """int holds a size, and int what is counted beyond it; ctypes would take the lower 32 bits of any number."""
+    import paper_2006_16236_amd as la
+    lib = b.raw()
+    args = (at(1), None, None, None, at(2), None)
+    for n in ((1 << 30) + 1, (1 << 31) - 1):
+        assert lib.la_conv_fwd(at(0), 4, *args, 1, n, 4, 4, 1, 0, NULL) == b.LA_ERR_SHAPE
+        assert lib.la_conv_fwd(at(0), n, *args, 1, 1, n, 4, 1, 0, NULL) == b.LA_ERR_SHAPE
+        assert lib.la_conv_bwd_workspace(1, n, 1, 4, 0) == 0 and lib.la_conv_bwd_workspace(1, 1, n, 4, 0) == 0
+        assert lib.la_scan_fwd_workspace(1, n, 1, 1, 8, 0, 1) == 0 and lib.la_scan_bwd_workspace(1, n, 1, 1, 8, 0, 1) == 0
+    assert lib.la_conv_bwd_workspace(1, 1 << 30, 1, 4, 0) > 0 and lib.la_scan_fwd_workspace(1, 1 << 30, 1, 1, 8, 0, 3) > 0
+    # tensors that are all strides: nothing is allocated
+    far = torch.empty((1 << 32) + 128, device="meta").as_strided((2, 1, 4), ((1 << 32) + 64, 4, 1))
+    w, v, y = (torch.empty(s, device="meta") for s in ((4, 4), (4,), (2, 1, 4)))
+    with pytest.raises(ValueError, match="x: the distance between tokens is 4294967360"):
+        la.la_conv_fwd(far, w, v, y)
+    long = torch.empty((1 << 32) + 4, 1, device="meta")
+    with pytest.raises(ValueError, match="number of rows"):
+        la.la_norm_fwd(long, None, None, long)
+    stat = torch.empty((1 << 32) + 4, device="meta")
+    with pytest.raises(ValueError, match="number of rows"):
+        la.la_norm_bwd(long, None, stat, stat, long, long)
+    many = torch.empty(1, (1 << 32) + 4, 1, device="meta")
+    with pytest.raises(ValueError, match="a size of x"):
+        la.la_conv_fwd(many, torch.empty(1, 4, device="meta"), None, many)
