@@ -288,7 +288,7 @@ hipError_t launch_conv_fwd(ConvArgs a, int dtype, hipStream_t s) {
     return hipGetLastError();
 }
 
-long conv_plan_bwd(ConvArgs &a, int) {
+long conv_plan_bwd(ConvArgs &a) {
     const int pieces = (a.E + kVBwd - 1) / kVBwd;
     a.lpr = 64;
     while (a.lpr / 2 >= pieces && a.lpr > 1) a.lpr /= 2;
@@ -307,7 +307,7 @@ long conv_plan_bwd(ConvArgs &a, int) {
 
 hipError_t launch_conv_bwd(const ConvArgs &a, int dtype, hipStream_t s) {
     ConvArgs p = a;
-    const long sets = conv_plan_bwd(p, dtype);
+    const long sets = conv_plan_bwd(p);
     const unsigned grid = (unsigned)(sets * p.groups);
     LA_CONV_DISPATCH(a.W, dtype, {
         if (a.E < kVBwd) conv_bwd_kernel<TT, kW, true><<<grid, 256, 0, s>>>(p);

@@ -142,7 +142,7 @@ struct ConvArgs {
     bool silu;
 };
 // how a backward cuts its tokens: sets run, runs, lpr, groups; the number of partial sums per channel
-long conv_plan_bwd(ConvArgs &a, int dtype);
+long conv_plan_bwd(ConvArgs &a);
 hipError_t launch_conv_fwd(ConvArgs a, int dtype, hipStream_t s);
 hipError_t launch_conv_bwd(const ConvArgs &a, int dtype, hipStream_t s);
 // x [B, E], state [B, W - 1, E] in and out

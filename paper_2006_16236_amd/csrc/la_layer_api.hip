@@ -38,10 +38,10 @@ int conv_sizes(int B, int N, int E, int W, la_dtype t) {
     if ((double)B * ((double)(N - 1) / 8 + 1) * (E / 4 + 1.0) >= 2147483648.0) return LA_ERR_SHAPE;  // threads of a launch
     return LA_OK;
 }
-size_t conv_bytes(int B, int N, int E, int W, la_dtype t) {
+size_t conv_bytes(int B, int N, int E, int W) {
     la::ConvArgs a{};
     a.B = B, a.N = N, a.E = E, a.W = W;
-    return align256((size_t)la::conv_plan_bwd(a, t) * E * (W + 1) * sizeof(float));
+    return align256((size_t)la::conv_plan_bwd(a) * E * (W + 1) * sizeof(float));
 }
 
 // ---- scan ---------------------------------------------------------------------------------------
@@ -152,7 +152,7 @@ int la_conv_fwd(const void *x, int ldx, const float *w, const float *bias, const
 }
 
 size_t la_conv_bwd_workspace(int B, int N, int E, int W, la_dtype t) {
-    return conv_sizes(B, N, E, W, t) == LA_OK ? conv_bytes(B, N, E, W, t) : 0;
+    return conv_sizes(B, N, E, W, t) == LA_OK ? conv_bytes(B, N, E, W) : 0;
 }
 
 int la_conv_bwd(const void *x, int ldx, const float *w, const float *bias, const void *x0, const int *lengths, const void *dy,
@@ -164,7 +164,7 @@ int la_conv_bwd(const void *x, int ldx, const float *w, const float *bias, const
     if (bad_rows(ldx, E)) return LA_ERR_SHAPE;
     if (any_misaligned(x, w, bias, x0, lengths, dy, dx1, dx, dw, db, dx0, ws)) return LA_ERR_ALIGN;
     const bool sums = dw != nullptr || db != nullptr;
-    const size_t need = sums ? conv_bytes(B, N, E, W, t) : 0;
+    const size_t need = sums ? conv_bytes(B, N, E, W) : 0;
     if (need > 0 && (ws == nullptr || ws_bytes < need)) return LA_ERR_WORKSPACE;
     const size_t rows = (size_t)B * N, e = esize_of(t), state = (size_t)B * (W - 1) * E * e, taps = (size_t)E * W * 4, col = (size_t)E * 4;
     const Span outs[] = {{dx, rows * E * e}, {dw, span_of(dw, taps)}, {db, span_of(db, col)}, {dx0, span_of(dx0, state)}, {ws, need}};
@@ -175,7 +175,7 @@ int la_conv_bwd(const void *x, int ldx, const float *w, const float *bias, const
     a.x = x, a.x0 = x0, a.w = w, a.bias = bias, a.lengths = lengths, a.dy = dy, a.dx1 = dx1, a.dx = dx, a.dx0 = dx0, a.ldx = ldx;
     a.part = sums ? static_cast<float *>(ws) : nullptr;
     a.B = B, a.N = N, a.E = E, a.W = W, a.silu = silu != 0;
-    const long parts = la::conv_plan_bwd(a, t);
+    const long parts = la::conv_plan_bwd(a);
     hipStream_t q = static_cast<hipStream_t>(stream);
     const int launched = hip_status(la::launch_conv_bwd(a, t, q));
     if (launched != LA_OK || !sums) return launched;

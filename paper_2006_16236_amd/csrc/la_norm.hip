@@ -3,8 +3,9 @@
 // Bound by memory: forward 2 tensors (4 with a residual and its sum), backward 3 (4).  A row lives in the
 // registers of the lanes that share it, so that each element is read once: mean, then the sum of squares around it
 // (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  16 or 32 lanes share a row
-// of as many 16-byte pieces, 64 one of up to 1024 elements (backward 2048, whose sums per column then need no barrier), 256 up to
-// 8192, 1024 (backward 512) up to 16384.
+// of as many 16-byte pieces, 64 one of up to 1024 elements, 256 (backward: 128 up to 2048) up to 8192, 1024 (backward 512) up to
+// 16384.  With a residual, bf16, 16384 x 4096: forward 91 us, backward 114, 5.9 and 4.7 TB/s of 4 tensors each, where a copy
+// of 256 MiB has 5.0; 16384 x 2048: 46 and 52 us.
 #include "la_layer.h"
 
 namespace la {
@@ -76,56 +77,56 @@ template <typename T, int TPR, int NV> __global__ __launch_bounds__(TPR > 256 ? 
         load_params<V>(a.beta == nullptr ? nullptr : a.beta + e, E - e, b[j]);
     }
     for (long first = (long)blockIdx.x * kRows; first < a.rows; first += (long)gridDim.x * kRows) {
-    const long row = first + threadIdx.x / TPR;
-    const bool live = row < a.rows;          // all lanes meet in row_sum
-    float f[NV][V];
-    float sum = 0.0f;
+        const long row = first + threadIdx.x / TPR;
+        const bool live = row < a.rows;          // all lanes meet in row_sum
+        float f[NV][V];
+        float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
-        const size_t at = (size_t)row * E + e;
-        Piece<T, V> p = load_piece<T, V>((const T *)a.x + at, valid);
-        if (a.r != nullptr) {
-            const Piece<T, V> q = load_piece<T, V>((const T *)a.r + at, valid);
-            float t[V];
+        for (int j = 0; j < NV; ++j) {
+            const int e = (j * TPR + l) * V, valid = live ? E - e : 0;
+            const size_t at = (size_t)row * E + e;
+            Piece<T, V> p = load_piece<T, V>((const T *)a.x + at, valid);
+            if (a.r != nullptr) {
+                const Piece<T, V> q = load_piece<T, V>((const T *)a.r + at, valid);
+                float t[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) t[i] = p.get(i) + q.get(i);
-            // the stored sum is what the backward (and the next layer) reads: it is what is normalised
-            p = pack_piece<T, V>(t);
-            if (a.s != nullptr) store_piece<T, V>((T *)a.s + at, valid, p);
+                for (int i = 0; i < V; ++i) t[i] = p.get(i) + q.get(i);
+                // the stored sum is what the backward (and the next layer) reads: it is what is normalised
+                p = pack_piece<T, V>(t);
+                if (a.s != nullptr) store_piece<T, V>((T *)a.s + at, valid, p);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum += f[j][i] = p.get(i);
+        }
+        const float mean = row_sum<TPR>(sum, red) / E;
+        float sq = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                f[j][i] -= mean;
+                if ((j * TPR + l) * V + i < E) sq = fmaf(f[j][i], f[j][i], sq);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, red) / E + a.eps);
+        if (l == 0 && live) {
+            if (a.mean != nullptr) a.mean[row] = mean;
+            if (a.rstd != nullptr) a.rstd[row] = rstd;
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum += f[j][i] = p.get(i);
-    }
-    const float mean = row_sum<TPR>(sum, red) / E;
-    float sq = 0.0f;
+        for (int j = 0; j < NV; ++j) {
+            const int e = (j * TPR + l) * V;
+            float o[V];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            f[j][i] -= mean;
-            if ((j * TPR + l) * V + i < E) sq = fmaf(f[j][i], f[j][i], sq);
+            for (int i = 0; i < V; ++i) o[i] = fmaf(f[j][i] * rstd, g[j][i], b[j][i]);
+            store_row<T, V>((T *)a.y + (size_t)row * E + e, live ? E - e : 0, o);
         }
-    }
-    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, red) / E + a.eps);
-    if (l == 0 && live) {
-        if (a.mean != nullptr) a.mean[row] = mean;
-        if (a.rstd != nullptr) a.rstd[row] = rstd;
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int e = (j * TPR + l) * V;
-        float o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = fmaf(f[j][i] * rstd, g[j][i], b[j][i]);
-        store_row<T, V>((T *)a.y + (size_t)row * E + e, live ? E - e : 0, o);
-    }
     }
 }
 
 // xhat = (s - mean) rstd, g = dy gamma, dx = rstd (g - mean(g) - xhat mean(g xhat)) + ds; a workgroup takes every
-// gridDim-th set of rows and keeps its part of dgamma = sum dy xhat, dbeta = sum dy in registers.  Up to 32 elements a lane
-// (bf16 rows of one wave: 64), so that most rows belong to one wave and the loop over rows has no barrier.
+// gridDim-th set of rows and keeps its part of dgamma = sum dy xhat, dbeta = sum dy in registers, which take as much room as
+// the row: 16 elements a lane up to 2048 (16384 x 2048 bf16: 52 us, 32 a lane 55, and 8 a lane 55).
 template <typename T, int TPR, int NV> __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const NormArgs a) {
     constexpr int V = 16 / sizeof(T), kRows = kBwdThreads / TPR, kHalf = kRows > 1 ? kRows / 2 : 1, kCols = NV * V;
     __shared__ float red[2 * kBwdThreads / kWave];
@@ -221,7 +222,7 @@ int lanes_of(int E, int dtype) {
 }
 int lanes_of_bwd(int E, int dtype) {
     const int pieces = dtype == 0 ? (E + 3) / 4 : (E + 7) / 8;
-    return pieces <= 16 ? 16 : pieces <= 32 ? 32 : E <= 2048 ? 64 : E <= 8192 ? 256 : 512;
+    return pieces <= 16 ? 16 : pieces <= 32 ? 32 : E <= 1024 ? 64 : E <= 2048 ? 128 : E <= 8192 ? 256 : 512;
 }
 
 }  // namespace
@@ -232,8 +233,8 @@ hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, 
     return hipGetLastError();
 }
 
-// Two workgroups a compute unit, or one where more than 16 elements a lane leave room for no more (16384 x 2048 bf16: 62 us
-// with 512 workgroups, 55 with 256; 16384 x 4096: 113 and 140).
+// Two workgroups a compute unit, or one where more than 16 elements a lane leave room for no more (16384 x 4096 bf16, 16 a
+// lane: 113 us with 512 workgroups, 140 with 256; with 32 a lane 62 and 55 at 16384 x 2048).
 int norm_groups(int rows, int E, int dtype) {
     const int tpr = lanes_of_bwd(E, dtype), per = kBwdThreads / tpr, most = E > 16 * tpr ? 256 : 512;
     const long sets = ((long)rows + per - 1) / per, turns = (sets + most - 1) / most;      // equal shares
@@ -302,8 +303,9 @@ hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
         } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(float, 64, 1);
             else if (nv == 2) LA_KERNEL(float, 64, 2);
-            else if (nv <= 4) LA_KERNEL(float, 64, 4);
-            else LA_KERNEL(float, 64, 8);
+            else LA_KERNEL(float, 64, 4);
+        } else if (tpr == 128) {
+            LA_KERNEL(float, 128, 4);
         } else if (tpr == 256) {
             if (nv <= 4) LA_KERNEL(float, 256, 4);
             else LA_KERNEL(float, 256, 8);
@@ -317,8 +319,9 @@ hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
             LA_KERNEL(bf16_t, 32, 1);
         } else if (tpr == 64) {
             if (nv <= 1) LA_KERNEL(bf16_t, 64, 1);
-            else if (nv == 2) LA_KERNEL(bf16_t, 64, 2);
-            else LA_KERNEL(bf16_t, 64, 4);
+            else LA_KERNEL(bf16_t, 64, 2);
+        } else if (tpr == 128) {
+            LA_KERNEL(bf16_t, 128, 2);
         } else if (tpr == 256) {
             if (nv == 2) LA_KERNEL(bf16_t, 256, 2);
             else LA_KERNEL(bf16_t, 256, 4);
