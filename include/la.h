@@ -4,7 +4,8 @@
  * Kernelised attention with the feature map phi(x) = elu(x) + 1 (paper eq. 7):
  * causal forward (eq. 9-12), its constant-memory backward (eq. 13-15,
  * Algorithm 1), the non-causal forward (eq. 4-6) and the recurrent decode step
- * (eq. 16-20).
+ * (eq. 16-20).  A section below adds what a residual layer runs around it and a
+ * second mixer: layer norm, selective scan and its short convolution.
  *
  * Conventions shared by every entry point
  *   Pointers   All tensor pointers are DEVICE pointers (HBM) valid on the

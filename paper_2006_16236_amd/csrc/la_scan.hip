@@ -6,13 +6,18 @@
 //   dd_t = x_t (g_t . B_t) + sum_n A g a h_{t-1},   dA = sum_t d_t g a h_{t-1},   dB_t = sum_e g_t d_t x_t,   dC_t = sum_e dv_t h_t.
 //
 // A decay per channel and state leaves no matrix product: the work is an exp2 and four vector instructions per
-// state and token (13 in the backward), and vector issue is the bound, not memory.  So:
+// state and token (12 in the backward, and 4 more to sum dB and dC over lanes), and vector issue is the bound, not memory:
+// with the functions, conversions and partial sums of a channel 9 and 25 slots of four cycles a state and token (an exp2
+// takes two), which at 8 x 2048 tokens of 2048 channels and 16 states is 119 and 339 us of all SIMDs at 2.4 GHz.  Measured (bf16,
+// gated): forward 188 us, the vector units active 65 % of the time, backward 490 us, 76 %; their tensors, 0.40 and
+// 0.67 GB with the kept states, take 81 and 135 us at a copy's rate.  So:
 // * A lane is a channel, a wave P = 2 (32 states: 4) states of 64 channels, S / P waves a workgroup.  B_t and C_t are then
 //   the same in all lanes of a wave: read from LDS at one address for all of them.
 // * What a token needs once per channel (softplus, d x, the gate, D x, conversions) is done by all waves together, a
 //   tile of 16 tokens at a time, and handed over through LDS; the waves' partial C . h come back the same way.
 // * Sequences too few to fill the machine are cut into pieces: the state each piece adds from zero, a scan over the
-//   pieces (a piece decays as exp(A sum d)), then the pass itself from the right states.
+//   pieces (a piece decays as exp(A sum d)), then the pass itself from the right states.  Twice the exponentials, but the
+//   whole machine: one sequence of 32768 x 1024 takes 122 + 6 + 160 us; uncut its 16 workgroups would need 3.0 ms (1.47 us a tile).
 #include <type_traits>
 
 #include "la_layer.h"
@@ -112,7 +117,8 @@ template <int P> __device__ __forceinline__ Pair<P> read_pair(const float (*at)[
 // kLocal: only what a piece adds to a state of zero, and its sum of d.
 // Two buffers in LDS and one barrier a tile: between two barriers a wave finishes tile i - 1 (C . h of all waves, gate,
 // store), prepares tile i + 1 and runs tile i, so that one wave's chains of functions hide behind another's states.
-// The elements come two tiles ahead.
+// The elements come two tiles ahead (fetched in branches, whose ends wait for all loads: 289 us instead of 188).  B and C by scalar loads, a broadcast
+// for free, cost 70 of 265 us in waits for the scalar cache; one state a wave (16 waves) 225 us: more partial sums.
 template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(64 * NW, 2) void scan_fwd_kernel(const ScanArgs a) {
     constexpr int K = T / NW;
     __shared__ __align__(16) float bc[2][T][NW * P][2];
@@ -359,7 +365,8 @@ template <int K, int CTRL> __device__ __forceinline__ void fold_row(float *v, bo
 // it and stay in registers (16 tokens x P states, and the decays), then the adjoint runs back over them.  dB and
 // dC are sums over channels, which are lanes: the 2 P products of a token are folded over the wave as they appear.
 // Between two barriers a wave prepares tile i - 1 and runs tile i; the second barrier only spans the reading of the
-// waves' partial sums, whose buffer does not fit twice.
+// waves' partial sums, whose buffer (98 of the 127 KB) does not fit twice.  Four waves of four states spill; reading the
+// partial sums while the next tile is prepared holds more registers, and took 559 us instead of 530 in the same run.
 template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(const ScanArgs a) {
     constexpr int K = T / NW;
     __shared__ __align__(16) float bc[2][T][NW * P][2];
@@ -583,7 +590,8 @@ template <typename TT> __global__ __launch_bounds__(256) void scan_sum_bc_kernel
 }
 
 // One token: a lane holds 4 states of a channel, S / 4 neighbouring lanes a channel.  Bound by the states, read and
-// written once.
+// written once (512 x 4096 x 16 fp32, 302 MB: 65 us a call, 4.6 TB/s; 49 again on the same states, a part of which the 256 MB
+// cache still holds), for few sequences by the launch (64 x 2048: 4 to 6 us).
 template <typename TT, int S> __global__ __launch_bounds__(256) void scan_step_kernel(const ScanArgs a, float *__restrict__ h) {
     constexpr int L = S / 4;
     const int wide = (a.E + 256 / L - 1) / (256 / L), b = blockIdx.x / wide;
