@@ -352,7 +352,32 @@ template <int K> __device__ __forceinline__ void fold16(float *v) {
         v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
 }
-// within 16 lanes; CTRL moves a lane's value to one that differs in the bit (row_ror 8, half mirror, quad permutations)
+// Twice four values over bits 3 and 2 of the lane, v[0 .. 3] to v[0] and v[4 .. 7] to v[1]: a lane gets value 2 bit2 + bit3 of the four,
+// summed over the four lanes.  An addition of a moved operand can leave the lanes of some groups of four as they are, and so
+// chooses between two values without an instruction of its own: 2 issue slots for each result, where a swap of half a wave
+// and the addition take 3, and two selections and a moved addition 3.  So these levels, with the most results, come first (the
+// swaps first: 543 us instead of 524 at 8 x 2048 x 2048, 16 states).  What a move reads, here and behind, has to be two slots old:
+// hence the order, and the pauses at both ends.  All lanes are active here.
+__device__ __forceinline__ void fold_quads(float *v) {
+    asm("s_nop 1\n\t"
+        "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %0, %4, %4 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %2, %2, %2 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %2, %6, %6 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %3, %3, %3 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %3, %7, %7 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %0, %0, %0 row_half_mirror row_mask:0xf bank_mask:0x5\n\t"
+        "v_add_f32_dpp %0, %1, %1 row_half_mirror row_mask:0xf bank_mask:0xa\n\t"
+        "v_add_f32_dpp %2, %2, %2 row_half_mirror row_mask:0xf bank_mask:0x5\n\t"
+        "v_add_f32_dpp %2, %3, %3 row_half_mirror row_mask:0xf bank_mask:0xa\n\t"
+        "s_nop 1"
+        : "+&v"(v[0]), "+&v"(v[2]), "+&v"(v[4]), "+&v"(v[6])
+        : "v"(v[1]), "v"(v[3]), "v"(v[5]), "v"(v[7]));
+    v[1] = v[4];
+}
+// within four lanes; CTRL moves a lane's value to one that differs in the bit (quad permutations)
 template <int K, int CTRL> __device__ __forceinline__ void fold_row(float *v, bool bit) {
 #pragma unroll
     for (int i = 0; i < K; ++i) {
@@ -448,12 +473,14 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
         prepare(buf ^ 1, max(i - 1, 0));
         constexpr int kHeld = P / 2;                              // registers a token's folded products take
         float acc[kHeld * T], sum[3][K], dA_tile[P] = {};         // (a sum of thousands of terms, in two levels)
+        float products[8];
 #pragma unroll
         for (int j = T - 1; j >= 0; --j) {
             const float2 v = in[buf][j / 2][lane][j % 2];
             const float dv = in_v[buf][j / 2][lane][j % 2];
             const Pair<P> p = read_pair<P>(&bc[buf][j][n0]);
-            float gB, gA, y, prod[2 * P];
+            float gB, gA, y;
+            float *prod = P == 2 && j % 2 ? products + 4 : products;
 #pragma unroll
             for (int n = 0; n < P; ++n) {
                 y = n == 0 ? p.C(n) * h[j + 1][n] : fmaf(p.C(n), h[j + 1][n], y);
@@ -471,24 +498,27 @@ template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) v
 #pragma unroll
                 for (int r = 0; r < 3; ++r) __builtin_memcpy(__builtin_assume_aligned(out[r][q][j / K][lane], 4 * K), sum[r], sizeof(sum[r]));
             }
-            fold32<P>(prod);
-            fold16<P / 2>(prod);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) acc[kHeld * j + r] = prod[r];
+            if constexpr (P == 4) {
+                fold_quads(prod);
+                acc[2 * j] = prod[0], acc[2 * j + 1] = prod[1];
+            } else if (j % 2 == 0) {                              // with the token before it in this order
+                fold_quads(prod);
+                acc[j] = prod[0], acc[j + 1] = prod[1];
+            }
         }
 #pragma unroll
         for (int n = 0; n < P; ++n) dA[n] += dA_tile[n];
-        // Lanes that differ in bits 5 and 4 now hold different products: value 4 r + 2 bit4 + bit5 of a token's 2 P.  The
-        // folds within 16 lanes choose between the two halves r (P = 4) by bit 3, and between tokens by the rest.
-        fold_row<P * T / 4, 0x128>(acc, lane & 8);
-        fold_row<P * T / 8, 0x141>(acc, lane & 4);
+        // Lanes that differ in bits 3 and 2 now hold different products: value 4 r + 2 bit2 + bit3 of a token's 2 P.  The
+        // other folds choose between the two r (P = 4) by bit 5, and between tokens by the rest.
+        fold32<P * T / 4>(acc);
+        fold16<P * T / 8>(acc);
         fold_row<P * T / 16, 0x4e>(acc, lane & 2);
         fold_row<P * T / 32, 0xb1>(acc, lane & 1);
 #pragma unroll
         for (int k = 0; k < P * T / 32; ++k) {
-            const int low = ((lane & 1) << 2) + (lane & 2) + ((lane & 4) >> 2);
-            const int j = P == 4 ? k * 8 + low : 2 * low + ((lane & 8) >> 3);
-            const int value = (P == 4 ? (lane & 8) >> 1 : 0) + ((lane & 16) >> 3) + ((lane & 32) >> 5);
+            const int bit5 = lane >> 5, low = ((lane & 16) >> 4) + (lane & 2) + ((lane & 1) << 2);
+            const int j = P == 4 ? k * 8 + low : bit5 + 2 * low;
+            const int value = (P == 4 ? 4 * bit5 : 0) + ((lane & 4) >> 1) + ((lane & 8) >> 3);
             if (i * T + j < tokens) pbc[(2 * j + value / P) * (NW * P) + value % P] = acc[k];
         }
         pbc -= T * 2 * NW * P;
