@@ -8,8 +8,8 @@
 // A decay per channel and state leaves no matrix product: the work is an exp2 and four vector instructions per
 // state and token (12 in the backward, and 4 more to sum dB and dC over lanes), and vector issue is the bound, not memory:
 // with the functions, conversions and partial sums of a channel 9 and 25 slots of four cycles a state and token (an exp2
-// takes two), which at 8 x 2048 tokens of 2048 channels and 16 states is 119 and 339 us of all SIMDs at 2.4 GHz.  Measured (bf16,
-// gated): forward 188 us, the vector units active 65 % of the time, backward 490 us, 76 %; their tensors, 0.40 and
+// takes two), which at 8 x 2048 tokens of 2048 channels and 16 states is 121 and 342 us of all SIMDs at 2.4 GHz.  Measured (bf16,
+// gated): forward 190 us, the vector units active 65 % of the time, backward 480 us, 77 %; their tensors, 0.40 and
 // 0.67 GB with the kept states, take 81 and 135 us at a copy's rate.  So:
 // * A lane is a channel, a wave P = 2 (32 states: 4) states of 64 channels, S / P waves a workgroup.  B_t and C_t are then
 //   the same in all lanes of a wave: read from LDS at one address for all of them.
@@ -117,7 +117,7 @@ template <int P> __device__ __forceinline__ Pair<P> read_pair(const float (*at)[
 // kLocal: only what a piece adds to a state of zero, and its sum of d.
 // Two buffers in LDS and one barrier a tile: between two barriers a wave finishes tile i - 1 (C . h of all waves, gate,
 // store), prepares tile i + 1 and runs tile i, so that one wave's chains of functions hide behind another's states.
-// The elements come two tiles ahead (fetched in branches, whose ends wait for all loads: 289 us instead of 188).  B and C by scalar loads, a broadcast
+// The elements come two tiles ahead (fetched in branches, whose ends wait for all loads: 289 us instead of 190).  B and C by scalar loads, a broadcast
 // for free, cost 70 of 265 us in waits for the scalar cache; one state a wave (16 waves) 225 us: more partial sums.
 template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(64 * NW, 2) void scan_fwd_kernel(const ScanArgs a) {
     constexpr int K = T / NW;
@@ -391,7 +391,8 @@ template <int K, int CTRL> __device__ __forceinline__ void fold_row(float *v, bo
 // dC are sums over channels, which are lanes: the 2 P products of a token are folded over the wave as they appear.
 // Between two barriers a wave prepares tile i - 1 and runs tile i; the second barrier only spans the reading of the
 // waves' partial sums, whose buffer (98 of the 127 KB) does not fit twice.  Four waves of four states spill; reading the
-// partial sums while the next tile is prepared holds more registers, and took 559 us instead of 530 in the same run.
+// partial sums, 10 % of the time, while the next tile is prepared holds more registers (559 us instead of 530 in the same run),
+// and the second barrier behind the next tile's states cuts what the compiler overlaps (561 instead of 525).
 template <typename TT, int NW, int P> __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(const ScanArgs a) {
     constexpr int K = T / NW;
     __shared__ __align__(16) float bc[2][T][NW * P][2];
