@@ -11,7 +11,7 @@
 // takes two), which at 8 x 2048 tokens of 2048 channels and 16 states is 121 and 342 us of all SIMDs at 2.4 GHz.  Measured (bf16,
 // gated): forward 190 us, the vector units active 65 % of the time, backward 480 us, 77 %; their tensors, 0.40 and
 // 0.67 GB with the kept states, take 81 and 135 us at a copy's rate.  So:
-// * A lane is a channel, a wave P = 2 (32 states: 4) states of 64 channels, S / P waves a workgroup.  B_t and C_t are then
+// * A lane is a channel, a wave P = 2 (or 4, 8) states of 64 channels, S / P waves a workgroup.  B_t and C_t are then
 //   the same in all lanes of a wave: read from LDS at one address for all of them.
 // * What a token needs once per channel (softplus, d x, the gate, D x, conversions) is done by all waves together, a
 //   tile of 16 tokens at a time, and handed over through LDS; the waves' partial C . h come back the same way.
@@ -71,6 +71,18 @@ template <typename TT, int K> struct Column {
 // P consecutive states from n0 on of a channel, in the layout of the kept states
 template <int P> __device__ __forceinline__ size_t state_at(const ScanArgs &a, int b, int slots, int slot, int n0, int e) {
     return ((((size_t)b * slots + slot) * (a.S / 4) + n0 / 4) * a.E + e) * 4 + n0 % 4;
+}
+
+// h of those states, from and to their place p: four side by side, the next four E quads on
+template <int P> __device__ __forceinline__ void load_states(float (&h)[P], const float *p, int E) {
+    constexpr int V = P < 4 ? P : 4;
+#pragma unroll
+    for (int n = 0; n < P; n += V) __builtin_memcpy(h + n, p + (size_t)n * E, V * sizeof(float));
+}
+template <int P> __device__ __forceinline__ void store_states(float *p, const float (&h)[P], int E) {
+    constexpr int V = P < 4 ? P : 4;
+#pragma unroll
+    for (int n = 0; n < P; n += V) __builtin_memcpy(p + (size_t)n * E, h + n, V * sizeof(float));
 }
 
 // B_t and C_t of a tile as fp32 pairs in LDS: a wave reads the 2 P values of a token at one address for all its lanes.
@@ -133,7 +145,7 @@ template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(
 #pragma unroll
     for (int n = 0; n < P; ++n) A[n] = a.A[(size_t)e * a.S + n0 + n] * kLog2e, h[n] = 0.0f;
     if constexpr (!kLocal) {
-        if (a.pieces > 1) __builtin_memcpy(h, a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), sizeof(h));
+        if (a.pieces > 1) load_states<P>(h, a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), a.E);
         else if (a.h0 != nullptr) __builtin_memcpy(h, a.h0 + ((size_t)w.b * a.E + e) * a.S + n0, sizeof(h));
     }
     const float bias = a.bias == nullptr ? 0.0f : a.bias[e], D = a.D == nullptr ? 0.0f : a.D[e];
@@ -171,7 +183,7 @@ template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(
     };
     auto step = [&](auto parity, int i) {
         constexpr int buf = decltype(parity)::value;
-        if (kept) __builtin_memcpy(pk, h, sizeof(h));
+        if (kept) store_states<P>(pk, h, a.E);
         pk += (size_t)a.E * (NW * P);
         fetch(buf, i + 2);                                        // this tile's elements are used up
         float y[T];
@@ -226,7 +238,7 @@ template <typename TT, int NW, int P, bool kLocal> __global__ __launch_bounds__(
     }
     if constexpr (kLocal) {
         if (live) {
-            __builtin_memcpy(a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), h, sizeof(h));
+            store_states<P>(a.piece_h + state_at<P>(a, w.b, a.pieces, w.piece, n0, e), h, a.E);
             if (q == 0) a.piece_d[((size_t)w.b * a.pieces + w.piece) * a.E + e] = sum_d;
         }
         return;
@@ -681,9 +693,10 @@ struct TileCost {
 };
 constexpr int kUnits = 256;
 // Sixteen states: eight waves of two states while a compute unit has one workgroup, else four waves of four (1.95 us
-// alone, but up to three fit: 3.6 us for the three, and 4.4 for three of the others, one after the other).
+// alone, but up to three fit: 3.6 us for the three, and 4.4 for three of the others, one after the other).  32 states: eight
+// waves of four (2.5 us), else four of eight (2.7 alone, 4.1 for the two that fit; of the others 4.9).
 TileCost fwd_cost(int S) {
-    return S == 8 ? TileCost{3, {1.53, 2.0, 2.6}, 0.6} : S == 16 ? TileCost{3, {1.47, 2.7, 3.6}, 0.9} : TileCost{1, {2.5}, 1.6};
+    return S == 8 ? TileCost{3, {1.53, 2.0, 2.6}, 0.6} : S == 16 ? TileCost{3, {1.47, 2.7, 3.6}, 0.9} : TileCost{2, {2.5, 4.1}, 1.6};
 }
 TileCost bwd_cost(int S) {
     return S == 8 ? TileCost{2, {3.3, 4.8}, 0.6} : S == 16 ? TileCost{1, {3.85}, 0.9} : TileCost{1, {6.5}, 1.75};
@@ -721,11 +734,8 @@ hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s) {
             scan_fwd_kernel<TT, NW, P, true><<<grid, 64 * NW, 0, s>>>(a);
             scan_pieces_kernel<false><<<4 * blocks_for((long)a.B * a.E * a.S), 64, 0, s>>>(a);
         }
-        if (a.S == 16 && workgroups > kUnits) {
-            scan_fwd_kernel<TT, 4, 4, false><<<grid, 256, 0, s>>>(a);
-            return hipGetLastError();
-        }
-        scan_fwd_kernel<TT, NW, P, false><<<grid, 64 * NW, 0, s>>>(a);
+        if (NW == 8 && workgroups > kUnits) scan_fwd_kernel<TT, 4, NW * P / 4, false><<<grid, 256, 0, s>>>(a);
+        else scan_fwd_kernel<TT, NW, P, false><<<grid, 64 * NW, 0, s>>>(a);
     });
     return hipGetLastError();
 }

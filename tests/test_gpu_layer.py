@@ -257,6 +257,23 @@ def test_scan(B, N, E, G, S, wider, lengths, state, gated, skip, softplus, dtype
         ref.check(n, host(o[n]), want[n], mag[n], "f32", 2 * k + B * N)
 
 
+# more workgroups than compute units, where a workgroup has fewer waves of more states: whole sequences, and pieces of them
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S", [8, 16, 32])
+@pytest.mark.parametrize("B,N,E,G,lengths", [(70, 35, 250, 1, None), (66, 18, 130, 2, [i % 19 for i in range(66)])])
+def test_scan_of_many_sequences(B, N, E, G, lengths, S, dtype):
+    test_scan(B, N, E, G, S, 0, lengths, True, True, True, True, dtype)
+
+
+@pytest.mark.parametrize("S", [16, 32])
+def test_scan_of_many_pieces(S):
+    B, N, E = 17, 500, 250
+    states, tiles = B * E * S * 4, (N + 15) // 16
+    pieces = (la.la_scan_fwd_workspace(B, N, E, 1, S, 0, 1) - 512) // (states + B * E * 4)
+    assert 4 * B * (pieces + 1) > 256 and pieces < tiles / 4       # four channel blocks a sequence
+    test_scan(B, N, E, 1, S, 0, [500, 0, 1, 499, 64, 65] + [450 + i for i in range(11)], True, True, True, True, "f32")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("case", [SCANS[3], SCANS[9], SCANS[11]])
 def test_scan_backward_with_and_without_the_forwards_states(case, dtype):
