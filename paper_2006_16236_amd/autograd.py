@@ -153,7 +153,7 @@ class _CausalConv(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, state, lengths, silu):
         ctx.set_materialize_grads(False)
-        x, w, bias, state = _rows(x), _dense(w), _dense(bias), _dense(state)
+        x, w, bias, state, lengths = _rows(x), _dense(w), _dense(bias), _dense(state), _dense(lengths)
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         x1 = torch.empty((x.shape[0], w.shape[1] - 1, x.shape[2]), dtype=x.dtype, device=x.device)
         _l.la_conv_fwd(x, w, bias, y, x0=state, x1=x1, lengths=lengths, silu=silu)
@@ -187,7 +187,7 @@ class _SelectiveScan(torch.autograd.Function):
     def forward(ctx, x, dt, A, Bt, Ct, D, z, dt_bias, state, lengths, softplus, keep):
         ctx.set_materialize_grads(False)
         x, dt, z, Bt, Ct = (_rows(t) for t in (x, dt, z, Bt, Ct))
-        A, D, dt_bias, state = (_dense(t) for t in (A, D, dt_bias, state))
+        A, D, dt_bias, state, lengths = (_dense(t) for t in (A, D, dt_bias, state, lengths))
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         h1 = torch.empty((x.shape[0], *A.shape), dtype=torch.float32, device=x.device)
         ws = _l.la_scan_fwd(x, dt, A, Bt, Ct, y, D=D, z=z, dt_bias=dt_bias, h0=state, h1=h1, lengths=lengths, softplus=softplus,
