@@ -15,6 +15,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <initializer_list>
+
 namespace {
 
 // addresses of the library's entry points, set once by bind()
@@ -282,11 +284,19 @@ struct Taker {
         return ws.data_ptr();
     }
 };
-template <typename F> int unlocked(F f) {
+// The call f, and what it wrote (None: not asked for) marked as changed in place: autograd then refuses a backward that has
+// saved one of these tensors, a state that has been stepped on meanwhile, as after torch's own operations.
+template <typename F> int unlocked(std::initializer_list<PyObject *> written, F f) {
     int st;
     Py_BEGIN_ALLOW_THREADS
     st = f();
     Py_END_ALLOW_THREADS
+    if (st != 0) return st;
+    for (PyObject *o : written) {
+        if (o == Py_None) continue;
+        c10::TensorImpl *t = THPVariable_Unpack(o).unsafeGetTensorImpl();
+        if (!t->is_inference()) t->bump_version();
+    }
     return st;
 }
 
@@ -308,7 +318,7 @@ PyObject *py_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const void *r = k.mine(a[6], all, true), *px = x->data_ptr();
         if (!k.ok) return not_taken();
         void *q = stream();
-        return PyLong_FromLong(unlocked([&] { return g_layer.norm_fwd(px, r, gamma, beta, y, s, mean, rstd, (int)rows, (int)E, (float)eps, k.code, q); }));
+        return PyLong_FromLong(unlocked({a[3], a[4], a[5], a[7]}, [&] { return g_layer.norm_fwd(px, r, gamma, beta, y, s, mean, rstd, (int)rows, (int)E, (float)eps, k.code, q); }));
     } catch (...) {
         return not_taken();
     }
@@ -333,7 +343,7 @@ PyObject *py_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         size_t bytes = 0;
         void *w = k.workspace(a[9], g_layer.norm_bwd_ws((int)rows, (int)E, k.code), ws, bytes), *q = stream();
         if (!k.ok) return not_taken();
-        return answer(unlocked([&] { return g_layer.norm_bwd(px, gamma, mean, rstd, dy, ds, dx, dg, db, (int)rows, (int)E, k.code, w, bytes, q); }), a[9], ws);
+        return answer(unlocked({a[5], a[6], a[7]}, [&] { return g_layer.norm_bwd(px, gamma, mean, rstd, dy, ds, dx, dg, db, (int)rows, (int)E, k.code, w, bytes, q); }), a[9], ws);
     } catch (...) {
         return not_taken();
     }
@@ -365,7 +375,7 @@ PyObject *py_conv_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int silu = k.flag(a[7]);
         if (!k.ok) return not_taken();
         void *q = stream();
-        return PyLong_FromLong(unlocked([&] { return g_layer.conv_fwd(px, ld, w, bias, x0, len, y, x1, (int)B, (int)N, (int)E, (int)W, silu, k.code, q); }));
+        return PyLong_FromLong(unlocked({a[3], a[5]}, [&] { return g_layer.conv_fwd(px, ld, w, bias, x0, len, y, x1, (int)B, (int)N, (int)E, (int)W, silu, k.code, q); }));
     } catch (...) {
         return not_taken();
     }
@@ -394,7 +404,7 @@ PyObject *py_conv_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         size_t bytes = 0;
         void *s = k.workspace(a[12], g_layer.conv_bwd_ws((int)B, (int)N, (int)E, (int)W, k.code), ws, bytes), *q = stream();
         if (!k.ok) return not_taken();
-        return answer(unlocked([&] { return g_layer.conv_bwd(px, ld, w, bias, x0, len, dy, dx1, dx, dw, db, dx0, (int)B, (int)N, (int)E, (int)W, silu,
+        return answer(unlocked({a[4], a[5], a[6], a[9]}, [&] { return g_layer.conv_bwd(px, ld, w, bias, x0, len, dy, dx1, dx, dw, db, dx0, (int)B, (int)N, (int)E, (int)W, silu,
                                                              k.code, s, bytes, q); }), a[12], ws);
     } catch (...) {
         return not_taken();
@@ -416,7 +426,7 @@ PyObject *py_conv_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int silu = k.flag(a[5]);
         if (!k.ok) return not_taken();
         void *q = stream();
-        return PyLong_FromLong(unlocked([&] { return g_layer.conv_step(px, w, bias, state, y, (int)B, (int)E, (int)W, silu, k.code, q); }));
+        return PyLong_FromLong(unlocked({a[3], a[4]}, [&] { return g_layer.conv_step(px, w, bias, state, y, (int)B, (int)E, (int)W, silu, k.code, q); }));
     } catch (...) {
         return not_taken();
     }
@@ -457,7 +467,7 @@ PyObject *py_scan_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         void *w = k.workspace(a[14], k.ok ? g_layer.scan_fwd_ws((int)i.B, (int)i.N, (int)i.E, (int)i.G, (int)i.S, k.code, flags) : 0, ws, bytes);
         if (!k.ok) return not_taken();
         void *q = stream();
-        return answer(unlocked([&] { return g_layer.scan_fwd(i.x, i.ld[0], i.dt, i.ld[1], i.z, i.ld[2], i.Bt, i.ld[3], i.Ct, i.ld[4], i.A, i.D, i.bias,
+        return answer(unlocked({a[5], a[10]}, [&] { return g_layer.scan_fwd(i.x, i.ld[0], i.dt, i.ld[1], i.z, i.ld[2], i.Bt, i.ld[3], i.Ct, i.ld[4], i.A, i.D, i.bias,
                                                              i.h0, i.len, y, h1, (int)i.B, (int)i.N, (int)i.E, (int)i.G, (int)i.S, flags, k.code, w,
                                                              bytes, q); }), a[14], ws);
     } catch (...) {
@@ -488,7 +498,7 @@ PyObject *py_scan_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!k.ok) return not_taken();
         const void *fp = fws->data_ptr();
         void *q = stream();
-        return answer(unlocked([&] { return g_layer.scan_bwd(i.x, i.ld[0], i.dt, i.ld[1], i.z, i.ld[2], i.Bt, i.ld[3], i.Ct, i.ld[4], i.A, i.D, i.bias,
+        return answer(unlocked({a[6], a[7], a[8], a[9], a[10], a[14], a[15], a[16], a[19]}, [&] { return g_layer.scan_bwd(i.x, i.ld[0], i.dt, i.ld[1], i.z, i.ld[2], i.Bt, i.ld[3], i.Ct, i.ld[4], i.A, i.D, i.bias,
                                                              i.h0, i.len, fp, dy, dh1, dx, ddt, dz, dB, dC, dA, dD, dbias, dh0, (int)i.B, (int)i.N,
                                                              (int)i.E, (int)i.G, (int)i.S, flags, k.code, w, bytes, q); }), a[23], ws);
     } catch (...) {
@@ -512,7 +522,7 @@ PyObject *py_scan_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int flags = k.flag(a[10]);
         if (!k.ok) return not_taken();
         void *q = stream();
-        return PyLong_FromLong(unlocked([&] { return g_layer.scan_step(px, dt, z, Bt, Ct, A, D, bias, h, y, (int)B, (int)E, (int)G, (int)S, flags, k.code, q); }));
+        return PyLong_FromLong(unlocked({a[5], a[6]}, [&] { return g_layer.scan_step(px, dt, z, Bt, Ct, A, D, bias, h, y, (int)B, (int)E, (int)G, (int)S, flags, k.code, q); }));
     } catch (...) {
         return not_taken();
     }

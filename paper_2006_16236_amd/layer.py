@@ -3,7 +3,8 @@ convolution and the selective state space scan of include/la.h.
 
 As in binding.py this is argument checking and marshalling only.  Inputs called rows [B, N, E] may be parts of a
 wider tensor (the half of a projection's output): their last dimension dense, their tokens at one distance.
-Everything else is dense.  A call runs on its tensors' device, on `stream` or that device's current stream.
+Everything else is dense.  A call runs on its tensors' device, on `stream` or that device's current stream.  What it
+writes counts as changed in place: a backward that has saved such a tensor (a state that has been stepped on) is refused.
 
 Each function first offers the call to its native counterpart (csrc/la_call.cpp), which takes it where all is as
 expected and the tensors are on the current device; otherwise it goes through the checks here, which name what is wrong.
@@ -68,8 +69,9 @@ def _rows(name, t, shape, dtype, device, optional=False):
     return _ints(f"{name}: the distance between tokens", ld)[0]
 
 
-def _run(where, device, stream, call):
-    """call(stream handle) with `device` current: launches go to the current device, whose stream it must be."""
+def _run(where, device, stream, call, written):
+    """call(stream handle) with `device` current: launches go to the current device, whose stream it must be.
+    written: the tensors it writes (None: not asked for)."""
     if device.type != "cuda":
         raise ValueError("tensors must be contiguous device tensors")
     if stream is None:
@@ -80,6 +82,7 @@ def _run(where, device, stream, call):
     else:
         with torch.cuda.device(device):
             _check(call(handle), where)
+    torch.autograd.graph.increment_version([t for t in written if t is not None])
 
 
 def _p(t):
@@ -133,7 +136,7 @@ def la_norm_fwd(x, gamma, beta, y, mean=None, rstd=None, r=None, s=None, eps=1e-
         raise ValueError(f"x: shape {tuple(shape)} is empty")
     _run("la_norm_fwd", dev, stream,
          lambda q: _lib.la_norm_fwd(_p(x), _p(r), _p(gamma), _p(beta), _p(y), _p(s), _p(mean), _p(rstd), lead.numel(), E,
-                                    float(eps), t, q))
+                                    float(eps), t, q), (y, mean, rstd, s))
 
 
 def la_norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ds=None, ws=None, stream=None):
@@ -163,7 +166,7 @@ def la_norm_bwd(s, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, ds=None, 
         ws = _workspace(ws, la_norm_bwd_workspace(rows, E, t), dev, stream)
     _run("la_norm_bwd", dev, stream,
          lambda q: _lib.la_norm_bwd(_p(s), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(ds), _p(dx), _p(dgamma), _p(dbeta),
-                                    rows, E, t, _p(ws), 0 if ws is None else _size(ws), q))
+                                    rows, E, t, _p(ws), 0 if ws is None else _size(ws), q), (dx, dgamma, dbeta))
     return ws
 
 
@@ -197,7 +200,7 @@ def la_conv_fwd(x, w, bias, y, x0=None, x1=None, lengths=None, silu=True, stream
     _like("x1", x1, (B, W - 1, E), dt, dev, optional=True)
     _like("lengths", lengths, (B,), torch.int32, dev, optional=True)
     _run("la_conv_fwd", dev, stream,
-         lambda q: _lib.la_conv_fwd(_p(x), ldx, _p(w), _p(bias), _p(x0), _p(lengths), _p(y), _p(x1), B, N, E, W, int(silu), t, q))
+         lambda q: _lib.la_conv_fwd(_p(x), ldx, _p(w), _p(bias), _p(x0), _p(lengths), _p(y), _p(x1), B, N, E, W, int(silu), t, q), (y, x1))
 
 
 def la_conv_bwd(x, w, bias, dy, dx, dw=None, db=None, x0=None, dx1=None, dx0=None, lengths=None, silu=True, ws=None,
@@ -222,7 +225,7 @@ def la_conv_bwd(x, w, bias, dy, dx, dw=None, db=None, x0=None, dx1=None, dx0=Non
         ws = _workspace(ws, la_conv_bwd_workspace(B, N, E, W, t), dev, stream)
     _run("la_conv_bwd", dev, stream,
          lambda q: _lib.la_conv_bwd(_p(x), ldx, _p(w), _p(bias), _p(x0), _p(lengths), _p(dy), _p(dx1), _p(dx), _p(dw), _p(db),
-                                    _p(dx0), B, N, E, W, int(silu), t, _p(ws), 0 if ws is None else _size(ws), q))
+                                    _p(dx0), B, N, E, W, int(silu), t, _p(ws), 0 if ws is None else _size(ws), q), (dx, dw, db, dx0))
     return ws
 
 
@@ -236,7 +239,7 @@ def la_conv_step(x, w, bias, state, y, silu=True, stream=None):
     _like("y", y, (B, E), dt, dev)
     _like("state", state, (B, W - 1, E), dt, dev)
     _run("la_conv_step", dev, stream,
-         lambda q: _lib.la_conv_step(_p(x), _p(w), _p(bias), _p(state), _p(y), B, E, W, int(silu), t, q))
+         lambda q: _lib.la_conv_step(_p(x), _p(w), _p(bias), _p(state), _p(y), B, E, W, int(silu), t, q), (state, y))
 
 
 # ---- selective scan ------------------------------------------------------------------------------
@@ -298,7 +301,7 @@ def la_scan_fwd(x, dt, A, Bt, Ct, y, D=None, z=None, dt_bias=None, h0=None, h1=N
     ws = _workspace(ws, la_scan_fwd_workspace(*k.dims, k.t, flags), k.dev, stream)
     _run("la_scan_fwd", k.dev, stream,
          lambda q: _lib.la_scan_fwd(*k.inputs(x, dt, z, Bt, Ct), _p(A), _p(D), _p(dt_bias), _p(h0), _p(lengths), _p(y), _p(h1),
-                                    *k.dims, flags, k.t, _p(ws), _size(ws), q))
+                                    *k.dims, flags, k.t, _p(ws), _size(ws), q), (y, h1))
     return ws
 
 
@@ -336,7 +339,7 @@ def la_scan_bwd(x, dt, A, Bt, Ct, dy, dx, ddt, dA, dB, dC, D=None, z=None, dt_bi
     _run("la_scan_bwd", k.dev, stream,
          lambda q: _lib.la_scan_bwd(*k.inputs(x, dt, z, Bt, Ct), _p(A), _p(D), _p(dt_bias), _p(h0), _p(lengths), _p(fwd_ws),
                                     _p(dy), _p(dh1), _p(dx), _p(ddt), _p(dz), _p(dB), _p(dC), _p(dA), _p(dD), _p(ddt_bias),
-                                    _p(dh0), *k.dims, flags, k.t, _p(ws), _size(ws), q))
+                                    _p(dh0), *k.dims, flags, k.t, _p(ws), _size(ws), q), (dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dh0))
     return ws
 
 
@@ -363,4 +366,4 @@ def la_scan_step(x, dt, A, Bt, Ct, h, y, D=None, z=None, dt_bias=None, softplus=
     _like("dt_bias", dt_bias, (E,), _F32, dev, optional=True)
     _run("la_scan_step", dev, stream,
          lambda q: _lib.la_scan_step(_p(x), _p(dt), _p(z), _p(Bt), _p(Ct), _p(A), _p(D), _p(dt_bias), _p(h), _p(y), B, E, G, S,
-                                     LA_SCAN_SOFTPLUS if softplus else 0, t, q))
+                                     LA_SCAN_SOFTPLUS if softplus else 0, t, q), (h, y))
