@@ -274,7 +274,10 @@ template <bool kReverse> __global__ __launch_bounds__(64) void scan_pieces_kerne
                 if (i0 + i >= a.pieces) break;
                 const int k = kReverse ? a.pieces - 1 - (i0 + i) : i0 + i;
                 a.piece_h[state_at<1>(a, b, a.pieces, k, n, e)] = h;
-                h = fmaf(__builtin_amdgcn_exp2f(A * d[i]), h, add[i]);
+                // A piece's decay can leave fp32's range where the state behind it does not (growth from a state of zero, which would
+                // be inf * 0; a large state that vanishes): so it enters in two factors, of which the second is 1 in between.
+                const float power = A * d[i], first = fminf(fmaxf(power, -126.0f), 126.0f), rest = fminf(fmaxf(power - first, -126.0f), 126.0f);
+                h = fmaf(__builtin_amdgcn_exp2f(first), __builtin_amdgcn_exp2f(rest) * h, add[i]);
             }
         }
     }

@@ -1,0 +1,49 @@
+"""The scan of sequences that are cut into pieces, whose states are formed side by side and then carried from piece to piece."""
+import numpy as np
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2006_16236_amd as la
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+def pieces_of(B, N, E, G, S):
+    """Pieces of the forward and of the backward, as their workspaces show them: a state and a sum of steps for each piece
+    (rounded up to 256 bytes each); backward also the kept states, channel blocks' dB and dC, and sums for each piece."""
+    up = lambda n: -(-n // 256) * 256
+    room = lambda p: 0 if p < 2 else up(B * E * S * 4 * p) + up(B * p * E * 4)
+    tiles, blocks = -(-N // 16), G * -(-(E // G) // 64)
+    fwd, bwd = la.la_scan_fwd_workspace(B, N, E, G, S, 0, 1), la.la_scan_bwd_workspace(B, N, E, G, S, 0, 3)
+    found = [p for p in range(1, tiles + 1) if room(p) == fwd]
+    back = [p for p in range(1, tiles + 1) if room(p) + up(blocks * B * N * 2 * S * 4) + up(B * p * E * (S + 2) * 4) == bwd]
+    assert len(found) == len(back) == 1
+    return found[0], back[0]
+
+
+def test_decays_of_a_piece_beyond_the_range_of_fp32():
+    """exp(A sum d) over a piece: infinite before a state (backwards: a gradient) that is still zero, zero behind a state
+    that is large enough to survive it.  Steps given as they are, so A is what a state grows or falls by at each token."""
+    B, N, E, S, some = 1, 512, 64, 8, 20
+    assert min(pieces_of(B, N, E, 1, S)) > 2
+    r = np.random.default_rng(11)
+    a = {n: r.standard_normal((B, N, E)).astype(np.float32) for n in ("x", "dy")}
+    a.update({n: r.standard_normal((B, N, 1, S)).astype(np.float32) for n in ("Bt", "Ct")}, dt=np.ones((B, N, E), np.float32))
+    a["A"] = np.tile(np.array([2, -2, -1.5, 0.01, 1.5, -0.01, 0, -1], np.float32), (E, 1))
+    a["x"][:, :N - some] = 0                                       # growth by exp(2 * 20) of what enters near the end,
+    a["dy"][:, some:] = 0                                          # and of the gradient that enters near the start
+    a["dy"] *= 0.1
+    a["h0"] = np.zeros((B, E, S), np.float32)
+    a["h0"][:, :, 2] = 1e34                                        # exp(-1.5 * 64) 1e34 is 2e-8
+    t = {n: torch.from_numpy(v).to(DEV) for n, v in a.items()}
+    o = {n: torch.empty_like(t[m]) for n, m in (("y", "x"), ("dx", "x"), ("ddt", "x"), ("dA", "A"), ("dB", "Bt"), ("dC", "Ct"), ("h1", "h0"), ("dh0", "h0"))}
+    args = (t["x"], t["dt"], t["A"], t["Bt"], t["Ct"])
+    ws = la.la_scan_fwd(*args, o["y"], h0=t["h0"], h1=o["h1"], softplus=False, keep=True)
+    la.la_scan_bwd(*args, t["dy"], o["dx"], o["ddt"], o["dA"], o["dB"], o["dC"], h0=t["h0"], dh0=o["dh0"], softplus=False, fwd_ws=ws)
+    want, mag = (ref.scan(**a, softplus=False, mag=m) for m in (False, True))
+    # |A| <= 2 and steps of 1: the exponent of a piece is off by its sum's roundings too, at most one for each of its tokens
+    k = ref.roundings(N, S, a["A"], 1.0) + 2 * N
+    for n in o:
+        ref.check(n, o[n].double().cpu().numpy(), want[n], mag[n] + 1e-30, "f32", 2 * k + E)
