@@ -47,3 +47,39 @@ def test_decays_of_a_piece_beyond_the_range_of_fp32():
     k = ref.roundings(N, S, a["A"], 1.0) + 2 * N
     for n in o:
         ref.check(n, o[n].double().cpu().numpy(), want[n], mag[n] + 1e-30, "f32", 2 * k + E)
+
+
+# Against bounds that follow the recurrence (scan_bounds.py).  B, N, E, G, S, lengths, softplus, dtype, slow: how much slower than
+# 1 to S the states fall.  Whole sequences and pieces of them, both widths of a workgroup forwards.
+BOUNDED = [
+    (1, 1, 3, 1, 8, None, True, "f32", 1), (2, 16, 63, 1, 16, [16, 3], True, "f32", 1), (3, 17, 130, 2, 8, [0, 17, 16], True, "bf16", 1),
+    (1, 33, 96, 4, 16, None, False, "f32", 1), (1, 200, 64, 1, 32, None, True, "f32", 4), (2, 300, 72, 2, 16, [300, 77], True, "bf16", 4),
+    (70, 35, 250, 1, 16, None, True, "f32", 1), (66, 18, 130, 2, 32, [i % 19 for i in range(66)], True, "f32", 1),
+    (66, 18, 130, 2, 16, [i % 19 for i in range(66)], True, "bf16", 1), (70, 35, 250, 1, 32, None, True, "bf16", 1),
+    (17, 500, 250, 1, 16, [500, 0, 1, 499, 64, 65] + [450 + i for i in range(11)], True, "bf16", 4),
+    (17, 500, 250, 1, 32, [500, 0, 1, 499, 64, 65] + [450 + i for i in range(11)], True, "f32", 4),
+]
+
+
+def case_id(case):
+    return "-".join(map(str, case[:5])) + f"-{case[7]}"
+
+
+def bounded_data(case):
+    from test_gpu_layer import scan_data
+    B, N, E, G, S, lengths, softplus, dtype, slow = case
+    _, a = scan_data(B, N, E, G, S, lengths, True, True, True, softplus, dtype)
+    a["A"] = (a["A"] / slow).astype(np.float32)
+    return a
+
+
+@pytest.mark.parametrize("case", BOUNDED, ids=case_id)
+def test_scan_within_the_bounds_of_its_recurrence(case):
+    import scan_bounds
+    from test_gpu_layer import Data, scan_on_device
+    softplus, dtype = case[6:8]
+    a = bounded_data(case)
+    o, _ = scan_on_device(Data(0, dtype), a, 0, softplus)
+    for name, (want, bound) in scan_bounds.scan(**a, softplus=softplus, pieces=pieces_of(*case[:5])).items():
+        kind = dtype if name in ("y", "dx", "ddt", "dz", "dB", "dC") else "f32"
+        ref.check(name, o[name].double().cpu().numpy(), want, bound, kind, 1)
