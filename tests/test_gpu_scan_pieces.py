@@ -50,7 +50,8 @@ def test_decays_of_a_piece_beyond_the_range_of_fp32():
 
 
 # Against bounds that follow the recurrence (scan_bounds.py).  B, N, E, G, S, lengths, softplus, dtype, slow: how much slower than
-# 1 to S the states fall.  Whole sequences and pieces of them, both widths of a workgroup forwards.
+# 1 to S the states fall.  The pieces' states are carried from piece to piece 16 at a time: exactly one batch, one piece more,
+# two, and three with one that is not full; lengths that end in different batches; both widths of a workgroup forwards.
 BOUNDED = [
     (1, 1, 3, 1, 8, None, True, "f32", 1), (2, 16, 63, 1, 16, [16, 3], True, "f32", 1), (3, 17, 130, 2, 8, [0, 17, 16], True, "bf16", 1),
     (1, 33, 96, 4, 16, None, False, "f32", 1), (1, 200, 64, 1, 32, None, True, "f32", 4), (2, 300, 72, 2, 16, [300, 77], True, "bf16", 4),
@@ -58,6 +59,8 @@ BOUNDED = [
     (66, 18, 130, 2, 16, [i % 19 for i in range(66)], True, "bf16", 1), (70, 35, 250, 1, 32, None, True, "bf16", 1),
     (17, 500, 250, 1, 16, [500, 0, 1, 499, 64, 65] + [450 + i for i in range(11)], True, "bf16", 4),
     (17, 500, 250, 1, 32, [500, 0, 1, 499, 64, 65] + [450 + i for i in range(11)], True, "f32", 4),
+    (1, 1024, 40, 1, 8, None, True, "f32", 16), (1, 1300, 64, 1, 16, [1281], True, "f32", 16), (2, 2500, 24, 2, 8, [2500, 1100], True, "f32", 16),
+    (1, 3001, 40, 1, 8, None, False, "f32", 16), (1, 3001, 20, 1, 32, None, True, "f32", 16), (3, 3001, 20, 1, 16, [3001, 1, 1800], True, "bf16", 16),
 ]
 
 
@@ -71,6 +74,12 @@ def bounded_data(case):
     _, a = scan_data(B, N, E, G, S, lengths, True, True, True, softplus, dtype)
     a["A"] = (a["A"] / slow).astype(np.float32)
     return a
+
+
+def test_the_bounded_scans_have_one_batch_of_pieces_and_more():
+    pieces = {(c[1], c[4]): pieces_of(*c[:5]) for c in BOUNDED if c[1] > 1000}
+    assert pieces[1024, 8] == (16, 16) and pieces[1300, 16] == (17, 17) and pieces[2500, 8] == (32, 32)
+    assert all(min(pieces[3001, S]) > 32 and all(p % 16 for p in pieces[3001, S]) for S in (8, 16, 32))
 
 
 @pytest.mark.parametrize("case", BOUNDED, ids=case_id)
