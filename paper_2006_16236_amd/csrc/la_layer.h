@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "la_device.h"
+#include "la_scan_cut.h"
 
 namespace la {
 
@@ -149,8 +150,6 @@ hipError_t launch_conv_bwd(const ConvArgs &a, int dtype, hipStream_t s);
 hipError_t launch_conv_step(const void *x, const float *w, const float *bias, void *state, void *y, int B, int E, int W,
                             bool silu, int dtype, hipStream_t s);
 
-// The scan's tokens go in tiles of kScanTile; the states before each tile are what a backward starts from.
-constexpr int kScanTile = 16, kScanLanes = 64;                    // tokens of a tile, channels of a workgroup
 struct ScanArgs {
     const void *x, *dt, *z, *Bt, *Ct, *dy;
     const float *A, *D, *bias, *h0, *dh1;
@@ -167,9 +166,11 @@ struct ScanArgs {
     int B, N, E, G, S, tiles, pieces, piece_tiles;
     bool softplus;
 };
-// channel blocks of all groups; pieces that a pass cuts a sequence into (piece_tiles tiles each)
-int scan_blocks(int E, int G);
-void scan_cut(ScanArgs &a, bool backward);
+// pieces that a pass cuts a sequence into (piece_tiles tiles each), from the call's sizes
+inline void scan_cut(ScanArgs &a, bool backward) {
+    const ScanCut c = scan_cut_of(a.B, a.N, a.E, a.G, a.S, backward);
+    a.tiles = c.tiles, a.pieces = c.pieces, a.piece_tiles = c.piece_tiles;
+}
 // the states before each piece (pieces > 1), then outputs, kept states and the final state; y NULL: kept states only
 hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s);
 hipError_t launch_scan_bwd(const ScanArgs &a, int dtype, hipStream_t s);

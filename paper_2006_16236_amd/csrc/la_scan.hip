@@ -687,47 +687,7 @@ template <typename TT, int S> __global__ __launch_bounds__(256) void scan_step_k
 
 unsigned blocks_for(long n) { return (unsigned)((n + 255) / 256 < (1 << 20) ? (n + 255) / 256 : 1 << 20); }
 
-// ---- cutting sequences into pieces ------------------------------------------------------------------
-// Microseconds a tile of 16 tokens takes while every compute unit has 1, 2, .. `most` workgroups (its LDS holds no more),
-// and what each 256 workgroups of the kernel that only forms the pieces' states add; measured with 2048 channels, bf16.
-struct TileCost {
-    int most;
-    double us[3], local;
-};
-constexpr int kUnits = 256;
-// Sixteen states: eight waves of two states while a compute unit has one workgroup, else four waves of four (1.95 us
-// alone, but up to three fit: 3.6 us for the three, and 4.4 for three of the others, one after the other).  32 states: eight
-// waves of four (2.5 us), else four of eight (2.7 alone, 4.1 for the two that fit; of the others 4.9).
-TileCost fwd_cost(int S) {
-    return S == 8 ? TileCost{3, {1.53, 2.0, 2.6}, 0.6} : S == 16 ? TileCost{3, {1.47, 2.7, 3.6}, 0.9} : TileCost{2, {2.5, 4.1}, 1.6};
-}
-TileCost bwd_cost(int S) {
-    return S == 8 ? TileCost{2, {3.3, 4.8}, 0.6} : S == 16 ? TileCost{1, {3.85}, 0.9} : TileCost{1, {6.5}, 1.75};
-}
-double tile_us(const TileCost &c, long workgroups) {
-    const long full = workgroups / (kUnits * c.most), rest = workgroups % (kUnits * c.most);
-    return full * c.us[c.most - 1] + (rest > 0 ? c.us[(rest - 1) / kUnits] : 0.0);
-}
-
 }  // namespace
-
-int scan_blocks(int E, int G) { return G * ((E / G + kLanes - 1) / kLanes); }
-
-// The number of pieces with the least time: all of a sequence's tiles one after the other, or pieces of at least 4 tiles side by
-// side after the kernel that forms their states (one piece fewer), a scan over the pieces and two more launches.
-void scan_cut(ScanArgs &a, bool backward) {
-    a.tiles = (a.N + T - 1) / T;
-    const long whole = (long)a.B * scan_blocks(a.E, a.G);
-    const TileCost c = backward ? bwd_cost(a.S) : fwd_cost(a.S);
-    double best = tile_us(c, whole) * a.tiles;
-    a.pieces = 1, a.piece_tiles = a.tiles;
-    for (int pieces = 2; pieces <= a.tiles / 4 && whole * pieces <= kUnits * c.most + whole; ++pieces) {
-        const int tiles = (a.tiles + pieces - 1) / pieces;
-        if ((a.tiles + tiles - 1) / tiles != pieces) continue;
-        const double us = tiles * (tile_us(c, whole * pieces) + c.local * ((whole * (pieces - 1) + kUnits - 1) / kUnits)) + 10.0 + 0.25 * pieces;
-        if (us < best) best = us, a.pieces = pieces, a.piece_tiles = tiles;
-    }
-}
 
 hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s) {
     const long workgroups = (long)a.B * a.pieces * scan_blocks(a.E, a.G);
@@ -737,7 +697,7 @@ hipError_t launch_scan_fwd(const ScanArgs &a, int dtype, hipStream_t s) {
             scan_fwd_kernel<TT, NW, P, true><<<grid, 64 * NW, 0, s>>>(a);
             scan_pieces_kernel<false><<<4 * blocks_for((long)a.B * a.E * a.S), 64, 0, s>>>(a);
         }
-        if (NW == 8 && workgroups > kUnits) scan_fwd_kernel<TT, 4, NW * P / 4, false><<<grid, 256, 0, s>>>(a);
+        if (NW == 8 && workgroups > scan_cost::kUnits) scan_fwd_kernel<TT, 4, NW * P / 4, false><<<grid, 256, 0, s>>>(a);
         else scan_fwd_kernel<TT, NW, P, false><<<grid, 64 * NW, 0, s>>>(a);
     });
     return hipGetLastError();
