@@ -13,40 +13,35 @@ namespace {
 
 constexpr int kSumSlices = 16;
 constexpr int kBwdThreads = 512;
-// Workgroups of a launch; more rows (of the sums: columns) go round again.  A workgroup of 1024 lanes that keeps its weights for several rows is 6 %
-// faster than one a row, one of 256 is 5 % slower.
+// Workgroups of a launch; more rows go round again (more columns of the sums in another launch).  A workgroup of 1024 lanes that keeps
+// its weights for several rows is 6 % faster than one a row, one of 256 is 5 % slower.
 constexpr long kMaxGrid = 1 << 20, kWideGrid = 2048;
 
-__global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ part, long rows, const SumTargets out) {
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ part, long rows, const SumTargets out, long first) {
     __shared__ float red[kSumSlices][kWave];
     const int lane = threadIdx.x % kWave, slice = threadIdx.x / kWave;
-    const long cols = out.n[0] + out.n[1] + out.n[2];
-    for (long first = (long)blockIdx.x * kWave; first < cols; first += (long)gridDim.x * kWave) {
-        const long c = first + lane;
-        float v = 0.0f;
-        if (c < cols) {
-            long r = slice;
-            for (; r + 3 * kSumSlices < rows; r += 4 * kSumSlices) {    // four loads on their way at a time
-                float t[4];
+    const long cols = out.n[0] + out.n[1] + out.n[2], c = first + (long)blockIdx.x * kWave + lane;
+    float v = 0.0f;
+    if (c < cols) {
+        long r = slice;
+        for (; r + 3 * kSumSlices < rows; r += 4 * kSumSlices) {        // four loads on their way at a time
+            float t[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t[i] = part[(r + i * kSumSlices) * cols + c];
+            for (int i = 0; i < 4; ++i) t[i] = part[(r + i * kSumSlices) * cols + c];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v += t[i];
-            }
-            for (; r < rows; r += kSumSlices) v += part[r * cols + c];
+            for (int i = 0; i < 4; ++i) v += t[i];
         }
-        red[slice][lane] = v;
-        __syncthreads();
-        if (slice == 0 && c < cols) {
-#pragma unroll
-            for (int i = 1; i < kSumSlices; ++i) v += red[i][lane];
-            const int k = c < out.n[0] ? 0 : c < out.n[0] + out.n[1] ? 1 : 2;
-            const long at = c - (k > 0 ? out.n[0] : 0) - (k > 1 ? out.n[1] : 0);
-            float *to = k == 0 ? out.to[0] : k == 1 ? out.to[1] : out.to[2];
-            if (to != nullptr) to[at] = v;
-        }
-        __syncthreads();                     // before `red` is written for the next columns
+        for (; r < rows; r += kSumSlices) v += part[r * cols + c];
     }
+    red[slice][lane] = v;
+    __syncthreads();
+    if (slice != 0 || c >= cols) return;
+#pragma unroll
+    for (int i = 1; i < kSumSlices; ++i) v += red[i][lane];
+    const int k = c < out.n[0] ? 0 : c < out.n[0] + out.n[1] ? 1 : 2;
+    const long at = c - (k > 0 ? out.n[0] : 0) - (k > 1 ? out.n[1] : 0);
+    float *to = k == 0 ? out.to[0] : k == 1 ? out.to[1] : out.to[2];
+    if (to != nullptr) to[at] = v;
 }
 
 // sum over the TPR lanes that share a row; `red`: one slot per wave of the workgroup
@@ -257,8 +252,10 @@ int lanes_of_bwd(int E, int dtype) {
 
 hipError_t launch_sum_rows(const float *part, long rows, const SumTargets &out, hipStream_t s) {
     const long cols = out.n[0] + out.n[1] + out.n[2];
-    const long blocks = (cols + kWave - 1) / kWave;       // beyond 2^20 (2^32 lanes are no launch) the columns go round again
-    sum_rows_kernel<<<(unsigned)(blocks < kMaxGrid ? blocks : kMaxGrid), 1024, 0, s>>>(part, rows, out);
+    for (long first = 0; first < cols; first += kMaxGrid * kWave) {       // one launch; 2^32 lanes and more would be none
+        const long blocks = (cols - first + kWave - 1) / kWave;
+        sum_rows_kernel<<<(unsigned)(blocks < kMaxGrid ? blocks : kMaxGrid), 1024, 0, s>>>(part, rows, out, first);
+    }
     return hipGetLastError();
 }
 
