@@ -358,7 +358,7 @@ int la_recurrent_steps(const void *q, const void *k, const void *v, float *S, fl
  *              at least the row's width (a part of a wider projection's output); all others are dense.
  *              Widths and leading dimensions need no alignment unless said; pointers need 16 bytes.
  *   lengths    [B] int32 on the device, or NULL (every sequence has N tokens).  Tokens from
- *              lengths[b] on are not part of sequence b: nothing is read from their rows, their rows of
+ *              lengths[b] on are not part of sequence b: nothing depends on their rows, their rows of
  *              the outputs (and of the gradients) are zero, and the state handed out is that behind the
  *              last real token.  0 is a sequence without tokens; values outside 0 .. N are taken as
  *              the nearest of these.

@@ -4,8 +4,8 @@
 // registers of the lanes that share it, so that each element is read once: mean, then the sum of squares around it
 // (two passes over registers, no cancellation as in E[x^2] - mean^2), then the result.  16 or 32 lanes share a row
 // of as many 16-byte pieces, 64 one of up to 1024 elements, 256 (backward: 128 up to 2048) up to 8192, 1024 (backward 512) up to
-// 16384.  With a residual, bf16, 16384 x 4096: forward 91 us, backward 114, 5.9 and 4.7 TB/s of 4 tensors each, where a copy
-// of 256 MiB has 5.0; 16384 x 2048: 46 and 49 us.
+// 16384.  With a residual, bf16, 16384 x 4096: forward 96 us, backward 117, 5.6 and 4.6 TB/s of 4 tensors each, where a copy
+// of 256 MiB has 5.0; 16384 x 2048: 52 and 54 us.
 #include "la_layer.h"
 
 namespace la {

@@ -88,7 +88,7 @@ template <int P> __device__ __forceinline__ void store_states(float *p, const fl
 // B_t and C_t of a tile as fp32 pairs in LDS: a wave reads the 2 P values of a token at one address for all its lanes.
 // A thread brings kEach values of a tile there, neighbouring threads neighbouring ones.
 template <typename TT, int NW, int P> struct Pairs {
-    static constexpr int S = NW * P, kEach = 2 * T * S / (64 * NW);        // T * S / 32 / NW: 1 or 2
+    static constexpr int S = NW * P, kEach = 2 * T * S / (64 * NW);        // T * S / 32 / NW: 1, 2 or (four waves of eight states) 4
     float (*lds)[T][S][2];
     const TT *from;                  // this thread's value of the piece's first token
     unsigned ld;
