@@ -452,6 +452,75 @@ int la_scan_step(const void *x, const void *dt, const void *z, const void *Bt, c
                  la_dtype t, void *stream);
 
 /*
+ * ---- The gated delta rule and what stands before it -------------------------------------------
+ * A third recurrent mixer, on the attention's own state S [D,M]: instead of adding phi(k) v^T to it, a token
+ * replaces what the state holds for its key (la_delta_*).  It wants keys of unit length: la_qk_* norms the
+ * queries and keys of each head and turns them by their position in the same pass, also for the attention
+ * above (token-major, as the _bnhd calls take them).  Sizes, types, rows, lengths and the rule for non-finite
+ * inputs are those of the layer's calls; the state's, weights, g and beta are fp32.
+ */
+
+/*
+ * Norm and rotation of H heads of queries and Hk heads of keys of D elements, D a multiple of 8 up to 512:
+ *   n = x * r * w,   r = 1 / sqrt(mean(x^2) + eps) (LA_QK_RMS) or 1 / sqrt(sum(x^2) + eps) (LA_QK_L2), else 1,
+ * and of the first R elements (a multiple of 8, 0 .. D) the pairs (n_i, n_j), i < R / 2, by the angle a = pos * freq[i]:
+ *   (n_i cos a - n_j sin a,  n_i sin a + n_j cos a),   j = i + R / 2, or with LA_QK_ADJACENT the neighbours 2i, 2i + 1.
+ * q [B,N,H,D] (ldq between tokens), k [B,N,Hk,D] (ldk) -> yq, yk dense; Hk = 0: no keys (k, yk NULL).  wq, wk [D] or
+ * NULL (ones).  freq [R/2].  pos [B,N] int32, or NULL: token n is at position n.  Angles are formed in fp64.
+ * One new token of every sequence is N = 1.
+ */
+#define LA_QK_RMS 1
+#define LA_QK_L2 2
+#define LA_QK_ADJACENT 4
+int la_qk_fwd(const void *q, int ldq, const void *k, int ldk, const float *wq, const float *wk, const float *freq,
+              const int *pos, const int *lengths, void *yq, void *yk, int B, int N, int H, int Hk, int D, int R,
+              int flags, float eps, la_dtype t, void *stream);
+/*
+ * Its gradient: dyq, dyk -> dq, dk (all dense), and dwq, dwk [D], each or NULL (also without the weight, as if it were
+ * ones).  ws: la_qk_bwd_workspace() bytes (not needed if both are NULL).
+ */
+size_t la_qk_bwd_workspace(int B, int N, int H, int Hk, int D, la_dtype t);
+int la_qk_bwd(const void *q, int ldq, const void *k, int ldk, const float *wq, const float *wk, const float *freq,
+              const int *pos, const int *lengths, const void *dyq, const void *dyk, void *dq, void *dk,
+              float *dwq, float *dwk, int B, int N, int H, int Hk, int D, int R, int flags, float eps, la_dtype t,
+              void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Gated delta rule over H heads, D = 32, 64 or 128, M a multiple of 16 up to 512:
+ *   S_t = e^{g_t} S_{t-1} + beta_t k_t (v_t - e^{g_t} S_{t-1}^T k_t)^T,   o_t = scale S_t^T q_t.
+ * q, k [B,N,Hk,D] (ldq, ldk): state h has the queries and keys of head h / (H / Hk), Hk divides H.  v [B,N,H,M] (ldv).
+ * g [B,N,H]: logarithm of the decay, usually <= 0, -inf forgets everything before; NULL: no decay.  beta [B,N,H].  o [B,N,H,M].
+ * h0 [B,H,D,M]: the state before token 0, or NULL (zero); h1 [B,H,D,M] out, or NULL: the state behind the last token, for
+ * the next call or la_delta_step.  States stay bounded while beta |k|^2 is at most 2.  Steps whose logarithms are below -1000
+ * count as -1000 (nothing is left either way).
+ * LA_DELTA_KEEP: the workspace then holds, behind the call, what la_delta_bwd starts from.
+ * ws: la_delta_fwd_workspace() bytes with the same flags.  LA_ERR_SHAPE: Hk does not divide H, or B * H chunks of 64 (bf16)
+ * or 32 (fp32) tokens from 2^23 on.  LA_ERR_UNSUPPORTED: D, M, or an unknown flag.
+ */
+#define LA_DELTA_KEEP 1
+size_t la_delta_fwd_workspace(int B, int N, int H, int Hk, int D, int M, la_dtype t, int flags);
+int la_delta_fwd(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *g,
+                 const float *beta, const float *h0, const int *lengths, void *o, float *h1, int B, int N, int H,
+                 int Hk, int D, int M, float scale, int flags, la_dtype t, void *ws, size_t ws_bytes, void *stream);
+/*
+ * Its gradient: dO [B,N,H,M] in; dq, dk [B,N,Hk,D] (sums over the states that share them), dv [B,N,H,M], dbeta [B,N,H]
+ * and dg [B,N,H] out (dg NULL exactly if g is).  dh1 [B,H,D,M]: gradient that reaches h1, or NULL (zero); dh0 [B,H,D,M] out, or NULL.
+ * fwd_ws: the workspace of la_delta_fwd with LA_DELTA_KEEP on the same inputs and sizes, untouched since, and flags then
+ * has LA_DELTA_KEEP; or NULL: it is formed again.  ws: la_delta_bwd_workspace() bytes with the same flags.
+ */
+size_t la_delta_bwd_workspace(int B, int N, int H, int Hk, int D, int M, la_dtype t, int flags);
+int la_delta_bwd(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, const float *g,
+                 const float *beta, const float *h0, const int *lengths, const void *fwd_ws, const void *dO,
+                 const float *dh1, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *dh0, int B, int N,
+                 int H, int Hk, int D, int M, float scale, int flags, la_dtype t, void *ws, size_t ws_bytes,
+                 void *stream);
+/*
+ * One token of every sequence: q, k [B,Hk,D]; v, o [B,H,M]; g (or NULL), beta [B,H]; h [B,H,D,M] in and out.
+ */
+int la_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float *h, void *o,
+                  int B, int H, int Hk, int D, int M, float scale, la_dtype t, void *stream);
+
+/*
  * Optional profiling hook (measurement aid, not part of the method).  The caller creates a
  * la_profile object and owns it.  Between la_profile_begin(p, mask) and la_profile_end(p, ...)
  * every launch that THE CALLING THREAD makes of a kernel whose bit (1u << la_kernel_id) is set

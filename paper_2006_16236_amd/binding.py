@@ -27,8 +27,10 @@ EXPORTS = ("la_status_string", "la_version", "la_causal_fwd_workspace", "la_caus
            "la_recurrent_step", "la_recurrent_steps", "la_causal_fwd_noalloc", "la_kernel_name", "la_profile_begin",
            "la_profile_end", "la_tuning_reload", "la_norm_fwd", "la_norm_bwd_workspace", "la_norm_bwd", "la_conv_fwd",
            "la_conv_bwd_workspace", "la_conv_bwd", "la_conv_step", "la_scan_fwd_workspace", "la_scan_fwd",
-           "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step")
+           "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step", "la_qk_fwd", "la_qk_bwd_workspace", "la_qk_bwd",
+           "la_delta_fwd_workspace", "la_delta_fwd", "la_delta_bwd_workspace", "la_delta_bwd", "la_delta_step")
 LA_SCAN_SOFTPLUS, LA_SCAN_KEEP = 1, 2
+LA_QK_RMS, LA_QK_L2, LA_QK_ADJACENT, LA_DELTA_KEEP = 1, 2, 4, 1
 LA_K_COUNT = 8
 
 
@@ -108,7 +110,13 @@ def _load() -> ctypes.CDLL:
             ("la_scan_fwd_workspace", sz, [i] * 7), ("la_scan_bwd_workspace", sz, [i] * 7),
             ("la_scan_fwd", i, [vp, i] * 5 + [vp] * 7 + [i] * 7 + [vp, sz, vp]),
             ("la_scan_bwd", i, [vp, i] * 5 + [vp] * 17 + [i] * 7 + [vp, sz, vp]),
-            ("la_scan_step", i, [vp] * 10 + [i] * 6 + [vp])):
+            ("la_scan_step", i, [vp] * 10 + [i] * 6 + [vp]),
+            ("la_qk_fwd", i, [vp, i] * 2 + [vp] * 7 + [i] * 7 + [f, i, vp]), ("la_qk_bwd_workspace", sz, [i] * 6),
+            ("la_qk_bwd", i, [vp, i] * 2 + [vp] * 11 + [i] * 7 + [f, i, vp, sz, vp]),
+            ("la_delta_fwd_workspace", sz, [i] * 8), ("la_delta_bwd_workspace", sz, [i] * 8),
+            ("la_delta_fwd", i, [vp, i] * 3 + [vp] * 6 + [i] * 6 + [f, i, i, vp, sz, vp]),
+            ("la_delta_bwd", i, [vp, i] * 3 + [vp] * 13 + [i] * 6 + [f, i, i, vp, sz, vp]),
+            ("la_delta_step", i, [vp] * 7 + [i] * 5 + [f, i, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, argtypes
     return lib
@@ -124,7 +132,7 @@ def _bind_call():
     if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_call.so")):
         class c:
             fwd = bwd = step = norm_fwd = norm_bwd = conv_fwd = conv_bwd = conv_step = scan_fwd = scan_bwd = scan_step = \
-                staticmethod(lambda *args: None)
+                qk_fwd = delta_fwd = delta_step = staticmethod(lambda *args: None)
         return c
     from . import _call as c
     names = ["la_recurrent_step"]
@@ -132,7 +140,8 @@ def _bind_call():
     names += [f"la_{kind}_{way}_workspace" for way in ("fwd", "bwd") for kind in ("causal", "global")]
     c.bind([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names])
     names = ["la_norm_fwd", "la_norm_bwd_workspace", "la_norm_bwd", "la_conv_fwd", "la_conv_bwd_workspace", "la_conv_bwd", "la_conv_step",
-             "la_scan_fwd_workspace", "la_scan_fwd", "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step"]
+             "la_scan_fwd_workspace", "la_scan_fwd", "la_scan_bwd_workspace", "la_scan_bwd", "la_scan_step", "la_qk_fwd",
+             "la_delta_fwd_workspace", "la_delta_fwd", "la_delta_step"]
     c.bind_layer([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names])
     return c
 

@@ -5,6 +5,8 @@
 // Every function answers None when it does not take the call (an argument that is not a plain dense
 // device tensor of the expected sizes, an option it does not know); the caller then goes through its own
 // checks, which name what is wrong.  Nothing is kept between calls.
+#include <math.h>
+
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
@@ -216,7 +218,15 @@ struct Layer {                       // addresses of the library's entry points,
                     void *, void *, void *, float *, float *, float *, float *, int, int, int, int, int, int, int, void *, size_t, void *);
     int (*scan_step)(const void *, const void *, const void *, const void *, const void *, const float *, const float *, const float *,
                      float *, void *, int, int, int, int, int, int, void *);
+    int (*qk_fwd)(const void *, int, const void *, int, const float *, const float *, const float *, const int *, const int *, void *,
+                  void *, int, int, int, int, int, int, int, float, int, void *);
+    size_t (*delta_fwd_ws)(int, int, int, int, int, int, int, int);
+    int (*delta_fwd)(const void *, int, const void *, int, const void *, int, const float *, const float *, const float *, const int *,
+                     void *, float *, int, int, int, int, int, int, float, int, int, void *, size_t, void *);
+    int (*delta_step)(const void *, const void *, const void *, const float *, const float *, float *, void *, int, int, int, int, int,
+                      float, int, void *);
 } g_layer = {};
+constexpr int kLayer = sizeof(Layer) / sizeof(void *);
 
 // Collects the pointers of a call's tensors; ok goes to false at the first one that is not as expected.
 struct Taker {
@@ -528,15 +538,96 @@ PyObject *py_scan_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
-// bind_layer([12 addresses]): in the order of Layer
+PyObject *py_qk_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 12 || g_layer.qk_fwd == nullptr) return not_taken();
+    try {
+        Taker k;
+        const at::Tensor *q = k.lead(a[0], 4), *keys = a[2] == Py_None ? nullptr : Taker::tensor(a[2]), *freq = a[6] == Py_None ? nullptr : Taker::tensor(a[6]);
+        if (q == nullptr || (a[2] != Py_None && (keys == nullptr || keys->dim() != 4 || keys->numel() == 0 || !fits(*keys))) ||
+            (a[6] != Py_None && (freq == nullptr || freq->dim() != 1 || freq->numel() > 0x3fffffff)))
+            return not_taken();
+        const int64_t B = q->size(0), N = q->size(1), H = q->size(2), D = q->size(3), Hk = keys != nullptr ? keys->size(2) : 0;
+        const int64_t R = freq != nullptr ? 2 * freq->size(0) : 0;
+        int ldq, ldk = 0, flags = -1;
+        const void *pq = k.rows(a[0], q->sizes(), ldq), *pk = k.rows(a[2], {B, N, Hk, D}, ldk, true);
+        void *yq = k.mine(a[1], q->sizes()), *yk = keys != nullptr ? k.mine(a[3], {B, N, Hk, D}) : nullptr;
+        const float *wq = k.f32(a[4], {D}, true), *wk = k.f32(a[5], {D}, true), *fr = k.f32(a[6], {R / 2}, true);
+        const int *pos = static_cast<const int *>(k.dense(a[7], {B, N}, at::kInt, true)), *len = static_cast<const int *>(k.dense(a[8], {B}, at::kInt, true));
+        if (a[9] == Py_None) flags = 0;
+        else if (PyUnicode_Check(a[9])) flags = PyUnicode_CompareWithASCIIString(a[9], "rms") == 0 ? 1 : PyUnicode_CompareWithASCIIString(a[9], "l2") == 0 ? 2 : -1;
+        const int adjacent = k.flag(a[10]);
+        if (!k.ok || flags < 0 || (keys == nullptr && a[3] != Py_None) || !PyFloat_Check(a[11])) return not_taken();
+        const float eps = (float)PyFloat_AS_DOUBLE(a[11]);
+        void *s = stream();
+        return PyLong_FromLong(unlocked({a[1], a[3]}, [&] { return g_layer.qk_fwd(pq, ldq, pk, ldk, wq, wk, fr, pos, len, yq, yk, (int)B, (int)N, (int)H, (int)Hk,
+                                                                        (int)D, (int)R, flags | 4 * adjacent, eps, k.code, s); }));
+    } catch (...) {
+        return not_taken();
+    }
+}
+
+// the scale of the outputs: a float, or None for D ** -0.5
+bool scale_of(PyObject *o, int64_t D, float &scale) {
+    if (o != Py_None && !PyFloat_Check(o)) return false;
+    scale = o == Py_None ? (float)(1.0 / sqrt((double)D)) : (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+PyObject *py_delta_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 12 || g_layer.delta_fwd == nullptr) return not_taken();
+    try {
+        Taker k;
+        const at::Tensor *q = k.lead(a[0], 4), *v = Taker::tensor(a[2]);
+        if (q == nullptr || v == nullptr || v->dim() != 4 || !fits(*v)) return not_taken();
+        const int64_t B = q->size(0), N = q->size(1), Hk = q->size(2), D = q->size(3), H = v->size(2), M = v->size(3);
+        if (H < 1 || M < 1 || H % Hk != 0) return not_taken();
+        int ldq, ldk, ldv;
+        const void *pq = k.rows(a[0], q->sizes(), ldq), *pk = k.rows(a[1], q->sizes(), ldk), *pv = k.rows(a[2], {B, N, H, M}, ldv);
+        const float *g = k.f32(a[3], {B, N, H}, true), *beta = k.f32(a[4], {B, N, H}), *h0 = k.f32(a[6], {B, H, D, M}, true);
+        void *o = k.mine(a[5], {B, N, H, M});
+        float *h1 = k.f32(a[7], {B, H, D, M}, true), scale;
+        const int *len = static_cast<const int *>(k.dense(a[8], {B}, at::kInt, true));
+        const int flags = k.flag(a[10]);
+        if (!k.ok || !scale_of(a[9], D, scale)) return not_taken();
+        at::Tensor ws;
+        size_t bytes = 0;
+        void *w = k.workspace(a[11], g_layer.delta_fwd_ws((int)B, (int)N, (int)H, (int)Hk, (int)D, (int)M, k.code, flags), ws, bytes), *s = stream();
+        if (!k.ok) return not_taken();
+        return answer(unlocked({a[5], a[7]}, [&] { return g_layer.delta_fwd(pq, ldq, pk, ldk, pv, ldv, g, beta, h0, len, o, h1, (int)B, (int)N, (int)H, (int)Hk,
+                                                                  (int)D, (int)M, scale, flags, k.code, w, bytes, s); }), a[11], ws);
+    } catch (...) {
+        return not_taken();
+    }
+}
+
+PyObject *py_delta_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 8 || g_layer.delta_step == nullptr) return not_taken();
+    try {
+        Taker k;
+        const at::Tensor *q = k.lead(a[0], 3), *v = Taker::tensor(a[2]);
+        if (q == nullptr || v == nullptr || v->dim() != 3 || !fits(*v)) return not_taken();
+        const int64_t B = q->size(0), Hk = q->size(1), D = q->size(2), H = v->size(1), M = v->size(2);
+        if (H < 1 || M < 1 || H % Hk != 0) return not_taken();
+        const void *pq = k.mine(a[0], {B, Hk, D}), *pk = k.mine(a[1], {B, Hk, D}), *pv = k.mine(a[2], {B, H, M});
+        const float *g = k.f32(a[3], {B, H}, true), *beta = k.f32(a[4], {B, H});
+        float *h = k.f32(a[5], {B, H, D, M}), scale;
+        void *o = k.mine(a[6], {B, H, M});
+        if (!k.ok || !scale_of(a[7], D, scale)) return not_taken();
+        void *s = stream();
+        return PyLong_FromLong(unlocked({a[5], a[6]}, [&] { return g_layer.delta_step(pq, pk, pv, g, beta, h, o, (int)B, (int)H, (int)Hk, (int)D, (int)M, scale, k.code, s); }));
+    } catch (...) {
+        return not_taken();
+    }
+}
+
+// bind_layer([addresses]): in the order of Layer
 PyObject *py_bind_layer(PyObject *, PyObject *list) {
-    static_assert(sizeof(Layer) == 12 * sizeof(void *), "one address each");
-    if (!PyList_Check(list) || PyList_GET_SIZE(list) != 12) {
-        PyErr_SetString(PyExc_ValueError, "12 addresses expected");
+    if (!PyList_Check(list) || PyList_GET_SIZE(list) != kLayer) {
+        PyErr_Format(PyExc_ValueError, "%d addresses expected", kLayer);
         return nullptr;
     }
-    void *p[12];
-    for (int i = 0; i < 12; ++i) {
+    void *p[kLayer];
+    for (int i = 0; i < kLayer; ++i) {
         p[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
         if (PyErr_Occurred()) return nullptr;
     }
@@ -569,6 +660,7 @@ PyMethodDef methods[] = {
 #define LA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
     LA_METHOD(norm_fwd), LA_METHOD(norm_bwd), LA_METHOD(conv_fwd), LA_METHOD(conv_bwd), LA_METHOD(conv_step),
     LA_METHOD(scan_fwd), LA_METHOD(scan_bwd), LA_METHOD(scan_step),
+    LA_METHOD(qk_fwd), LA_METHOD(delta_fwd), LA_METHOD(delta_step),
 #undef LA_METHOD
     {"bind_layer", py_bind_layer, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

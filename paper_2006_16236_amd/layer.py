@@ -367,3 +367,194 @@ def la_scan_step(x, dt, A, Bt, Ct, h, y, D=None, z=None, dt_bias=None, softplus=
     _run("la_scan_step", dev, stream,
          lambda q: _lib.la_scan_step(_p(x), _p(dt), _p(z), _p(Bt), _p(Ct), _p(A), _p(D), _p(dt_bias), _p(h), _p(y), B, E, G, S,
                                      LA_SCAN_SOFTPLUS if softplus else 0, t, q), (h, y))
+
+
+# ---- norm of queries and keys for each head, with the rotation -----------------------------------
+
+_NORMS = {None: 0, "rms": _b.LA_QK_RMS, "l2": _b.LA_QK_L2}
+
+
+def la_qk_bwd_workspace(B, N, H, Hk, D, dtype_code=_b.LA_F32) -> int:
+    return int(_lib.la_qk_bwd_workspace(B, N, H, Hk, D, dtype_code))
+
+
+class _Qk:
+    """Checks the inputs of a head norm: sizes from q and k, distances between tokens."""
+
+    def __init__(self, q, k, wq, wk, freq, pos, lengths, norm, adjacent):
+        self.t, self.dtype, self.dev = _code("q", q), q.dtype, q.device
+        self.B, self.N, self.H, self.D = B, N, H, D = _dims("q", q, 4)
+        if norm not in _NORMS:
+            raise ValueError("norm must be 'rms', 'l2' or None")
+        self.flags = _NORMS[norm] | (_b.LA_QK_ADJACENT if adjacent else 0)
+        self.ldq = _rows("q", q, (B, N, H, D), self.dtype, self.dev)
+        self.Hk, self.ldk = 0, 0
+        if k is not None:
+            _code("k", k)
+            self.Hk = _dims("k", k, 4)[2]
+            self.ldk = _rows("k", k, (B, N, self.Hk, D), self.dtype, self.dev)
+        self.qs, self.ks = (B, N, H, D), (B, N, self.Hk, D)
+        for name, w in (("wq", wq), ("wk", wk)):
+            _like(name, w, (D,), _F32, self.dev, optional=True)
+        self.R = 0
+        if freq is not None:
+            if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
+                raise ValueError("freq must be a tensor [R / 2]")
+            _like("freq", freq, freq.shape, _F32, self.dev)
+            self.R = 2 * freq.shape[0]
+        _like("pos", pos, (B, N), torch.int32, self.dev, optional=True)
+        _like("lengths", lengths, (B,), torch.int32, self.dev, optional=True)
+        self.dims = (B, N, H, self.Hk, D, self.R, self.flags)
+
+    def of_keys(self, k, **named):
+        for name, t in named.items():
+            if (k is None) != (t is None):
+                raise ValueError(f"{name} goes with k")
+            _like(name, t, self.ks, self.dtype, self.dev, optional=True)
+
+
+def la_qk_fwd(q, yq, k=None, yk=None, wq=None, wk=None, freq=None, pos=None, lengths=None, norm="rms", adjacent=False, eps=1e-6, stream=None):
+    """Norm of each head of q [B, N, H, D] and k [B, N, Hk, D] or None ("rms", "l2" or None) with weights wq, wk [D] fp32, and the
+    rotation of its first 2 len(freq) elements by pos * freq (pos [B, N] int32; None: 0 .. N - 1), into yq, yk; pairs are i and
+    i + len(freq), or with adjacent=True neighbours; lengths [B] int32."""
+    took = _call.qk_fwd(q, yq, k, yk, wq, wk, freq, pos, lengths, norm, adjacent, eps) if stream is None else None
+    if took is not None:
+        return _check(took, "la_qk_fwd")
+    c = _Qk(q, k, wq, wk, freq, pos, lengths, norm, adjacent)
+    _like("yq", yq, c.qs, c.dtype, c.dev)
+    c.of_keys(k, yk=yk)
+    _run("la_qk_fwd", c.dev, stream,
+         lambda s: _lib.la_qk_fwd(_p(q), c.ldq, _p(k), c.ldk, _p(wq), _p(wk), _p(freq), _p(pos), _p(lengths), _p(yq), _p(yk), *c.dims,
+                                  float(eps), c.t, s), (yq, yk))
+
+
+def la_qk_bwd(q, dyq, dq, k=None, dyk=None, dk=None, wq=None, wk=None, freq=None, pos=None, lengths=None, norm="rms", adjacent=False,
+              eps=1e-6, dwq=None, dwk=None, ws=None, stream=None):
+    """dq, dk, dwq, dwk of la_qk_fwd from dyq, dyk.  Returns the workspace it used (None if it needed none)."""
+    c = _Qk(q, k, wq, wk, freq, pos, lengths, norm, adjacent)
+    for name, t in (("dyq", dyq), ("dq", dq)):
+        _like(name, t, c.qs, c.dtype, c.dev)
+    c.of_keys(k, dyk=dyk, dk=dk)
+    for name, t in (("dwq", dwq), ("dwk", dwk)):
+        _like(name, t, (c.D,), _F32, c.dev, optional=True)
+    if k is None and dwk is not None:
+        raise ValueError("dwk goes with k")
+    if dwq is not None or dwk is not None:
+        ws = _workspace(ws, la_qk_bwd_workspace(c.B, c.N, c.H, c.Hk, c.D, c.t), c.dev, stream)
+    _run("la_qk_bwd", c.dev, stream,
+         lambda s: _lib.la_qk_bwd(_p(q), c.ldq, _p(k), c.ldk, _p(wq), _p(wk), _p(freq), _p(pos), _p(lengths), _p(dyq), _p(dyk), _p(dq),
+                                  _p(dk), _p(dwq), _p(dwk), *c.dims, float(eps), c.t, _p(ws), 0 if ws is None else _size(ws), s),
+         (dq, dk, dwq, dwk))
+    return ws
+
+
+# ---- gated delta rule ------------------------------------------------------------------------------
+
+def la_delta_fwd_workspace(B, N, H, Hk, D, M, dtype_code=_b.LA_F32, flags=0) -> int:
+    return int(_lib.la_delta_fwd_workspace(B, N, H, Hk, D, M, dtype_code, flags))
+
+
+def la_delta_bwd_workspace(B, N, H, Hk, D, M, dtype_code=_b.LA_F32, flags=0) -> int:
+    """flags = LA_DELTA_KEEP: for a call that is given the forward's workspace."""
+    return int(_lib.la_delta_bwd_workspace(B, N, H, Hk, D, M, dtype_code, flags))
+
+
+class _Delta:
+    """Checks the inputs of a delta rule: sizes from q and v, distances between tokens."""
+
+    def __init__(self, q, k, v, g, beta, lengths, scale):
+        self.t, self.dtype, self.dev = _code("q", q), q.dtype, q.device
+        B, N, Hk, D = _dims("q", q, 4)
+        if not isinstance(v, torch.Tensor) or v.dim() != 4:
+            raise ValueError("v must be a tensor [B, N, H, M]")
+        H, M = _dims("v", v, 4)[2:]
+        if Hk < 1 or H % Hk:
+            raise ValueError(f"q: {Hk} heads do not divide the {H} of v")
+        self.keys, self.rows, self.per, self.state = (B, N, Hk, D), (B, N, H, M), (B, N, H), (B, H, D, M)
+        self.ld = [_rows("q", q, self.keys, self.dtype, self.dev), _rows("k", k, self.keys, self.dtype, self.dev),
+                   _rows("v", v, self.rows, self.dtype, self.dev)]
+        _like("g", g, self.per, _F32, self.dev, optional=True)
+        _like("beta", beta, self.per, _F32, self.dev)
+        _like("lengths", lengths, (B,), torch.int32, self.dev, optional=True)
+        self.scale = float(D) ** -0.5 if scale is None else float(scale)
+        self.dims = (B, N, H, Hk, D, M)
+
+    def states(self, **named):
+        for name, t in named.items():
+            _like(name, t, self.state, _F32, self.dev, optional=True)
+
+    def inputs(self, q, k, v, g, beta, h0, lengths):
+        return _p(q), self.ld[0], _p(k), self.ld[1], _p(v), self.ld[2], _p(g), _p(beta), _p(h0), _p(lengths)
+
+
+def la_delta_fwd(q, k, v, g, beta, o, h0=None, h1=None, lengths=None, scale=None, keep=False, ws=None, stream=None):
+    """Gated delta rule of q, k [B, N, Hk, D], v [B, N, H, M] with logarithms of the decay g (or None) and strengths beta
+    [B, N, H] fp32 into o [B, N, H, M]; h0, h1 [B, H, D, M] fp32: the states before and after; lengths [B] int32; scale (None:
+    D ** -0.5) is that of the outputs.  Returns the workspace it used; with keep=True it holds what la_delta_bwd starts
+    from (fwd_ws)."""
+    took = _call.delta_fwd(q, k, v, g, beta, o, h0, h1, lengths, scale, keep, ws) if stream is None else None
+    if took is not None:
+        if type(took) is int:
+            _check(took, "la_delta_fwd")
+        return took
+    c = _Delta(q, k, v, g, beta, lengths, scale)
+    _like("o", o, c.rows, c.dtype, c.dev)
+    c.states(h0=h0, h1=h1)
+    flags = _b.LA_DELTA_KEEP if keep else 0
+    ws = _workspace(ws, la_delta_fwd_workspace(*c.dims, c.t, flags), c.dev, stream)
+    _run("la_delta_fwd", c.dev, stream,
+         lambda s: _lib.la_delta_fwd(*c.inputs(q, k, v, g, beta, h0, lengths), _p(o), _p(h1), *c.dims, c.scale, flags, c.t, _p(ws),
+                                     _size(ws), s), (o, h1))
+    return ws
+
+
+def la_delta_bwd(q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, h0=None, dh1=None, dh0=None, lengths=None, scale=None, fwd_ws=None,
+                 ws=None, stream=None):
+    """The gradients of la_delta_fwd from do [B, N, H, M] and dh1 [B, H, D, M], the gradient of the state handed on.  fwd_ws: the
+    workspace of la_delta_fwd(keep=True) on the same inputs (None: it is formed again).  Returns the workspace it used."""
+    c = _Delta(q, k, v, g, beta, lengths, scale)
+    _like("do", do, c.rows, c.dtype, c.dev)
+    _like("dv", dv, c.rows, c.dtype, c.dev)
+    for name, t in (("dq", dq), ("dk", dk)):
+        _like(name, t, c.keys, c.dtype, c.dev)
+    if (g is None) != (dg is None):
+        raise ValueError("dg goes with g")
+    _like("dg", dg, c.per, _F32, c.dev, optional=True)
+    _like("dbeta", dbeta, c.per, _F32, c.dev)
+    c.states(h0=h0, dh1=dh1, dh0=dh0)
+    flags = 0
+    if fwd_ws is not None:
+        _bytes("fwd_ws", fwd_ws, c.dev)
+        flags = _b.LA_DELTA_KEEP
+        need = la_delta_fwd_workspace(*c.dims, c.t, flags)
+        if _size(fwd_ws) < need:
+            raise ValueError(f"fwd_ws: {_size(fwd_ws)} bytes, {need} expected: not a workspace of la_delta_fwd(keep=True) on these sizes")
+    ws = _workspace(ws, la_delta_bwd_workspace(*c.dims, c.t, flags), c.dev, stream)
+    _run("la_delta_bwd", c.dev, stream,
+         lambda s: _lib.la_delta_bwd(*c.inputs(q, k, v, g, beta, h0, lengths), _p(fwd_ws), _p(do), _p(dh1), _p(dq), _p(dk), _p(dv),
+                                     _p(dg), _p(dbeta), _p(dh0), *c.dims, c.scale, flags, c.t, _p(ws), _size(ws), s),
+         (dq, dk, dv, dg, dbeta, dh0))
+    return ws
+
+
+def la_delta_step(q, k, v, g, beta, h, o, scale=None, stream=None):
+    """One token of every sequence: q, k [B, Hk, D]; v, o [B, H, M]; g (or None), beta [B, H] fp32; h [B, H, D, M] fp32, updated in
+    place."""
+    took = _call.delta_step(q, k, v, g, beta, h, o, scale) if stream is None else None
+    if took is not None:
+        return _check(took, "la_delta_step")
+    t, dtype, dev = _code("q", q), q.dtype, q.device
+    B, Hk, D = _dims("q", q, 3)
+    if not isinstance(v, torch.Tensor) or v.dim() != 3:
+        raise ValueError("v must be a tensor [B, H, M]")
+    H, M = _dims("v", v, 3)[1:]
+    if Hk < 1 or H % Hk:
+        raise ValueError(f"q: {Hk} heads do not divide the {H} of v")
+    for name, x, shape in (("q", q, (B, Hk, D)), ("k", k, (B, Hk, D)), ("v", v, (B, H, M)), ("o", o, (B, H, M))):
+        _like(name, x, shape, dtype, dev)
+    _like("g", g, (B, H), _F32, dev, optional=True)
+    _like("beta", beta, (B, H), _F32, dev)
+    _like("h", h, (B, H, D, M), _F32, dev)
+    _run("la_delta_step", dev, stream,
+         lambda s: _lib.la_delta_step(_p(q), _p(k), _p(v), _p(g), _p(beta), _p(h), _p(o), B, H, Hk, D, M,
+                                      float(D) ** -0.5 if scale is None else float(scale), t, s), (h, o))
