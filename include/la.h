@@ -489,6 +489,7 @@ int la_qk_bwd(const void *q, int ldq, const void *k, int ldk, const float *wq, c
  * Gated delta rule over H heads, D = 32, 64 or 128, M a multiple of 16 up to 512:
  *   S_t = e^{g_t} S_{t-1} + beta_t k_t (v_t - e^{g_t} S_{t-1}^T k_t)^T,   o_t = scale S_t^T q_t.
  * q, k [B,N,Hk,D] (ldq, ldk): state h has the queries and keys of head h / (H / Hk), Hk divides H.  v [B,N,H,M] (ldv).
+ * ldq, ldk, ldv: multiples of 8 (LA_ERR_ALIGN) up to 2^23 (LA_ERR_SHAPE).
  * g [B,N,H]: logarithm of the decay, usually <= 0, -inf forgets everything before; NULL: no decay.  beta [B,N,H].  o [B,N,H,M].
  * h0 [B,H,D,M]: the state before token 0, or NULL (zero); h1 [B,H,D,M] out, or NULL: the state behind the last token, for
  * the next call or la_delta_step.  States stay bounded while beta |k|^2 is at most 2.  Steps whose logarithms are below -1000

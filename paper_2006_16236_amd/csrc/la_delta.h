@@ -21,9 +21,10 @@ __device__ __forceinline__ int paired(int tile, int i) { return 32 * (tile >> 1)
 template <int P> struct Parts {
     bf16x8_t p[P];
 };
-template <int PA, int PB> __device__ __forceinline__ f32x4 product(const Parts<PA> &a, const Parts<PB> &b, f32x4 acc) {
+// kLast = 1: down to 2^-8 only, for values that are rounded to bf16 next
+template <int kLast = 2, int PA, int PB> __device__ __forceinline__ f32x4 product(const Parts<PA> &a, const Parts<PB> &b, f32x4 acc) {
 #pragma unroll
-    for (int s = 2; s >= 0; --s)                              // the small part products first
+    for (int s = kLast; s >= 0; --s)                          // the small part products first
 #pragma unroll
         for (int i = 0; i <= s; ++i)
             if (i < PA && s - i < PB) acc = mfma32_bf16(a.p[i], b.p[s - i], acc);
@@ -34,6 +35,69 @@ __device__ __forceinline__ Parts<3> cut(f32x4 lo, f32x4 hi) {
     const Split3 a = split3(x), b = split3(y);
     return Parts<3>{{cat_parts(a.h, b.h), cat_parts(a.m, b.m), cat_parts(a.l, b.l)}};
 }
+// N products with one right operand, a part product of all of them at a time: what follows on each other goes to other results
+template <int kLast = 2, int N, int PA, int PB> __device__ __forceinline__ void products(const Parts<PA> (&a)[N], const Parts<PB> &b, f32x4 (&acc)[N]) {
+#pragma unroll
+    for (int s = kLast; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i <= s; ++i)
+            if (i < PA && s - i < PB) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) acc[n] = mfma32_bf16(a[n].p[i], b.p[s - i], acc[n]);
+            }
+}
+// acc[t] += tri[t][s] b[s] over the 32 x 32 blocks on and below the diagonal
+template <int kLast, int N, int S, int PA, int PB> __device__ __forceinline__ void lower_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = kLast; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i <= k; ++i)
+                if (i < PA && k - i < PB) {
+#pragma unroll
+                    for (int t = 2 * s; t < N; ++t) acc[t] = mfma32_bf16(tri[t][s].p[i], b[s].p[k - i], acc[t]);
+                }
+}
+// the same with the transposed matrix: acc[t] += tri[s][t]^T b[s], blocks s >= t / 2 of block column t / 2
+template <int kLast, int N, int S, int PA, int PB> __device__ __forceinline__ void upper_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = kLast; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i <= k; ++i)
+                if (i < PA && k - i < PB) {
+#pragma unroll
+                    for (int t = 0; t < 2 * (s + 1); ++t) acc[t] = mfma32_bf16(tri[t][s].p[i], b[s].p[k - i], acc[t]);
+                }
+}
+// What is written before this point is issued before what is written behind it: the reads of operands that a later product
+// takes stay ahead of the products before that.
+__device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
+// Between two such points: a matrix instruction (16 cycles of its pipe), then `valu` vector instructions that run beside it, N times.
+template <int N> __device__ __forceinline__ void side_by_side() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+    }
+}
+template <int P> __device__ __forceinline__ Parts<P> cut_to(f32x4 lo, f32x4 hi) {
+    if constexpr (P == 3) {
+        return cut(lo, hi);
+    } else {
+        const float x[4] = {lo[0], lo[1], lo[2], lo[3]}, y[4] = {hi[0], hi[1], hi[2], hi[3]};
+        const Split2 a = split2(x), b = split2(y);
+        return Parts<2>{{cat_parts(a.h, b.h), cat_parts(a.m, b.m)}};
+    }
+}
+template <int P> __device__ __forceinline__ Parts<P> first(const Parts<3> &x) {
+    Parts<P> y;
+#pragma unroll
+    for (int i = 0; i < P; ++i) y.p[i] = x.p[i];
+    return y;
+}
 // A value that a later token of the chunk may have spoiled: its products with masked zeros have to be zeros.
 __device__ __forceinline__ f32x4 finite(f32x4 v) {
 #pragma unroll
@@ -42,16 +106,19 @@ __device__ __forceinline__ f32x4 finite(f32x4 v) {
 }
 
 // ---- matrices of bf16 parts in LDS --------------------------------------------------------------
-// Rows of COLS elements in pieces of eight (16 bytes), the pieces of a row exchanged by a function of the row, so that
-// 16 lanes that read one piece of 16 rows (also of 16 paired ones) meet all banks.
-template <int COLS> __device__ __forceinline__ int mat_at(int row, int piece) {
-    const int f = COLS == 32 ? ((row >> 1) & 1) | ((row >> 2) & 2) : (row & 3) | ((row >> 1) & 4);
+// Rows of COLS elements in pieces of eight (16 bytes), the pieces of a row exchanged by a function of the row such that a wave's
+// reads below take 4.4 cycles, the least for 1 KB (measured; others took 8 or 16): 16-byte reads of one piece of 16 paired
+// rows, transposed reads of paired and of neighbouring columns.  kPlain: the same for 16 rows in a run.
+template <int COLS, bool kPlain = false> __device__ __forceinline__ int mat_at(int row, int piece) {
+    int f;
+    if constexpr (kPlain) f = COLS == 128 ? row & 15 : COLS == 64 ? row & 7 : (row >> 1) & 3;
+    else f = ((row >> 2) & 3) | (COLS == 128 ? 4 * (row & 3) : COLS == 64 ? 2 * (row & 2) : 0);
     return row * COLS + 8 * (piece ^ f);
 }
 // lane (c, g): eight neighbours of one row
-template <int COLS, int P> __device__ __forceinline__ Parts<P> row_operand(const uint16_t *m, int plane, int row, int piece) {
+template <int COLS, int P, bool kPlain = false> __device__ __forceinline__ Parts<P> row_operand(const uint16_t *m, int plane, int row, int piece) {
     Parts<P> o;
-    const uint16_t *p = m + mat_at<COLS>(row, piece);
+    const uint16_t *p = m + mat_at<COLS, kPlain>(row, piece);
 #pragma unroll
     for (int i = 0; i < P; ++i) o.p[i] = *reinterpret_cast<const bf16x8_t *>(p + i * plane);
     return o;
@@ -64,15 +131,15 @@ __device__ __forceinline__ u32x2_t read_column(const uint16_t *p) {
     return __builtin_bit_cast(u32x2_t, v);
 }
 // lane (c, g): rows row0 + 8g .. 8g + 7 of one column, 16 tile + c or paired(tile, c)
-template <int COLS, bool kPaired> __device__ __forceinline__ bf16x8_t column_part(const uint16_t *m, int row0, int tile, int lane) {
+template <int COLS, bool kPaired, bool kPlain> __device__ __forceinline__ bf16x8_t column_part(const uint16_t *m, int row0, int tile, int lane) {
     const int q = lane & 15, r = row0 + 8 * (lane >> 4) + (q >> 2);
     const int piece = kPaired ? 4 * (tile >> 1) + (q & 3) : 2 * tile + ((q >> 1) & 1), half = kPaired ? 4 * (tile & 1) : 4 * (q & 1);
-    return cat_parts(read_column(m + mat_at<COLS>(r, piece) + half), read_column(m + mat_at<COLS>(r + 4, piece) + half));
+    return cat_parts(read_column(m + mat_at<COLS, kPlain>(r, piece) + half), read_column(m + mat_at<COLS, kPlain>(r + 4, piece) + half));
 }
-template <int COLS, bool kPaired, int P> __device__ __forceinline__ Parts<P> column_operand(const uint16_t *m, int plane, int row0, int tile, int lane) {
+template <int COLS, bool kPaired, int P, bool kPlain = false> __device__ __forceinline__ Parts<P> column_operand(const uint16_t *m, int plane, int row0, int tile, int lane) {
     Parts<P> o;
 #pragma unroll
-    for (int i = 0; i < P; ++i) o.p[i] = column_part<COLS, kPaired>(m + i * plane, row0, tile, lane);
+    for (int i = 0; i < P; ++i) o.p[i] = column_part<COLS, kPaired, kPlain>(m + i * plane, row0, tile, lane);
     return o;
 }
 
@@ -139,60 +206,166 @@ __device__ __forceinline__ bool head_and_columns(const DeltaArgs &a, int &bh, in
 }
 inline unsigned head_grid(const DeltaArgs &a) { return (unsigned)((a.B * a.H + 7) / 8 * 8 * ((a.M + kCols - 1) / kCols)); }
 
-// K, Q and the chunk-local matrices on their way from memory to LDS.
+// Rows of a tensor as the range check of a buffer descriptor sees them: loads behind the last one's `width` elements give zeros,
+// stores there are left out.  The whole offset goes into the lane's own address, which is what is checked.
+typedef __amdgpu_buffer_rsrc_t Range;
+template <typename T> __device__ __forceinline__ Range range_of(const T *first, int rows, long ld, int width) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(first), 0, rows > 0 ? (int)(((rows - 1) * ld + width) * (long)sizeof(T)) : 0, 0x00020000);
+}
+template <typename T> __device__ __forceinline__ Eight<T> load_eight(Range r, int byte) {
+    Eight<T> e;
+    const u32x4_t lo = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, byte, 0, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.w[i] = lo[i];
+    if constexpr (sizeof(T) == 4) {
+        const u32x4_t hi = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, byte + 16, 0, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.w[4 + i] = hi[i];
+    }
+    return e;
+}
+template <typename T> __device__ __forceinline__ void store_value(Range r, int byte, float v) {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16_bits(v), r, byte, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, byte, 0, 0);
+}
+
+// A chunk in LDS, and on its way there: K, Q, a workgroup's columns of V (or dO), the chunk-local matrices, the factors of the
+// decay and beta.  Four waves of a workgroup do nothing else: they cut the next chunk's values into parts and write them to the
+// other of two buffers while the four others work, one barrier a chunk, and have the one after that on its way from memory.
+template <typename T, int D> struct Chunked {
+    using Ch = Chunk<T>;
+    static constexpr int kTok = Ch::P * Ch::C * D, kVal = Ch::P * Ch::C * kCols, kTri = 3 * Ch::kTri;
+    alignas(16) uint16_t k[kTok], q[kTok], v[kVal], z[kTri], m[kTri];
+    alignas(16) float gates[3 * Ch::C];
+};
 template <typename T, int D> struct Fetch {
     using Ch = Chunk<T>;
-    static constexpr int kTok = Ch::C * D / 8, kTokEach = (kTok + 255) / 256, kTriEach = (2 * Ch::kTri / 8 + 255) / 256;
-    Eight<T> k[kTokEach], q[kTokEach];
+    static constexpr int C = Ch::C, kTok = C * D / 8, kTokEach = (kTok + 255) / 256, kVal = C * kCols / 8, kValEach = (kVal + 255) / 256;
+    static constexpr int kTri = Ch::kTri / 8, kTriEach = (2 * kTri + 255) / 256;
+    static_assert(2 * kTri % 256 == 0 && kVal % 256 == 0, "whole turns of 256 threads");
+    Eight<T> k[kTokEach], q[kTokEach], v[kValEach];
     Eight<float> tri[kTriEach];
     float gate, beta;
-    __device__ __forceinline__ void load(const DeltaArgs &a, long unit, size_t row0, int left, int hk, int h, int tid) {
+    // left: tokens from this chunk's first to the sequence's end, rows behind it come as zeros; values: at the workgroup's first
+    // column, `cols` of them
+    __device__ __forceinline__ void load(const DeltaArgs &a, long unit, size_t row0, int left, int hk, int h, const T *values, long ldv, int cols, int tid) {
+        const int rows = left < C ? left : C;
+        const Range kr = range_of((const T *)a.k + row0 * a.ldk + (size_t)hk * D, rows, a.ldk, D);
+        const Range qr = range_of((const T *)a.q + row0 * a.ldq + (size_t)hk * D, rows, a.ldq, D);
+        const Range vr = range_of(values + row0 * ldv, rows, ldv, cols);
+        const Range br = range_of(a.beta + row0 * a.H + h, rows, a.H, 1);
+        constexpr int e = sizeof(T);
 #pragma unroll
         for (int j = 0; j < kTokEach; ++j) {
             const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
-            const bool live = i < kTok && t < left;
-            k[j] = load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, live);
-            q[j] = load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, live);
+            k[j] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * e);
+            q[j] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * e);
+        }
+#pragma unroll
+        for (int j = 0; j < kValEach; ++j) {
+            const int i = tid + 256 * j, t = i / 8, piece = i % 8;
+            v[j] = load_eight<T>(vr, 8 * piece < cols ? (t * (int)ldv + 8 * piece) * e : 0x7fffff00);
         }
         const float *m = a.tri + unit * 2 * Ch::kTri;
 #pragma unroll
-        for (int j = 0; j < kTriEach; ++j) tri[j] = load_eight<float>(m + 8 * (tid + 256 * j), tid + 256 * j < 2 * Ch::kTri / 8);
-        gate = tid < 2 * Ch::C ? a.gate[unit * 4 * Ch::C + tid] : 0.0f;
-        beta = tid < Ch::C && tid < left ? a.beta[(row0 + tid) * a.H + h] : 0.0f;
+        for (int j = 0; j < kTriEach; ++j) __builtin_memcpy(tri[j].w, m + 8 * (tid + 256 * j), sizeof(tri[j].w));
+        gate = a.gate[unit * 4 * C + tid % (2 * C)];
+        beta = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(br, tid * a.H * 4, 0, 0));
     }
-    __device__ __forceinline__ void park(uint16_t *kS, uint16_t *qS, uint16_t *triS, float *gates, int tid) const {
+    __device__ __forceinline__ void park(Chunked<T, D> &to, int tid) const {
 #pragma unroll
         for (int j = 0; j < kTokEach; ++j) {
             const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
-            if (i >= kTok) break;
-            park_eight<T>(kS + mat_at<D>(t, piece), Ch::C * D, k[j]);
-            park_eight<T>(qS + mat_at<D>(t, piece), Ch::C * D, q[j]);
+            if (kTok % 256 != 0 && i >= kTok) break;
+            park_eight<T>(to.k + mat_at<D>(t, piece), C * D, k[j]);
+            park_eight<T>(to.q + mat_at<D>(t, piece), C * D, q[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kValEach; ++j) {
+            const int i = tid + 256 * j;
+            park_eight<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kTriEach; ++j) {
-            const int i = tid + 256 * j, which = i / (Ch::kTri / 8), at = i % (Ch::kTri / 8);
-            if (i >= 2 * Ch::kTri / 8) break;
-            park_eight<float>(triS + which * 3 * Ch::kTri + mat_at<32>(at / 4, at % 4), Ch::kTri, tri[j]);
+            const int i = tid + 256 * j, at = i < kTri ? i : i - kTri;
+            park_eight<float>((i < kTri ? to.z : to.m) + mat_at<32>(at / 4, at % 4), Ch::kTri, tri[j]);
         }
-        if (tid < 2 * Ch::C) gates[tid] = gate;
-        if (tid < Ch::C) gates[2 * Ch::C + tid] = beta;
+        if (tid < 2 * C) to.gates[tid] = gate;
+        if (tid < C) to.gates[2 * C + tid] = beta;
     }
 };
+// The fetching waves: chunks first, first + by, .. of `count`.  The others meet the same barriers: one before their first chunk, and
+// one behind each.
+template <typename T, int D> __device__ __forceinline__ void fetch_chunks(Chunked<T, D> (&to)[2], const DeltaArgs &a, int bh, int len, int first, int by, int count,
+                                                                          const T *values, long ldv, int cols, int tid) {
+    constexpr int C = Chunk<T>::C;
+    const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
+    Fetch<T, D> f;
+    const auto load = [&](int i) {
+        const int chunk = first + by * (i < count ? i : count - 1);
+        f.load(a, (long)bh * a.K + chunk, (size_t)b * a.N + (size_t)chunk * C, len - chunk * C, hk, h, values, ldv, cols, tid);
+    };
+    if (count == 0) return;
+    load(0);
+    f.park(to[0], tid);
+    load(1);
+    __syncthreads();
+    for (int i = 0; i < count; ++i) {
+        f.park(to[(i + 1) & 1], tid);
+        load(i + 2);
+        __syncthreads();
+    }
+}
+// The loads of a state before the first chunk: waited for here, so that the loop need not wait for them with everything else.
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// Values in LDS, of P parts: rows row0 .. + 3 of the lane's group, column of this lane, and their sum in fp32.
+template <int P> struct Raw4 {
+    u32x2_t p[P];
+    __device__ __forceinline__ f32x4 sum() const {
+        f32x4 v = widen(p[P - 1]);
+#pragma unroll
+        for (int i = P - 2; i >= 0; --i) v += widen(p[i]);
+        return v;
+    }
+};
+template <int COLS, int P, bool kPlain = false> __device__ __forceinline__ Raw4<P> column_values(const uint16_t *m, int plane, int row0, int tile, int lane) {
+    const int q = lane & 15, r = row0 + (q >> 2), piece = 2 * tile + ((q >> 1) & 1), half = 4 * (q & 1);
+    Raw4<P> v;
+#pragma unroll
+    for (int i = 0; i < P; ++i) v.p[i] = read_column(m + i * plane + mat_at<COLS, kPlain>(r, piece) + half);
+    return v;
+}
 
-// 16 columns of a state: tile t, register r holds row paired(t, 4g + r)
-template <int D> __device__ __forceinline__ void load_state(const float *p, int M, int g, f32x4 (&S)[D / 16]) {
+// 16 columns of a state (zeros without it); `column`: this lane's; tile t, register r holds row paired(t, 4g + r)
+template <int D> __device__ __forceinline__ void load_state(const float *state, int column, int M, int g, f32x4 (&S)[D / 16]) {
+    const Range r = range_of(state, state == nullptr ? 0 : D, M, M);
+    const int lane = (8 * g * M + column) * 4;
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = p == nullptr ? 0.0f : p[(size_t)paired(t, 4 * g + r) * M];
+        for (int i = 0; i < 4; ++i) S[t][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, lane + paired(t, i) * M * 4, 0, 0));
 }
-template <int D> __device__ __forceinline__ void store_state(float *p, int M, int g, const f32x4 (&S)[D / 16]) {
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p[(size_t)paired(t, 4 * g + r) * M] = S[t][r];
+// The 4 x 4 block of four neighbouring lanes and their four values, transposed: lane 4i + b then has row b of the four columns
+// 4i .. + 3, which leave as one 16-byte store instead of four of 4 bytes.
+__device__ __forceinline__ f32x4 transpose4(f32x4 v, int lane) {
+    const bool odd = lane & 1, high = lane & 2;
+    const float a = dpp_move<0xB1>(odd ? v[0] : v[1]), b = dpp_move<0xB1>(odd ? v[2] : v[3]);
+    v = f32x4{odd ? a : v[0], odd ? v[1] : a, odd ? b : v[2], odd ? v[3] : b};
+    const float c = dpp_move<0x4E>(high ? v[0] : v[2]), d = dpp_move<0x4E>(high ? v[1] : v[3]);
+    return f32x4{high ? c : v[0], high ? d : v[1], high ? v[2] : c, high ? v[3] : d};
 }
-
+// A wave's 16 x 16 tile of rows `row` + (0 .. 3) per lane group, 16 columns from `column` on, of a row-major matrix
+template <typename T> __device__ __forceinline__ void store_tile(Range r, int row, int column, int ld, f32x4 v, int lane) {
+    v = transpose4(v, lane);
+    const int at = ((row + (lane & 3)) * ld + column + (lane & 12)) * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{round_pair(v[0], v[1]), round_pair(v[2], v[3])}, r, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, at, 0, 0);
+}
+template <int D> __device__ __forceinline__ void store_state(float *state, int column, int M, int lane, const f32x4 (&S)[D / 16]) {
+    const Range r = range_of(state, D, M, M);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) store_tile<float>(r, paired(t, 4 * (lane / 16)), column, M, S[t], lane);
+}
 #define LA_BY_WIDTH(CALL)                                    \
     if (dtype == 0) {                                        \
         if (a.D == 32) CALL(float, 32);                      \

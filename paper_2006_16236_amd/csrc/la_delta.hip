@@ -23,9 +23,9 @@ namespace {
 template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kRow = C + 4;
-    __shared__ uint16_t kS[P * C * D], qS[P * C * D];
-    __shared__ float low[C * kRow];                          // A, strictly lower
-    __shared__ float gh[C], gl[C], bt[C];
+    __shared__ alignas(16) uint16_t kS[P * C * D], qS[P * C * D];
+    __shared__ alignas(16) float low[C * kRow];                          // A, strictly lower
+    __shared__ alignas(16) float gh[C], gl[C], bt[C];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16;
     const long unit = blockIdx.x;
     const int chunk = (int)(unit % a.K), bh = (int)(unit / a.K), b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
@@ -37,8 +37,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         const bool live = t0 + t < len;
         const Eight<T> k = load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, live);
         const Eight<T> q = load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, live);
-        park_eight<T>(kS + mat_at<D>(t, piece), C * D, k);
-        park_eight<T>(qS + mat_at<D>(t, piece), C * D, q);
+        park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, k);
+        park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, q);
     }
     float *gate = a.gate + unit * 4 * C;
     if (wave == 0) {
@@ -69,9 +69,9 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         if (ct <= rt) {
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) {
-                const Parts<P> y = row_operand<D, P>(kS, C * D, 16 * ct + c, 4 * s + g);
-                kk = product(row_operand<D, P>(kS, C * D, 16 * rt + c, 4 * s + g), y, kk);
-                qk = product(row_operand<D, P>(qS, C * D, 16 * rt + c, 4 * s + g), y, qk);
+                const Parts<P> y = row_operand<D, P, true>(kS, C * D, 16 * ct + c, 4 * s + g);
+                kk = product(row_operand<D, P, true>(kS, C * D, 16 * rt + c, 4 * s + g), y, kk);
+                qk = product(row_operand<D, P, true>(qS, C * D, 16 * rt + c, 4 * s + g), y, qk);
             }
         }
         const int s = 16 * ct + c;
@@ -102,112 +102,157 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
 }
 
 // ---- through the chunks -----------------------------------------------------------------------------
-template <typename T, int D> __global__ __launch_bounds__(256) void delta_fwd_kernel(const DeltaArgs a) {
+// What only leads to outputs in bf16 takes two parts a value (2^-16): Q S and M beta u.  The state's way takes three.
+// A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
+// the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
+// depends on a branch.
+template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks;
-    __shared__ uint16_t kS[P * C * D], qS[P * C * D], triS[2 * 3 * Ch::kTri];
-    __shared__ float gates[3 * C];
-    const uint16_t *zS = triS, *mS = triS + 3 * Ch::kTri;
+    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
+    __shared__ Chunked<T, D> buffers[2];
     int bh, m0;
     if (!head_and_columns(a, bh, m0)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16, m = m0 + tid / kWave * 16 + c;
-    const bool mine = m < a.M;                               // all of a wave's columns or none (M is a multiple of 16)
-    const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk), len = length_of(a, b), chunks = (len + C - 1) / C;
-    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M + m, ldo = (size_t)a.H * a.M;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, m = m0 + wave * 16 + c;
+    const int b = bh / a.H, h = bh % a.H, len = length_of(a, b), chunks = (len + C - 1) / C;
+    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, ldo = a.H * a.M;
+    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M;
+    if (wave >= 4) {
+        fetch_chunks<T, D>(buffers, a, bh, len, 0, 1, chunks, (const T *)a.v + (size_t)h * a.M + m0, a.ldv, cols, tid - 256);
+        return;
+    }
+    if (wave * 16 >= cols) {                                 // no columns (M is a multiple of 16)
+        if (chunks > 0) __syncthreads();
+        for (int chunk = 0; chunk < chunks; ++chunk) __syncthreads();
+        return;
+    }
     f32x4 S[D / 16];
-    load_state<D>(a.h0 == nullptr || !mine ? nullptr : a.h0 + state, a.M, g, S);
-    Fetch<T, D> next;
-    f32x4 v[kTiles];
-    const auto load_values = [&](int chunk) {                // a column's elements of the paired rows
+    load_state<D>(a.h0 == nullptr ? nullptr : a.h0 + state, m, a.M, g, S);
+    loads_done();
+    Parts<3> sp[kSteps];                                     // the state as an operand
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = chunk * C + paired(t, 4 * g + r);
-                v[t][r] = mine && n < len ? raw_to_f32((const T *)a.v + (seq + n) * a.ldv + (size_t)h * a.M + m) : 0.0f;
-            }
-    };
-    if (chunks > 0) next.load(a, (long)bh * a.K, seq, len, hk, h, tid), load_values(0);
+    for (int s = 0; s < kSteps; ++s) sp[s] = cut(S[2 * s], S[2 * s + 1]);
+    if (chunks > 0) __syncthreads();
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const long unit = (long)bh * a.K + chunk;
-        __syncthreads();                                     // the chunk before has been read
-        next.park(kS, qS, triS, gates, tid);
-        __syncthreads();
-        f32x4 rest[kTiles];
+        const size_t row0 = seq + (size_t)chunk * C;
+        const int left = len - chunk * C;
+        const Chunked<T, D> &in = buffers[chunk & 1];
+        const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
+        const auto rows = [&](const uint16_t *mat, int s, Parts<P> (&f)[kTiles]) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) rest[t] = v[t];
-        if (chunk + 1 < chunks) {
-            next.load(a, unit + 1, seq + (size_t)(chunk + 1) * C, len - (chunk + 1) * C, hk, h, tid);
-            load_values(chunk + 1);
-        }
-        if (!mine) continue;
-        if (a.state != nullptr) store_state<D>(a.state + (size_t)unit * D * a.M + m, a.M, g, S);
-        f32x4 ks[kTiles], qs[kTiles];
+            for (int t = 0; t < kTiles; ++t) f[t] = row_operand<D, P>(mat, C * D, paired(t, c), 4 * s + g);
+        };
+        f32x4 ks[kTiles], qs[kTiles], rest[kTiles], since[kTiles], strength[kTiles];
+        Raw4<P> v[kTiles];
+        Parts<P> f[2][kTiles];
+        // K S; what comes with it is on its way meanwhile
+        rows(in.k, 0, f[0]);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) ks[t] = qs[t] = f32x4{0, 0, 0, 0};
+        if constexpr (kKeep) store_state<D>(a.state + (size_t)unit * D * a.M, m - c, a.M, lane, S);
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const Parts<3> x = cut(S[2 * s], S[2 * s + 1]);
+        for (int s = 0; s < kSteps; ++s) {
+            if (s + 1 < kSteps) rows(in.k, s + 1, f[(s + 1) % 2]);
+            else {
+                rows(in.q, 0, f[kSteps % 2]);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                ks[t] = product(row_operand<D, P>(kS, C * D, paired(t, c), 4 * s + g), x, ks[t]);
-                qs[t] = product(row_operand<D, P>(qS, C * D, paired(t, c), 4 * s + g), x, qs[t]);
-            }
-        }
-        const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(gates + which * C + paired(t, 4 * g)); };
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) rest[t] -= gate4(0, t) * ks[t];
-        Parts<3> x[kBlocks];
-#pragma unroll
-        for (int s = 0; s < kBlocks; ++s)
-            x[s] = cut(finite(gate4(2, 2 * s) * rest[2 * s]), finite(gate4(2, 2 * s + 1) * rest[2 * s + 1]));
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            f32x4 y = {0, 0, 0, 0};
-#pragma unroll
-            for (int s = 0; s <= t / 2; ++s)
-                y = product(row_operand<32, 3>(zS, Ch::kTri, tri_row<C>(paired(t, c), s), g), x[s], y);
-            rest[t] -= y;                                    // what the tokens find missing
-        }
-        if (a.miss != nullptr) {
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) a.miss[((size_t)unit * C + paired(t, 4 * g + r)) * a.M + m] = rest[t][r];
-        }
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) rest[t] = gate4(2, t) * rest[t];
-        if (a.o != nullptr) {
-#pragma unroll
-            for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(rest[2 * s]), finite(rest[2 * s + 1]));
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                f32x4 y = gate4(0, t) * qs[t];
-#pragma unroll
-                for (int s = 0; s <= t / 2; ++s)
-                    y = product(row_operand<32, 3>(mS, Ch::kTri, tri_row<C>(paired(t, c), s), g), x[s], y);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int n = chunk * C + paired(t, 4 * g + r);
-                    if (n < a.N) store_elem<false>((T *)a.o + (seq + n) * ldo + (size_t)h * a.M + m, n < len ? a.scale * y[r] : 0.0f);
+                for (int t = 0; t < kTiles; ++t) {
+                    v[t] = column_values<kCols, P>(in.v, C * kCols, paired(t, 4 * g), wave, lane);
+                    since[t] = gate4(0, t), strength[t] = gate4(2, t);
                 }
             }
+            in_this_order();
+            products(f[s % 2], sp[s], ks);
+        }
+        in_this_order();
+        // Q S beside what the tokens miss of the state before the chunk
+        Parts<3> x[kBlocks], zf[kTiles][kBlocks];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) rest[t] = v[t].sum() - since[t] * ks[t];
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(strength[2 * s] * rest[2 * s]), finite(strength[2 * s + 1] * rest[2 * s + 1]));
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s + 1 < kSteps) rows(in.q, s + 1, f[(kSteps + s + 1) % 2]);
+            products(f[(kSteps + s) % 2], first<kOut>(sp[s]), qs);
+        }
+        side_by_side<kSteps * kTiles * (P == 1 ? 2 : 6)>();
+        in_this_order();
+        // ... and of what the chunk's earlier tokens write
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+            for (int t = 2 * i; t < kTiles; ++t) zf[t][i] = row_operand<32, 3>(in.z, Ch::kTri, tri_row<C>(paired(t, c), i), g);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) ks[t] = f32x4{0, 0, 0, 0};
+        lower_products<2>(zf, x, ks);
+        in_this_order();
+        Parts<kOut> mf[kTiles][kBlocks], u[kBlocks];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            qs[t] *= since[t];
+#pragma unroll
+            for (int i = 0; i <= t / 2; ++i) mf[t][i] = row_operand<32, kOut>(in.m, Ch::kTri, tri_row<C>(paired(t, c), i), g);
+            since[t] = gate4(1, t);
         }
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s)
-            x[s] = cut(finite(gate4(1, 2 * s) * rest[2 * s]), finite(gate4(1, 2 * s + 1) * rest[2 * s + 1]));
-        const float whole = gates[C - 1];
+        for (int t = 0; t < kTiles; ++t) rest[t] -= ks[t];
+        if constexpr (kKeep) {
+            const Range r = range_of(a.miss + (size_t)unit * C * a.M, C, a.M, a.M);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
-            S[t] *= whole;
-#pragma unroll
-            for (int s = 0; s < kBlocks; ++s) S[t] = product(column_operand<D, true, P>(kS, C * D, 32 * s, t, lane), x[s], S[t]);
+            for (int t = 0; t < kTiles; ++t) store_tile<float>(r, paired(t, 4 * g), m - c, a.M, rest[t], lane);
         }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) rest[t] = finite(strength[t] * rest[t]);
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) u[s] = cut_to<kOut>(rest[2 * s], rest[2 * s + 1]);
+        constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;      // tiles of the state at a time
+        Parts<P> kt[2][kGroup];
+        const auto columns = [&](int n) {                    // n counts (group, block)
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) kt[n % 2][t] = column_operand<D, true, P>(in.k, C * D, 32 * (n % kBlocks), n / kBlocks * kGroup + t, lane);
+        };
+        in_this_order();
+        columns(0);
+        lower_products<kOut - 1>(mf, u, qs);
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(since[2 * s] * rest[2 * s]), finite(since[2 * s + 1] * rest[2 * s + 1]));
+        const float whole = in.gates[C - 1];
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) S[t] *= whole;
+        side_by_side<(kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
+        in_this_order();
+        const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, a.o == nullptr ? 0 : left < C ? left : C, ldo, a.M);
+#pragma unroll
+        for (int n = 0; n < kGroups * kBlocks; ++n) {
+            if (n + 1 < kGroups * kBlocks) columns(n + 1);
+            f32x4 part[kGroup];
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) part[t] = S[n / kBlocks * kGroup + t];
+            products(kt[n % 2], x[n % kBlocks], part);
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) S[n / kBlocks * kGroup + t] = part[t];
+            if (n == 0) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) store_tile<T>(r, paired(t, 4 * g), m - c, ldo, a.scale * qs[t], lane);
+            }
+            if (n % kBlocks == 0 && n > 0) {                 // the group before is complete
+#pragma unroll
+                for (int s = 0; s < kGroup / 2; ++s) {
+                    const int i = (n / kBlocks - 1) * kGroup / 2 + s;
+                    sp[i] = cut(S[2 * i], S[2 * i + 1]);
+                }
+            }
+            if (n == 0 || n % kBlocks == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order();
+        }
+#pragma unroll
+        for (int i = (kGroups - 1) * kGroup / 2; i < kSteps; ++i) sp[i] = cut(S[2 * i], S[2 * i + 1]);
+        __syncthreads();
     }
-    if (!mine) return;
-    if (a.h1 != nullptr) store_state<D>(a.h1 + state, a.M, g, S);
-    if (a.o != nullptr)
-        for (int n = chunks * C + g; n < a.N; n += 4) store_elem<false>((T *)a.o + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);
+    if (a.h1 != nullptr) store_state<D>(a.h1 + state, m - c, a.M, lane, S);
+    if (a.o != nullptr)                                      // tokens behind the sequence
+        for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.o + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);
 }
 
 // ---- one token ------------------------------------------------------------------------------------------
@@ -216,7 +261,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_fwd_ke
 template <typename T, int D> __global__ __launch_bounds__(256) void delta_step_kernel(const DeltaArgs a, float *h) {
     constexpr int kRows = D / 16;
     __shared__ f32x4 red[4][2][16];
-    __shared__ float dots[4];
+    __shared__ alignas(16) float dots[4];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, l = tid % 16, part = tid / 16;
     const int blocks = (a.M + kCols - 1) / kCols, bh = blockIdx.x / blocks, m = blockIdx.x % blocks * kCols + 4 * l;
     const int b = bh / a.H, head = bh % a.H, hk = head / (a.H / a.Hk);
@@ -267,7 +312,7 @@ hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
     const unsigned units = (unsigned)((long)a.B * a.H * a.K);
 #define LA_LOCAL(T, D) delta_local_kernel<T, D><<<units, 256, 0, s>>>(a)
     LA_BY_WIDTH(LA_LOCAL)
-#define LA_PASS(T, D) delta_fwd_kernel<T, D><<<head_grid(a), 256, 0, s>>>(a)
+#define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, true><<<head_grid(a), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, false><<<head_grid(a), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_PASS)
     return hipGetLastError();
 }

@@ -19,120 +19,146 @@
 namespace la {
 namespace {
 
-template <typename T, int D> __global__ __launch_bounds__(256) void delta_states_bwd_kernel(const DeltaArgs a) {
+// As the forward: 16 columns of dS' a wave; products that y does not wait for (Q^T e^G dO) run beside the cutting of values.
+template <typename T, int D> __global__ __launch_bounds__(512) void delta_states_bwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks;
-    __shared__ uint16_t kS[P * C * D], qS[P * C * D], triS[2 * 3 * Ch::kTri];
-    __shared__ float gates[3 * C];
-    const uint16_t *zS = triS, *mS = triS + 3 * Ch::kTri;
+    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kSteps = D / 32;
+    __shared__ Chunked<T, D> buffers[2];
     int bh, m0;
     if (!head_and_columns(a, bh, m0)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16, m = m0 + tid / kWave * 16 + c;
-    const bool mine = m < a.M;
-    const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk), len = length_of(a, b), chunks = (len + C - 1) / C;
-    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M + m, ldo = (size_t)a.H * a.M;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, m = m0 + wave * 16 + c;
+    const int b = bh / a.H, h = bh % a.H, len = length_of(a, b), chunks = (len + C - 1) / C;
+    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, ldo = a.H * a.M;
+    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M;
+    if (wave >= 4) {
+        fetch_chunks<T, D>(buffers, a, bh, len, chunks - 1, -1, chunks, (const T *)a.dO + (size_t)h * a.M + m0, ldo, cols, tid - 256);
+        return;
+    }
+    if (wave * 16 >= cols) {
+        if (chunks > 0) __syncthreads();
+        for (int chunk = 0; chunk < chunks; ++chunk) __syncthreads();
+        return;
+    }
     f32x4 S[D / 16];                                         // dS'
-    load_state<D>(a.dh1 == nullptr || !mine ? nullptr : a.dh1 + state, a.M, g, S);
-    Fetch<T, D> next;
-    f32x4 v[kTiles];
-    const auto load_values = [&](int chunk) {
+    load_state<D>(a.dh1 == nullptr ? nullptr : a.dh1 + state, m, a.M, g, S);
+    loads_done();
+    Parts<3> sp[kSteps];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = chunk * C + paired(t, 4 * g + r);
-                v[t][r] = mine && n < len ? raw_to_f32((const T *)a.dO + (seq + n) * ldo + (size_t)h * a.M + m) : 0.0f;
-            }
-    };
-    const auto load = [&](int chunk) {
-        next.load(a, (long)bh * a.K + chunk, seq + (size_t)chunk * C, len - chunk * C, hk, h, tid);
-        load_values(chunk);
-    };
-    if (mine)                                                // tokens behind the sequence
-        for (int n = chunks * C + g; n < a.N; n += 4) store_elem<false>((T *)a.dv + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);
-    if (chunks > 0) load(chunks - 1);
-    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    for (int s = 0; s < kSteps; ++s) sp[s] = cut(S[2 * s], S[2 * s + 1]);
+    for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.dv + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);      // tokens behind the sequence
+    if (chunks > 0) __syncthreads();
+    for (int i = 0; i < chunks; ++i) {
+        const int chunk = chunks - 1 - i, left = len - chunk * C;
         const long unit = (long)bh * a.K + chunk;
-        __syncthreads();
-        next.park(kS, qS, triS, gates, tid);
-        __syncthreads();
-        f32x4 out[kTiles];
+        const Chunked<T, D> &in = buffers[i & 1];
+        const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
+        f32x4 y[kTiles], w[kTiles];
+        Parts<P> f[2][kTiles], o[kBlocks];
+        Raw4<P> out[kTiles];
+        const auto rows = [&](int s) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) out[t] = v[t];
-        if (chunk > 0) load(chunk - 1);
-        if (!mine) continue;
-        store_state<D>(a.dstate + (size_t)unit * D * a.M + m, a.M, g, S);
-        const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(gates + which * C + paired(t, 4 * g)); };
-        f32x4 y[kTiles];
+            for (int t = 0; t < kTiles; ++t) f[s % 2][t] = row_operand<D, P>(in.k, C * D, paired(t, c), 4 * s + g);
+        };
+        // a block column's tiles of a transposed chunk-local matrix
+        const auto upper = [&](const uint16_t *mat, Parts<3> (&tri)[kTiles][kBlocks]) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) y[t] = f32x4{0, 0, 0, 0};
+            for (int s = 0; s < kBlocks; ++s)
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const Parts<3> x = cut(S[2 * s], S[2 * s + 1]);
+                for (int t = 0; t < 2 * (s + 1); ++t) tri[t][s] = column_operand<32, true, 3>(mat, Ch::kTri, tri_row<C>(32 * s, t / 2), t % 2, lane);
+        };
+        Parts<3> tri[kTiles][kBlocks];
+        rows(0);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) y[t] = product(row_operand<D, P>(kS, C * D, paired(t, c), 4 * s + g), x, y[t]);
-        }
-        Parts<3> x[kBlocks];
+        for (int t = 0; t < kTiles; ++t) y[t] = w[t] = f32x4{0, 0, 0, 0};
+        store_state<D>(a.dstate + (size_t)unit * D * a.M, m - c, a.M, lane, S);
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s) x[s] = cut(out[2 * s], out[2 * s + 1]);        // bf16: the lower parts are zeros
+        for (int s = 0; s < kSteps; ++s) {
+            if (s + 1 < kSteps) rows(s + 1);
+            else {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            f32x4 w = {0, 0, 0, 0};
-#pragma unroll
-            for (int s = t / 2; s < kBlocks; ++s) {
-                const Parts<3> mt = column_operand<32, true, 3>(mS, Ch::kTri, tri_row<C>(32 * s, t / 2), t % 2, lane);
-                if constexpr (P == 1) w = product(mt, Parts<1>{{x[s].p[0]}}, w);
-                else w = product(mt, x[s], w);
+                for (int x = 0; x < kBlocks; ++x) o[x] = column_operand<kCols, false, P>(in.v, C * kCols, 32 * x, wave, lane);
+                upper(in.m, tri);
             }
-            y[t] = a.scale * w + gate4(1, t) * y[t];
+            in_this_order();
+            products(f[s % 2], sp[s], y);
         }
+        in_this_order();
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s) x[s] = cut(gate4(2, 2 * s) * y[2 * s], gate4(2, 2 * s + 1) * y[2 * s + 1]);
+        for (int t = 0; t < kTiles; ++t) out[t] = column_values<kCols, P>(in.v, C * kCols, paired(t, 4 * g), wave, lane);
+        upper_products<2>(tri, o, w);
+        in_this_order();
+        // dU, and beside it the state's share of the outputs
+        constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;
+        Parts<P> kt[2][kGroup];
+        const auto columns = [&](const uint16_t *mat, int n) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            f32x4 w = {0, 0, 0, 0};
+            for (int t = 0; t < kGroup; ++t) kt[n % 2][t] = column_operand<D, true, P>(mat, C * D, 32 * (n % kBlocks), n / kBlocks * kGroup + t, lane);
+        };
+        const float whole = in.gates[C - 1];
+        Parts<3> x[kBlocks], z[kBlocks];
 #pragma unroll
-            for (int s = t / 2; s < kBlocks; ++s)
-                w = product(column_operand<32, true, 3>(zS, Ch::kTri, tri_row<C>(32 * s, t / 2), t % 2, lane), x[s], w);
-            y[t] -= w;
-        }
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) a.write[((size_t)unit * C + paired(t, 4 * g + r)) * a.M + m] = y[t][r];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            y[t] = gate4(2, t) * y[t];                       // dV
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = chunk * C + paired(t, 4 * g + r);
-                if (n < a.N) store_elem<false>((T *)a.dv + (seq + n) * ldo + (size_t)h * a.M + m, n < len ? y[t][r] : 0.0f);
-            }
-        }
-        const float whole = gates[C - 1];
+        for (int s = 0; s < kBlocks; ++s)
+            x[s] = cut(a.scale * gate4(0, 2 * s) * out[2 * s].sum(), a.scale * gate4(0, 2 * s + 1) * out[2 * s + 1].sum());
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) S[t] *= whole;
+        columns(in.q, 0);
+        in_this_order();
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s) {
-            const Parts<3> o = cut(a.scale * gate4(0, 2 * s) * out[2 * s], a.scale * gate4(0, 2 * s + 1) * out[2 * s + 1]);
-            const Parts<3> w = cut(-gate4(0, 2 * s) * y[2 * s], -gate4(0, 2 * s + 1) * y[2 * s + 1]);
+        for (int t = 0; t < kTiles; ++t) y[t] = a.scale * w[t] + gate4(1, t) * y[t], w[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) {
-                S[t] = product(column_operand<D, true, P>(qS, C * D, 32 * s, t, lane), o, S[t]);
-                S[t] = product(column_operand<D, true, P>(kS, C * D, 32 * s, t, lane), w, S[t]);
-            }
+        for (int s = 0; s < kBlocks; ++s) z[s] = cut(gate4(2, 2 * s) * y[2 * s], gate4(2, 2 * s + 1) * y[2 * s + 1]);
+        const auto update = [&](int n, const Parts<3> &by) {
+            f32x4 part[kGroup];
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) part[t] = S[n / kBlocks * kGroup + t];
+            products(kt[n % 2], by, part);
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) S[n / kBlocks * kGroup + t] = part[t];
+        };
+#pragma unroll
+        for (int n = 0; n < kGroups * kBlocks; ++n) {
+            if (n + 1 < kGroups * kBlocks) columns(in.q, n + 1);
+            update(n, x[n % kBlocks]);
+            if (n == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order();
         }
-    }
-    if (mine && a.dh0 != nullptr) store_state<D>(a.dh0 + state, a.M, g, S);
-}
-
-// Lower parts of a column operand added up again: rows 4g .. + 3 of tile `rows`, column of this lane, in fp32.
-template <int COLS, int P> __device__ __forceinline__ f32x4 column_values(const uint16_t *m, int plane, int rows, int tile, int lane) {
-    const int q = lane & 15, r = 16 * rows + 4 * (lane >> 4) + (q >> 2), piece = 2 * tile + ((q >> 1) & 1), half = 4 * (q & 1);
-    f32x4 v = {0, 0, 0, 0};
+        upper(in.z, tri);
+        upper_products<2>(tri, z, w);
+        columns(in.k, 0);
+        in_this_order();
+        const Range wr = range_of(a.write + (size_t)unit * C * a.M, C, a.M, a.M);
+        const Range vr = range_of((T *)a.dv + (seq + (size_t)chunk * C) * ldo + (size_t)h * a.M, left < C ? left : C, ldo, a.M);
 #pragma unroll
-    for (int i = P - 1; i >= 0; --i) v += widen(read_column(m + i * plane + mat_at<COLS>(r, piece) + half));
-    return v;
+        for (int t = 0; t < kTiles; ++t) y[t] -= w[t], w[t] = gate4(2, t) * y[t];       // w: dV
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) x[s] = cut(-gate4(0, 2 * s) * w[2 * s], -gate4(0, 2 * s + 1) * w[2 * s + 1]);
+        in_this_order();
+#pragma unroll
+        for (int n = 0; n < kGroups * kBlocks; ++n) {
+            if (n + 1 < kGroups * kBlocks) columns(in.k, n + 1);
+            update(n, x[n % kBlocks]);
+            if (n == 0) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    store_tile<float>(wr, paired(t, 4 * g), m - c, a.M, y[t], lane);
+                    store_tile<T>(vr, paired(t, 4 * g), m - c, ldo, w[t], lane);
+                }
+            }
+            if (n % kBlocks == 0 && n > 0) {                 // the group before is complete
+#pragma unroll
+                for (int s = 0; s < kGroup / 2; ++s) {
+                    const int j = (n / kBlocks - 1) * kGroup / 2 + s;
+                    sp[j] = cut(S[2 * j], S[2 * j + 1]);
+                }
+            }
+            if (n % kBlocks == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order();
+        }
+#pragma unroll
+        for (int j = (kGroups - 1) * kGroup / 2; j < kSteps; ++j) sp[j] = cut(S[2 * j], S[2 * j + 1]);
+        __syncthreads();
+    }
+    if (a.dh0 != nullptr) store_state<D>(a.dh0 + state, m - c, a.M, lane, S);
 }
 
 // A workgroup takes one chunk and the heads that share its queries and keys, one after the other, D / 16 waves with 16
@@ -142,8 +168,8 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kWaves = D / 16, kThreads = 4 * D;
     constexpr int kLow = kTiles * (kTiles + 1) / 2, kLowEach = (kLow + kWaves - 1) / kWaves;
     constexpr int kStage = (6 + P) * C * kCols, kSquares = 6 * C * C, kWork = kStage > kSquares ? kStage : kSquares;
-    __shared__ uint16_t kS[P * C * D], qS[P * C * D], work[kWork];
-    __shared__ float gates[4 * C], bt[C], miss[C], db[C], red[kWaves][C], ends[kWaves];
+    __shared__ alignas(16) uint16_t kS[P * C * D], qS[P * C * D], work[kWork];
+    __shared__ alignas(16) float gates[4 * C], bt[C], miss[C], db[C], red[kWaves][C], ends[kWaves];
     uint16_t *uS = work, *wS = work + 3 * C * kCols, *oS = work + 6 * C * kCols;          // U, dV, dO
     uint16_t *pS = work, *bS = work + 3 * C * C;                                            // P, B + B^T
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, d = 16 * wave + c;
@@ -156,8 +182,8 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
     if (left > 0) {
         for (int i = tid; i < C * D / 8; i += kThreads) {
             const int t = i / (D / 8), piece = i % (D / 8);
-            park_eight<T>(kS + mat_at<D>(t, piece), C * D, load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, t < left));
-            park_eight<T>(qS + mat_at<D>(t, piece), C * D, load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, t < left));
+            park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, t < left));
+            park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, t < left));
         }
         for (int h = hk * per; h < (hk + 1) * per; ++h) {
             const long unit = (long)(b * a.H + h) * a.K + chunk;
@@ -186,7 +212,7 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
                         dots = fmaf(w[e], vs.get(e) - us.get(e), dots);
                         dbs = fmaf(ys.get(e), us.get(e), dbs);
                     }
-                    const int at = mat_at<kCols>(t, piece);
+                    const int at = mat_at<kCols, true>(t, piece);
                     park_eight(uS + at, C * kCols, u);
                     park_eight(wS + at, C * kCols, w);
                     park_eight<T>(oS + at, C * kCols, os);
@@ -204,9 +230,9 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
                     while (n > ct) n -= ++ct;                // n-th tile s of column tile t = ct
 #pragma unroll
                     for (int s = 0; s < kCols / 32; ++s) {
-                        const Parts<3> u = row_operand<kCols, 3>(uS, C * kCols, 16 * n + c, 4 * s + g);
-                        p[i] = product(u, row_operand<kCols, P>(oS, C * kCols, 16 * ct + c, 4 * s + g), p[i]);
-                        bb[i] = product(u, row_operand<kCols, 3>(wS, C * kCols, 16 * ct + c, 4 * s + g), bb[i]);
+                        const Parts<3> u = row_operand<kCols, 3, true>(uS, C * kCols, 16 * n + c, 4 * s + g);
+                        p[i] = product(u, row_operand<kCols, P, true>(oS, C * kCols, 16 * ct + c, 4 * s + g), p[i]);
+                        bb[i] = product(u, row_operand<kCols, 3, true>(wS, C * kCols, 16 * ct + c, 4 * s + g), bb[i]);
                     }
                 }
 #pragma unroll
@@ -220,9 +246,9 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
                     const Parts<3> x1 = cut(f32x4{s1.get(0), s1.get(1), s1.get(2), s1.get(3)}, f32x4{s1.get(4), s1.get(5), s1.get(6), s1.get(7)});
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t) {
-                        q1[t] = product(row_operand<kCols, P>(oS, C * kCols, 16 * t + c, 4 * s + g), x0, q1[t]);
-                        k1[t] = product(row_operand<kCols, 3>(wS, C * kCols, 16 * t + c, 4 * s + g), x0, k1[t]);
-                        k2[t] = product(row_operand<kCols, 3>(uS, C * kCols, 16 * t + c, 4 * s + g), x1, k2[t]);
+                        q1[t] = product(row_operand<kCols, P, true>(oS, C * kCols, 16 * t + c, 4 * s + g), x0, q1[t]);
+                        k1[t] = product(row_operand<kCols, 3, true>(wS, C * kCols, 16 * t + c, 4 * s + g), x0, k1[t]);
+                        k2[t] = product(row_operand<kCols, 3, true>(uS, C * kCols, 16 * t + c, 4 * s + g), x1, k2[t]);
                     }
                 }
             }
@@ -243,7 +269,7 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
                 const float pq[4] = {pv[0], pv[1], pv[2], pv[3]}, bq[4] = {bv[0], bv[1], bv[2], bv[3]};
                 const Split3 ps = split3(pq), bs = split3(bq);
                 const u32x2_t parts[2][3] = {{ps.h, ps.m, ps.l}, {bs.h, bs.m, bs.l}};
-                const int here = mat_at<C>(t, s / 8) + s % 8;
+                const int here = mat_at<C, true>(t, s / 8) + s % 8;
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {
                     *reinterpret_cast<u32x2_t *>(pS + k * C * C + here) = parts[0][k];
@@ -251,16 +277,16 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const uint16_t e = (uint16_t)(parts[1][k][r / 2] >> (16 * (r & 1)));
-                            if (s + r <= t) bS[k * C * C + here + r] = bS[k * C * C + mat_at<C>(s + r, t / 8) + t % 8] = e;
+                            if (s + r <= t) bS[k * C * C + here + r] = bS[k * C * C + mat_at<C, true>(s + r, t / 8) + t % 8] = e;
                         }
                     } else {
                         *reinterpret_cast<u32x2_t *>(bS + k * C * C + here) = parts[1][k];
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            bS[k * C * C + mat_at<C>(s + r, t / 8) + t % 8] = (uint16_t)(parts[1][k][r / 2] >> (16 * (r & 1)));
+                            bS[k * C * C + mat_at<C, true>(s + r, t / 8) + t % 8] = (uint16_t)(parts[1][k][r / 2] >> (16 * (r & 1)));
                     }
                     // the tile right above the diagonal, which products over 32 tokens read
-                    if (n == ct && ct % 2 == 0) *reinterpret_cast<u32x2_t *>(pS + k * C * C + mat_at<C>(t, (s + 16) / 8) + s % 8) = u32x2_t{0, 0};
+                    if (n == ct && ct % 2 == 0) *reinterpret_cast<u32x2_t *>(pS + k * C * C + mat_at<C, true>(t, (s + 16) / 8) + s % 8) = u32x2_t{0, 0};
                 }
             }
             __syncthreads();
@@ -275,14 +301,14 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
                 kd = k2[t] - eg * k1[t];
 #pragma unroll
                 for (int s = 0; s < kBlocks; ++s) {
-                    const Parts<P> kx = column_operand<D, false, P>(kS, C * D, 32 * s, wave, lane);
-                    if (s <= t / 2) qd = product(row_operand<C, 3>(pS, C * C, 16 * t + c, 4 * s + g), kx, qd);
+                    const Parts<P> kx = column_operand<D, false, P, true>(kS, C * D, 32 * s, wave, lane);
+                    if (s <= t / 2) qd = product(row_operand<C, 3, true>(pS, C * C, 16 * t + c, 4 * s + g), kx, qd);
                     if (s >= t / 2)
-                        kd = product(column_operand<C, false, 3>(pS, C * C, 32 * s, t, lane), column_operand<D, false, P>(qS, C * D, 32 * s, wave, lane), kd);
-                    kd = product(row_operand<C, 3>(bS, C * C, 16 * t + c, 4 * s + g), kx, kd);
+                        kd = product(column_operand<C, false, 3, true>(pS, C * C, 32 * s, t, lane), column_operand<D, false, P, true>(qS, C * D, 32 * s, wave, lane), kd);
+                    kd = product(row_operand<C, 3, true>(bS, C * C, 16 * t + c, 4 * s + g), kx, kd);
                 }
                 dq[t] += qd, dk[t] += kd;
-                const f32x4 qv = column_values<D, P>(qS, C * D, t, wave, lane), kv = column_values<D, P>(kS, C * D, t, wave, lane);
+                const f32x4 qv = column_values<D, P, true>(qS, C * D, 16 * t + 4 * g, wave, lane).sum(), kv = column_values<D, P, true>(kS, C * D, 16 * t + 4 * g, wave, lane).sum();
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     into = fmaf(kv[r], k2[t][r], into);
@@ -338,7 +364,7 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
 }  // namespace
 
 hipError_t launch_delta_bwd(const DeltaArgs &a, int dtype, hipStream_t s) {
-#define LA_STATES(T, D) delta_states_bwd_kernel<T, D><<<head_grid(a), 256, 0, s>>>(a)
+#define LA_STATES(T, D) delta_states_bwd_kernel<T, D><<<head_grid(a), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_STATES)
     const unsigned units = (unsigned)((long)a.B * a.Hk * a.K);
 #define LA_CHUNKS(T, D) delta_chunks_bwd_kernel<T, D><<<units, 4 * D, 0, s>>>(a)

@@ -17,6 +17,7 @@ template <typename... Ps> bool any_null(Ps... p) { return ((p == nullptr) || ...
 
 constexpr int kMostInt = 1 << 30;                            // tokens are counted in int, a chunk ahead of the last one
 constexpr double kMostElements = 68719476736.0;              // 2^36
+constexpr int kMostApart = 1 << 23;                          // elements between tokens: a chunk is addressed with 31 bits of bytes
 constexpr double kMostUnits = 8388608.0;                     // 2^23 workgroups of up to 512 threads are one launch
 
 // ---- head norm and rotation -------------------------------------------------------------------------
@@ -44,10 +45,11 @@ int delta_sizes(int B, int N, int H, int Hk, int D, int M, la_dtype t, int flags
     if (B < 1 || N < 1 || H < 1 || Hk < 1 || D < 1 || M < 1 || H % Hk != 0 || N > kMostInt) return LA_ERR_SHAPE;
     if (!(D == 32 || D == 64 || D == 128) || M % 16 != 0 || M > 512) return LA_ERR_UNSUPPORTED;
     const int C = la::delta_chunk(t);
-    if ((double)H * M > kMostInt || (double)Hk * D > kMostInt || (double)B * N * H * (M > D ? M : D) >= kMostElements) return LA_ERR_SHAPE;
+    if ((double)H * M > kMostApart || (double)Hk * D > kMostApart || (double)B * N * H * (M > D ? M : D) >= kMostElements) return LA_ERR_SHAPE;
     if (((double)B * H + 8) * ((N + (double)C - 1) / C) >= kMostUnits || ((double)B * H + 8) * ((M + 63) / 64) >= kMostUnits) return LA_ERR_SHAPE;
     return LA_OK;
 }
+bool bad_apart(int ld, int width) { return ld < width || ld > kMostApart; }
 struct Delta {
     la::DeltaArgs a{};
     size_t tri, gate, rows, state;
@@ -131,8 +133,8 @@ int la_delta_fwd(const void *q, int ldq, const void *k, int ldk, const void *v, 
     if (any_null(q, k, v, beta, o)) return LA_ERR_NULL;
     const int st = delta_sizes(B, N, H, Hk, D, M, t, flags);
     if (st != LA_OK) return st;
-    if (!isfinite(scale) || ldq < Hk * D || ldk < Hk * D || ldv < H * M) return LA_ERR_SHAPE;
-    if (any_misaligned(q, k, v, g, beta, h0, lengths, o, h1, ws)) return LA_ERR_ALIGN;
+    if (!isfinite(scale) || bad_apart(ldq, Hk * D) || bad_apart(ldk, Hk * D) || bad_apart(ldv, H * M)) return LA_ERR_SHAPE;
+    if (any_misaligned(q, k, v, g, beta, h0, lengths, o, h1, ws) || (ldq | ldk | ldv) % 8 != 0) return LA_ERR_ALIGN;
     Delta d(B, N, H, Hk, D, M, scale, t);
     const bool keep = (flags & LA_DELTA_KEEP) != 0;
     const size_t need = d.fwd_bytes(keep);
@@ -162,8 +164,8 @@ int la_delta_bwd(const void *q, int ldq, const void *k, int ldk, const void *v, 
     if (any_null(q, k, v, beta, dO, dq, dk, dv, dbeta) || (g == nullptr) != (dg == nullptr)) return LA_ERR_NULL;
     const int st = delta_sizes(B, N, H, Hk, D, M, t, flags);
     if (st != LA_OK) return st;
-    if (!isfinite(scale) || ldq < Hk * D || ldk < Hk * D || ldv < H * M || ((flags & LA_DELTA_KEEP) != 0) != (fwd_ws != nullptr)) return LA_ERR_SHAPE;
-    if (any_misaligned(q, k, v, g, beta, h0, lengths, fwd_ws, dO, dh1, dq, dk, dv, dg, dbeta, dh0, ws)) return LA_ERR_ALIGN;
+    if (!isfinite(scale) || bad_apart(ldq, Hk * D) || bad_apart(ldk, Hk * D) || bad_apart(ldv, H * M) || ((flags & LA_DELTA_KEEP) != 0) != (fwd_ws != nullptr)) return LA_ERR_SHAPE;
+    if (any_misaligned(q, k, v, g, beta, h0, lengths, fwd_ws, dO, dh1, dq, dk, dv, dg, dbeta, dh0, ws) || (ldq | ldk | ldv) % 8 != 0) return LA_ERR_ALIGN;
     Delta d(B, N, H, Hk, D, M, scale, t);
     const bool given = fwd_ws != nullptr;
     const size_t need = d.bwd_bytes(given);
