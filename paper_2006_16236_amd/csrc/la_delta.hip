@@ -19,34 +19,59 @@ namespace la {
 namespace {
 
 // ---- chunk-local matrices ------------------------------------------------------------------------
-// One workgroup a unit: decays, masked products of queries and keys, and the triangular system, column j of Z in lane j.
+// One workgroup a unit: decays, masked products of queries and keys, and the triangular system by blocks of 16.  The inverse
+// t = (1 + A beta)^-1 of the diagonal blocks comes by substitution, one block in each lane group and one column a lane, the
+// blocks below it from those above, t_ij = -t_ii sum_k (A beta)_ik t_kj, a diagonal at a time, and Z = t A.  All in fp32
+// (v_mfma_f32_16x16x4: lane (c, g) supplies elements 4g + q of its row c, register q of a result is that of the next operand).
+// One wave with a column of Z a lane, 2016 dependent steps, took 25 us instead of @SMALL@ for one chunk of 64 sequences.
+constexpr int kTriStride = 68;                               // floats between rows: 16 rows' 16-byte reads meet all banks
+__device__ __forceinline__ f32x4 times(f32x4 rows, f32x4 columns, f32x4 acc) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc = mfma16(rows[q], columns[q], acc);
+    return acc;
+}
+// block (i, j) of a matrix as the left operand, and as the right one
+__device__ __forceinline__ f32x4 block_rows(const float *m, int i, int j, int c, int g) {
+    return *reinterpret_cast<const f32x4 *>(m + (16 * i + c) * kTriStride + 16 * j + 4 * g);
+}
+__device__ __forceinline__ f32x4 block_columns(const float *m, int i, int j, int c, int g) {
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = m[(16 * i + 4 * g + q) * kTriStride + 16 * j + c];
+    return v;
+}
 template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kRow = C + 4;
-    __shared__ alignas(16) uint16_t kS[P * C * D], qS[P * C * D];
-    __shared__ alignas(16) float low[C * kRow];                          // A, strictly lower
+    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kTokens = 2 * P * C * D * (int)sizeof(uint16_t), kTri = C * kTriStride * (int)sizeof(float);
+    __shared__ alignas(16) char space[kTokens > kTri ? kTokens : kTri];
+    __shared__ alignas(16) float low[C * kTriStride];        // A, zeros on the diagonal and above
     __shared__ alignas(16) float gh[C], gl[C], bt[C];
+    uint16_t *kS = reinterpret_cast<uint16_t *>(space), *qS = kS + P * C * D;
+    float *inv = reinterpret_cast<float *>(space);           // takes their place
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16;
     const long unit = blockIdx.x;
     const int chunk = (int)(unit % a.K), bh = (int)(unit / a.K), b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
-    const int len = length_of(a, b), t0 = chunk * C;
-    if (t0 >= len) return;                                   // no later launch reads this unit
+    const int len = length_of(a, b), t0 = chunk * C, left = len - t0;
+    if (left <= 0) return;                                   // no later launch reads this unit
     const size_t row0 = (size_t)b * a.N + t0;
-    for (int i = tid; i < C * D / 8; i += 256) {
-        const int t = i / (D / 8), piece = i % (D / 8);
-        const bool live = t0 + t < len;
-        const Eight<T> k = load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, live);
-        const Eight<T> q = load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, live);
-        park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, k);
-        park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, q);
+    const Range kr = range_of((const T *)a.k + row0 * a.ldk + (size_t)hk * D, left < C ? left : C, a.ldk, D);
+    const Range qr = range_of((const T *)a.q + row0 * a.ldq + (size_t)hk * D, left < C ? left : C, a.ldq, D);
+    const size_t at = (row0 + lane) * a.H + h;
+    const bool live = wave == 0 && lane < C && lane < left;
+    const float gate_in = live && a.g != nullptr ? a.g[at] : 0.0f, beta_in = live ? a.beta[at] : 0.0f;
+    constexpr int kEach = (C * D / 8 + 255) / 256;
+    Eight<T> kq[kEach][2];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
+        kq[j][0] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * (int)sizeof(T));
+        kq[j][1] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * (int)sizeof(T));
     }
     float *gate = a.gate + unit * 4 * C;
     if (wave == 0) {
-        const bool live = lane < C && t0 + lane < len;
-        const size_t at = (row0 + lane) * a.H + h;
         // sums of many small logarithms, and differences of such sums: fp64, kept as two fp32.  Below -1000 a factor is zero
         // either way, and sums stay finite (a decay to nothing is g = -inf).
-        double sum = live && a.g != nullptr ? (double)fmaxf(a.g[at], -1000.0f) : 0.0;
+        double sum = (double)fmaxf(gate_in, -1000.0f);
 #pragma unroll
         for (int d = 1; d < C; d *= 2) {
             const double from = __shfl_up(sum, d);
@@ -55,15 +80,22 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         const double whole = __shfl(sum, C - 1);
         if (lane < C) {
             const float hi = (float)sum, lo = (float)(sum - (double)hi);
-            gh[lane] = hi, gl[lane] = lo, bt[lane] = live ? a.beta[at] : 0.0f;
+            gh[lane] = hi, gl[lane] = lo, bt[lane] = beta_in;
             gate[lane] = expf(hi) * (1.0f + lo), gate[C + lane] = expf((float)(whole - sum));
             gate[2 * C + lane] = hi, gate[3 * C + lane] = lo;
         }
     }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
+        if (C * D / 8 % 256 != 0 && i >= C * D / 8) break;
+        park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, kq[j][0]);
+        park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, kq[j][1]);
+    }
     __syncthreads();
     float *zOut = a.tri + unit * 2 * Ch::kTri, *mOut = zOut + Ch::kTri;
-    for (int i = wave; i < Ch::kTiles * Ch::kTiles; i += 4) {            // tiles (rt, ct) of 16 x 16
-        const int rt = i / Ch::kTiles, ct = i % Ch::kTiles;
+    for (int i = wave; i < kTiles * kTiles; i += 4) {        // tiles (rt, ct) of 16 x 16, the diagonals dealt to all waves
+        const int rt = i / kTiles, ct = (i + rt) % kTiles;
         if (ct / 2 > rt / 2) continue;                       // a 32 x 32 block above the diagonal
         f32x4 kk = {0, 0, 0, 0}, qk = {0, 0, 0, 0};
         if (ct <= rt) {
@@ -79,29 +111,60 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         for (int r = 0; r < 4; ++r) {
             const int t = 16 * rt + 4 * g + r;
             const float decay = s <= t ? expf((gh[t] - gh[s]) + (gl[t] - gl[s])) : 0.0f;
-            if (ct <= rt) low[t * kRow + s] = s < t ? kk[r] * decay : 0.0f;
+            if (ct <= rt) low[t * kTriStride + s] = s < t ? kk[r] * decay : 0.0f;
             mOut[tri_row<C>(t, ct / 2) * 32 + s % 32] = s <= t ? qk[r] * decay : 0.0f;
         }
     }
-    __syncthreads();
-    if (wave != 0) return;
-    float z[C];
-    const int j = lane % C;
+    __syncthreads();                                         // K and Q make way for the inverse
+    if (wave == 0 && g < kTiles) {
+        float x[16], y[16];                                  // column c of block (g, g), and beta times it
 #pragma unroll
-    for (int r = 0; r < C; ++r) {
-        float x = j < r ? low[r * kRow + j] : 0.0f, y = 0.0f;
+        for (int r = 0; r < 16; ++r) {
+            float v = r == c ? 1.0f : 0.0f, u = 0.0f;
+            f32x4 f[4];
 #pragma unroll
-        for (int s = 0; s < r; ++s) {
-            const float f = low[r * kRow + s] * bt[s];
-            if (s % 2 == 0) x = fmaf(-f, z[s], x);
-            else y = fmaf(-f, z[s], y);
+            for (int q = 0; q < 4; ++q)
+                if (4 * q < r) f[q] = *reinterpret_cast<const f32x4 *>(low + (16 * g + r) * kTriStride + 16 * g + 4 * q);
+#pragma unroll
+            for (int s = 0; s < r; ++s) {
+                if (s % 2 == 0) v = fmaf(-f[s / 4][s % 4], y[s], v);
+                else u = fmaf(-f[s / 4][s % 4], y[s], u);
+            }
+            x[r] = v + u, y[r] = bt[16 * g + r] * x[r];
         }
-        z[r] = x + y;
-        if (lane < C && j / 32 <= r / 32) zOut[tri_row<C>(r, j / 32) * 32 + j % 32] = z[r];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) inv[(16 * g + r) * kTriStride + 16 * g + c] = x[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int d = 1; d < kTiles; ++d) {
+        const int i = d + wave, j = wave;
+        if (i < kTiles) {
+            f32x4 sum = {0, 0, 0, 0}, t = {0, 0, 0, 0};
+            for (int k = j; k < i; ++k)
+                sum = times(block_rows(low, i, k, c, g) * *reinterpret_cast<const f32x4 *>(bt + 16 * k + 4 * g), block_columns(inv, k, j, c, g), sum);
+            t = times(block_rows(inv, i, i, c, g), finite(sum), t);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) inv[(16 * i + 4 * g + r) * kTriStride + 16 * j + c] = -t[r];
+        }
+        __syncthreads();
+    }
+    // block (i, j) of Z is i - j + 1 products: 20 of them, five a wave (of 32 tokens 4, in three waves)
+    for (int n = 0; n < kTiles * kTiles; ++n) {
+        const int i = n / kTiles, j = n % kTiles;
+        constexpr int kOf4[16] = {0, -1, -1, -1, 1, 3, -1, -1, 2, 3, 3, -1, 0, 1, 2, 3};
+        if ((kTiles == 4 ? kOf4[n] : n == 1 ? -1 : n % 4) != wave) continue;
+        f32x4 z = {0, 0, 0, 0};
+        for (int k = j; k <= i; ++k) z = times(block_rows(inv, i, k, c, g), finite(block_columns(low, k, j, c, g)), z);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * i + 4 * g + r;
+            zOut[tri_row<C>(t, j / 2) * 32 + (16 * j + c) % 32] = z[r];
+            if (i == j && i % 2 == 0) zOut[tri_row<C>(t, j / 2) * 32 + 16 + c] = 0.0f;     // the tile right of the diagonal's
+        }
     }
 }
 
-// ---- through the chunks -----------------------------------------------------------------------------
 // What only leads to outputs in bf16 takes two parts a value (2^-16): Q S and M beta u.  The state's way takes three.
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
