@@ -174,6 +174,13 @@ template <typename T> __device__ __forceinline__ void park_eight(uint16_t *p, in
     }
 }
 
+// The same number, of which the compiler knows nothing: what is computed from it is computed where it is used, instead of ahead of
+// a loop for all of its phases in registers that the loop has not got.
+__device__ __forceinline__ int here(int n) {
+    asm volatile("" : "+v"(n));
+    return n;
+}
+
 // ---- a chunk --------------------------------------------------------------------------------------
 // bf16: 64 tokens, whose elements are one part each.  fp32: 32 tokens of three parts, so that queries, keys and the chunk's
 // matrices fit LDS as they do in bf16.

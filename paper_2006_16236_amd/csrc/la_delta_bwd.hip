@@ -161,187 +161,30 @@ template <typename T, int D> __global__ __launch_bounds__(512) void delta_states
     if (a.dh0 != nullptr) store_state<D>(a.dh0 + state, m - c, a.M, lane, S);
 }
 
-// A workgroup takes one chunk and the heads that share its queries and keys, one after the other, D / 16 waves with 16
-// columns of dQ and dK each; the columns of the states 64 at a time.
-template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chunks_bwd_kernel(const DeltaArgs a) {
+// A workgroup takes one chunk and the heads that share its queries and keys, one after the other; a wave has kSlabs times 16
+// columns of dQ and dK; the columns of the states come 32 at a time ("turn").  What a turn reads from memory is on its way
+// during the turn before, and two workgroups share a compute unit: with all columns of eight waves at once, one workgroup, half
+// of the time went to waiting for loads (8 x 2048 x 16 heads of 128 bf16: 462 us).
+// kShared: sums over more than one head wait in LDS.
+template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 ? 128 : 256, kShared ? 1 : 2) void delta_chunks_bwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kWaves = D / 16, kThreads = 4 * D;
+    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kWaves = D == 32 ? 2 : 4, kThreads = 64 * kWaves;
+    constexpr int kSlabs = D / 16 / kWaves, kTurn = 32, kPieces = kTurn / 8;
     constexpr int kLow = kTiles * (kTiles + 1) / 2, kLowEach = (kLow + kWaves - 1) / kWaves;
-    constexpr int kStage = (6 + P) * C * kCols, kSquares = 6 * C * C, kWork = kStage > kSquares ? kStage : kSquares;
+    constexpr int kStage = (6 + P) * C * kTurn, kSquare = 3 * C * C, kWork = kStage > kSquare ? kStage : kSquare;
+    constexpr int kEach = (C * kPieces + kThreads - 1) / kThreads, kGateEach = (4 * C + kThreads - 1) / kThreads;
     __shared__ alignas(16) uint16_t kS[P * C * D], qS[P * C * D], work[kWork];
     __shared__ alignas(16) float gates[4 * C], bt[C], miss[C], db[C], red[kWaves][C], ends[kWaves];
-    uint16_t *uS = work, *wS = work + 3 * C * kCols, *oS = work + 6 * C * kCols;          // U, dV, dO
-    uint16_t *pS = work, *bS = work + 3 * C * C;                                            // P, B + B^T
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, d = 16 * wave + c;
+    __shared__ f32x4 sums[kShared ? 2 : 1][kShared ? kSlabs * kTiles : 1][kShared ? kThreads : 1];      // dQ, dK so far
+    uint16_t *uS = work, *wS = work + 3 * C * kTurn, *oS = work + 6 * C * kTurn, *square = work;          // U, dV, dO; P, then B + B^T
+    int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int chunk = (int)(blockIdx.x % a.K), bk = (int)(blockIdx.x / a.K), b = bk / a.Hk, hk = bk % a.Hk, per = a.H / a.Hk;
-    const int len = length_of(a, b), t0 = chunk * C, left = len - t0;
-    const size_t row0 = (size_t)b * a.N + t0, ldo = (size_t)a.H * a.M;
-    f32x4 dq[kTiles], dk[kTiles];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) dq[t] = dk[t] = f32x4{0, 0, 0, 0};
-    if (left > 0) {
-        for (int i = tid; i < C * D / 8; i += kThreads) {
-            const int t = i / (D / 8), piece = i % (D / 8);
-            park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, load_eight<T>((const T *)a.k + (row0 + t) * a.ldk + (size_t)hk * D + 8 * piece, t < left));
-            park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, load_eight<T>((const T *)a.q + (row0 + t) * a.ldq + (size_t)hk * D + 8 * piece, t < left));
-        }
-        for (int h = hk * per; h < (hk + 1) * per; ++h) {
-            const long unit = (long)(b * a.H + h) * a.K + chunk;
-            __syncthreads();                                 // the head before is done with everything below
-            for (int i = tid; i < 4 * C; i += kThreads) gates[i] = a.gate[unit * 4 * C + i];
-            for (int i = tid; i < C; i += kThreads) bt[i] = i < left ? a.beta[(row0 + i) * a.H + h] : 0.0f, miss[i] = db[i] = 0.0f;
-            f32x4 q1[kTiles], k1[kTiles], k2[kTiles], p[kLowEach], bb[kLowEach];
-            float both = 0.0f;                               // <S, dS'>
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) q1[t] = k1[t] = k2[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < kLowEach; ++i) p[i] = bb[i] = f32x4{0, 0, 0, 0};
-            for (int m0 = 0; m0 < a.M; m0 += kCols) {
-                __syncthreads();
-                for (int i = tid; i < C * 8; i += kThreads) {
-                    const int t = i / 8, piece = i % 8, m = m0 + 8 * piece;
-                    const bool have = m < a.M, live = have && t < left;
-                    const Eight<float> us = load_eight<float>(a.miss + ((size_t)unit * C + t) * a.M + m, have);
-                    const Eight<float> ys = load_eight<float>(a.write + ((size_t)unit * C + t) * a.M + m, have);
-                    const Eight<T> vs = load_eight<T>((const T *)a.v + (row0 + t) * a.ldv + (size_t)h * a.M + m, live);
-                    const Eight<T> os = load_eight<T>((const T *)a.dO + (row0 + t) * ldo + (size_t)h * a.M + m, live);
-                    float u[8], w[8], dots = 0.0f, dbs = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        u[e] = bt[t] * us.get(e), w[e] = bt[t] * ys.get(e);
-                        dots = fmaf(w[e], vs.get(e) - us.get(e), dots);
-                        dbs = fmaf(ys.get(e), us.get(e), dbs);
-                    }
-                    const int at = mat_at<kCols, true>(t, piece);
-                    park_eight(uS + at, C * kCols, u);
-                    park_eight(wS + at, C * kCols, w);
-                    park_eight<T>(oS + at, C * kCols, os);
-                    dots += dpp_move<0xB1>(dots), dbs += dpp_move<0xB1>(dbs);       // over the eight lanes of a token
-                    dots += dpp_move<0x4E>(dots), dbs += dpp_move<0x4E>(dbs);
-                    dots += dpp_move<0x141>(dots), dbs += dpp_move<0x141>(dbs);
-                    if (piece == 0) miss[t] += dots, db[t] += dbs;
-                }
-                __syncthreads();
-                // tiles of P^T and B^T: rows s, columns t >= s
-#pragma unroll
-                for (int i = 0; i < kLowEach; ++i) {
-                    int n = wave + i * kWaves, ct = 0;
-                    if (n >= kLow) break;
-                    while (n > ct) n -= ++ct;                // n-th tile s of column tile t = ct
-#pragma unroll
-                    for (int s = 0; s < kCols / 32; ++s) {
-                        const Parts<3> u = row_operand<kCols, 3, true>(uS, C * kCols, 16 * n + c, 4 * s + g);
-                        p[i] = product(u, row_operand<kCols, P, true>(oS, C * kCols, 16 * ct + c, 4 * s + g), p[i]);
-                        bb[i] = product(u, row_operand<kCols, 3, true>(wS, C * kCols, 16 * ct + c, 4 * s + g), bb[i]);
-                    }
-                }
-#pragma unroll
-                for (int s = 0; s < kCols / 32; ++s) {
-                    const int m = m0 + 32 * s + 8 * g;
-                    const size_t at = (size_t)unit * D * a.M + (size_t)d * a.M + m;
-                    const Eight<float> s0 = load_eight<float>(a.state + at, m < a.M), s1 = load_eight<float>(a.dstate + at, m < a.M);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) both = fmaf(s0.get(e), s1.get(e), both);
-                    const Parts<3> x0 = cut(f32x4{s0.get(0), s0.get(1), s0.get(2), s0.get(3)}, f32x4{s0.get(4), s0.get(5), s0.get(6), s0.get(7)});
-                    const Parts<3> x1 = cut(f32x4{s1.get(0), s1.get(1), s1.get(2), s1.get(3)}, f32x4{s1.get(4), s1.get(5), s1.get(6), s1.get(7)});
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
-                        q1[t] = product(row_operand<kCols, P, true>(oS, C * kCols, 16 * t + c, 4 * s + g), x0, q1[t]);
-                        k1[t] = product(row_operand<kCols, 3, true>(wS, C * kCols, 16 * t + c, 4 * s + g), x0, k1[t]);
-                        k2[t] = product(row_operand<kCols, 3, true>(uS, C * kCols, 16 * t + c, 4 * s + g), x1, k2[t]);
-                    }
-                }
-            }
-            __syncthreads();                                 // U, dV, dO make way for P and B + B^T
-#pragma unroll
-            for (int i = 0; i < kLowEach; ++i) {
-                int n = wave + i * kWaves, ct = 0;
-                if (n >= kLow) break;
-                while (n > ct) n -= ++ct;
-                const int t = 16 * ct + c, s = 16 * n + 4 * g;
-                f32x4 pv, bv;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float decay = s + r <= t ? expf((gates[2 * C + t] - gates[2 * C + s + r]) + (gates[3 * C + t] - gates[3 * C + s + r])) : 0.0f;
-                    pv[r] = s + r <= t ? a.scale * p[i][r] * decay : 0.0f;
-                    bv[r] = s + r < t ? -bb[i][r] * decay : 0.0f;
-                }
-                const float pq[4] = {pv[0], pv[1], pv[2], pv[3]}, bq[4] = {bv[0], bv[1], bv[2], bv[3]};
-                const Split3 ps = split3(pq), bs = split3(bq);
-                const u32x2_t parts[2][3] = {{ps.h, ps.m, ps.l}, {bs.h, bs.m, bs.l}};
-                const int here = mat_at<C, true>(t, s / 8) + s % 8;
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                    *reinterpret_cast<u32x2_t *>(pS + k * C * C + here) = parts[0][k];
-                    if (n == ct) {                           // on the diagonal both triangles are in one tile
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint16_t e = (uint16_t)(parts[1][k][r / 2] >> (16 * (r & 1)));
-                            if (s + r <= t) bS[k * C * C + here + r] = bS[k * C * C + mat_at<C, true>(s + r, t / 8) + t % 8] = e;
-                        }
-                    } else {
-                        *reinterpret_cast<u32x2_t *>(bS + k * C * C + here) = parts[1][k];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            bS[k * C * C + mat_at<C, true>(s + r, t / 8) + t % 8] = (uint16_t)(parts[1][k][r / 2] >> (16 * (r & 1)));
-                    }
-                    // the tile right above the diagonal, which products over 32 tokens read
-                    if (n == ct && ct % 2 == 0) *reinterpret_cast<u32x2_t *>(pS + k * C * C + mat_at<C, true>(t, (s + 16) / 8) + s % 8) = u32x2_t{0, 0};
-                }
-            }
-            __syncthreads();
-            float into = 0.0f;
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                f32x4 qd, kd, eg, eh;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) eg[r] = gates[16 * t + 4 * g + r], eh[r] = gates[C + 16 * t + 4 * g + r];
-                qd = a.scale * eg * q1[t];
-                k2[t] = eh * k2[t];
-                kd = k2[t] - eg * k1[t];
-#pragma unroll
-                for (int s = 0; s < kBlocks; ++s) {
-                    const Parts<P> kx = column_operand<D, false, P, true>(kS, C * D, 32 * s, wave, lane);
-                    if (s <= t / 2) qd = product(row_operand<C, 3, true>(pS, C * C, 16 * t + c, 4 * s + g), kx, qd);
-                    if (s >= t / 2)
-                        kd = product(column_operand<C, false, 3, true>(pS, C * C, 32 * s, t, lane), column_operand<D, false, P, true>(qS, C * D, 32 * s, wave, lane), kd);
-                    kd = product(row_operand<C, 3, true>(bS, C * C, 16 * t + c, 4 * s + g), kx, kd);
-                }
-                dq[t] += qd, dk[t] += kd;
-                const f32x4 qv = column_values<D, P, true>(qS, C * D, 16 * t + 4 * g, wave, lane).sum(), kv = column_values<D, P, true>(kS, C * D, 16 * t + 4 * g, wave, lane).sum();
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    into = fmaf(kv[r], k2[t][r], into);
-                    const float dot = row_sum16(qv[r] * qd[r] - kv[r] * kd[r]);
-                    if (c == 0) red[wave][16 * t + 4 * g + r] = dot;
-                }
-            }
-            into = wave_sum(fmaf(gates[C - 1], both, into));
-            if (lane == 0) ends[wave] = into;
-            __syncthreads();
-            if (wave == 0) {
-                double sum = 0.0;
-                if (lane < C) {
-                    sum = -2.0 * (double)miss[lane];
-#pragma unroll
-                    for (int w = 0; w < kWaves; ++w) {
-                        sum += (double)red[w][lane];
-                        if (lane == C - 1) sum += (double)ends[w];
-                    }
-                }
-#pragma unroll
-                for (int k = 1; k < C; k *= 2) {
-                    const double from = __shfl_down(sum, k);
-                    if (lane + k < C) sum += from;
-                }
-                if (lane < C && t0 + lane < a.N) {
-                    const size_t at = (row0 + lane) * a.H + h;
-                    if (a.dg != nullptr) a.dg[at] = lane < left ? (float)sum : 0.0f;
-                    a.dbeta[at] = lane < left ? db[lane] : 0.0f;
-                }
-            }
-        }
-    } else {
+    const int len = length_of(a, b), t0 = chunk * C, left = len - t0, rows = left < C ? left : C, ldo = a.H * a.M;
+    const size_t row0 = (size_t)b * a.N + t0;
+    const int inside = a.N - t0 < C ? a.N - t0 : C, ldd = a.Hk * D;
+    const Range dqr = range_of((T *)a.dq + row0 * ldd + (size_t)hk * D, inside, ldd, D), dkr = range_of((T *)a.dk + row0 * ldd + (size_t)hk * D, inside, ldd, D);
+    if (left <= 0) {                                         // behind the sequence
         for (int i = tid; i < C * per; i += kThreads) {
             const int t = i / per;
             const size_t at = (row0 + t) * a.H + hk * per + i % per;
@@ -349,17 +192,290 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void delta_chun
             if (a.dg != nullptr) a.dg[at] = 0.0f;
             a.dbeta[at] = 0.0f;
         }
-    }
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int n = 16 * t + 4 * g + r;
-            if (t0 + n >= a.N) continue;
-            const size_t at = ((row0 + n) * a.Hk + hk) * D + d;
-            store_elem<false>((T *)a.dq + at, n < left ? dq[t][r] : 0.0f);
-            store_elem<false>((T *)a.dk + at, n < left ? dk[t][r] : 0.0f);
+        for (int i = 0; i < kSlabs * kTiles; ++i) {
+            store_tile<T>(dqr, 16 * (i % kTiles) + 4 * g, 16 * (wave * kSlabs + i / kTiles), ldd, f32x4{0, 0, 0, 0}, lane);
+            store_tile<T>(dkr, 16 * (i % kTiles) + 4 * g, 16 * (wave * kSlabs + i / kTiles), ldd, f32x4{0, 0, 0, 0}, lane);
         }
+        return;
+    }
+    const int turns = (a.M + kTurn - 1) / kTurn, all = per * turns;
+    // what one turn reads: u, y, V, dO of its columns, S and dS' of this lane's rows
+    Eight<float> us[kEach], ys[kEach], s0[kSlabs], s1[kSlabs];
+    Eight<T> vs[kEach], os[kEach];
+    float gate_in[kGateEach], beta_in;
+    const auto load = [&](int n) {
+        const int h = hk * per + n / turns, m0 = n % turns * kTurn, cols = a.M - m0 < kTurn ? a.M - m0 : kTurn;
+        const long unit = (long)(b * a.H + h) * a.K + chunk;
+        const Range ur = range_of(a.miss + (size_t)unit * C * a.M + m0, C, a.M, cols), yr = range_of(a.write + (size_t)unit * C * a.M + m0, C, a.M, cols);
+        const Range vr = range_of((const T *)a.v + row0 * a.ldv + (size_t)h * a.M + m0, rows, a.ldv, cols);
+        const Range zr = range_of((const T *)a.dO + row0 * ldo + (size_t)h * a.M + m0, rows, ldo, cols);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = tid + kThreads * j, t = i / kPieces, piece = i % kPieces;
+            const bool in = 8 * piece < cols && (C * kPieces % kThreads == 0 || i < C * kPieces);
+            us[j] = load_eight<float>(ur, in ? (t * a.M + 8 * piece) * 4 : 0x7fffff00);
+            ys[j] = load_eight<float>(yr, in ? (t * a.M + 8 * piece) * 4 : 0x7fffff00);
+            vs[j] = load_eight<T>(vr, in ? (t * (int)a.ldv + 8 * piece) * (int)sizeof(T) : 0x7fffff00);
+            os[j] = load_eight<T>(zr, in ? (t * ldo + 8 * piece) * (int)sizeof(T) : 0x7fffff00);
+        }
+        const Range br = range_of(a.beta + row0 * a.H + h, rows, a.H, 1);
+#pragma unroll
+        for (int j = 0; j < kGateEach; ++j) gate_in[j] = a.gate[unit * 4 * C + (tid + kThreads * j) % (4 * C)];
+        beta_in = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(br, tid * a.H * 4, 0, 0));
+    };
+    const auto load_states = [&](int n) {
+        const int h = hk * per + n / turns, m0 = n % turns * kTurn, cols = a.M - m0 < kTurn ? a.M - m0 : kTurn;
+        const size_t at = (size_t)((long)(b * a.H + h) * a.K + chunk) * D * a.M + m0;
+        const Range s0r = range_of(a.state + at, D, a.M, cols), s1r = range_of(a.dstate + at, D, a.M, cols);
+#pragma unroll
+        for (int x = 0; x < kSlabs; ++x) {
+            const int in = 8 * g < cols ? ((16 * (wave * kSlabs + x) + c) * a.M + 8 * g) * 4 : 0x7fffff00;
+            s0[x] = load_eight<float>(s0r, in), s1[x] = load_eight<float>(s1r, in);
+        }
+    };
+    {
+        constexpr int kTok = C * D / 8, kTokEach = (kTok + kThreads - 1) / kThreads;
+        const Range kr = range_of((const T *)a.k + row0 * a.ldk + (size_t)hk * D, rows, a.ldk, D);
+        const Range qr = range_of((const T *)a.q + row0 * a.ldq + (size_t)hk * D, rows, a.ldq, D);
+        Eight<T> kq[kTokEach][2];
+#pragma unroll
+        for (int j = 0; j < kTokEach; ++j) {
+            const int i = tid + kThreads * j, t = i / (D / 8), piece = i % (D / 8);
+            kq[j][0] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * (int)sizeof(T));
+            kq[j][1] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * (int)sizeof(T));
+        }
+        load(0);
+#pragma unroll
+        for (int j = 0; j < kTokEach; ++j) {
+            const int i = tid + kThreads * j, t = i / (D / 8), piece = i % (D / 8);
+            park_eight<T>(kS + mat_at<D, true>(t, piece), C * D, kq[j][0]);
+            park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, kq[j][1]);
+        }
+    }
+    f32x4 q1[kSlabs][kTiles], k1[kSlabs][kTiles], k2[kSlabs][kTiles], p[kLowEach], bb[kLowEach];
+    float both = 0.0f;                                       // <S, dS'>
+    // the wave's i-th tile of a lower triangle: rows 16 ct.., columns 16 st..
+    const auto tile_of = [&](int i, int &st, int &ct) {
+        st = wave + i * kWaves, ct = 0;
+        if (st >= kLow) return false;
+        while (st > ct) st -= ++ct;
+        return true;
+    };
+    for (int n = 0; n < all; ++n) {
+        const int h = hk * per + n / turns;
+        load_states(n);
+        tid = here(tid), lane = tid % kWave, c = lane % 16, g = lane / 16;
+        __syncthreads();                                     // the turn before has been read
+        if (n % turns == 0) {
+#pragma unroll
+            for (int j = 0; j < kGateEach; ++j)
+                if (tid + kThreads * j < 4 * C) gates[tid + kThreads * j] = gate_in[j];
+            if (tid < C) bt[tid] = beta_in, miss[tid] = db[tid] = 0.0f;
+            __syncthreads();
+            both = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) q1[x][t] = k1[x][t] = k2[x][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kLowEach; ++i) p[i] = bb[i] = f32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = tid + kThreads * j, t = i / kPieces, piece = i % kPieces;
+            if (C * kPieces % kThreads != 0 && i >= C * kPieces) break;
+            float u[8], w[8], dots = 0.0f, dbs = 0.0f;
+            const float beta = bt[t];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u[e] = beta * us[j].get(e), w[e] = beta * ys[j].get(e);
+                dots = fmaf(w[e], vs[j].get(e) - us[j].get(e), dots);
+                dbs = fmaf(ys[j].get(e), us[j].get(e), dbs);
+            }
+            const int at = mat_at<kTurn, true>(t, piece);
+            park_eight(uS + at, C * kTurn, u);
+            park_eight(wS + at, C * kTurn, w);
+            park_eight<T>(oS + at, C * kTurn, os[j]);
+            dots += dpp_move<0xB1>(dots), dbs += dpp_move<0xB1>(dbs);           // over the four lanes of a token
+            dots += dpp_move<0x4E>(dots), dbs += dpp_move<0x4E>(dbs);
+            if (piece == 0) miss[t] += dots, db[t] += dbs;
+        }
+        load(n + 1 < all ? n + 1 : n);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kLowEach; ++i) {                 // P^T and B^T: rows s, columns t >= s
+            int st, ct;
+            if (!tile_of(i, st, ct)) break;
+            const Parts<3> u = row_operand<kTurn, 3, true>(uS, C * kTurn, 16 * st + c, g);
+            p[i] = product(u, row_operand<kTurn, P, true>(oS, C * kTurn, 16 * ct + c, g), p[i]);
+            bb[i] = product(u, row_operand<kTurn, 3, true>(wS, C * kTurn, 16 * ct + c, g), bb[i]);
+        }
+#pragma unroll
+        for (int x = 0; x < kSlabs; ++x) {                   // one after the other: their operands together are too many registers
+#pragma unroll
+            for (int e = 0; e < 8; ++e) both = fmaf(s0[x].get(e), s1[x].get(e), both);
+            const Parts<3> x0 = cut(f32x4{s0[x].get(0), s0[x].get(1), s0[x].get(2), s0[x].get(3)}, f32x4{s0[x].get(4), s0[x].get(5), s0[x].get(6), s0[x].get(7)});
+            const Parts<3> x1 = cut(f32x4{s1[x].get(0), s1[x].get(1), s1[x].get(2), s1[x].get(3)}, f32x4{s1[x].get(4), s1[x].get(5), s1[x].get(6), s1[x].get(7)});
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                q1[x][t] = product(row_operand<kTurn, P, true>(oS, C * kTurn, 16 * t + c, g), x0, q1[x][t]);
+                k1[x][t] = product(row_operand<kTurn, 3, true>(wS, C * kTurn, 16 * t + c, g), x0, k1[x][t]);
+                k2[x][t] = product(row_operand<kTurn, 3, true>(uS, C * kTurn, 16 * t + c, g), x1, k2[x][t]);
+                if (kSlabs > 1 && t % 2 == 1) in_this_order();
+            }
+        }
+        if (n % turns != turns - 1) continue;
+        tid = here(tid), lane = tid % kWave, c = lane % 16, g = lane / 16;
+        __syncthreads();                                     // U, dV, dO make way for P
+#pragma unroll
+        for (int i = 0; i < kLowEach; ++i) {
+            int st, ct;
+            if (!tile_of(i, st, ct)) break;
+            const int t = 16 * ct + c, s = 16 * st + 4 * g, place = mat_at<C, true>(t, s / 8) + s % 8;
+            float pq[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float decay = s + r <= t ? expf((gates[2 * C + t] - gates[2 * C + s + r]) + (gates[3 * C + t] - gates[3 * C + s + r])) : 0.0f;
+                pq[r] = s + r <= t ? a.scale * p[i][r] * decay : 0.0f;
+                bb[i][r] = s + r < t ? -bb[i][r] * decay : 0.0f;
+            }
+            const Split3 ps = split3(pq);
+            const u32x2_t parts[3] = {ps.h, ps.m, ps.l};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                *reinterpret_cast<u32x2_t *>(square + k * C * C + place) = parts[k];
+                // the tile right above the diagonal, which products over 32 tokens read
+                if (st == ct && ct % 2 == 0) *reinterpret_cast<u32x2_t *>(square + k * C * C + mat_at<C, true>(t, (s + 16) / 8) + s % 8) = u32x2_t{0, 0};
+            }
+        }
+        __syncthreads();
+        float into = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const f32x4 eg = *reinterpret_cast<const f32x4 *>(gates + 16 * t + 4 * g), eh = *reinterpret_cast<const f32x4 *>(gates + C + 16 * t + 4 * g);
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) {
+                const f32x4 kv = column_values<D, P, true>(kS, C * D, 16 * t + 4 * g, wave * kSlabs + x, lane).sum();
+                k2[x][t] = eh * k2[x][t];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) into = fmaf(kv[r], k2[x][t][r], into);
+                q1[x][t] = a.scale * eg * q1[x][t];
+                k1[x][t] = k2[x][t] - eg * k1[x][t];
+            }
+            if (kSlabs > 1) in_this_order();
+        }
+        // products with a square matrix in LDS, from the left: its rows, and of P its columns too
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) {
+            Parts<P> kx[kSlabs], qx[kSlabs];
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) {
+                kx[x] = column_operand<D, false, P, true>(kS, C * D, 32 * s, wave * kSlabs + x, lane);
+                qx[x] = column_operand<D, false, P, true>(qS, C * D, 32 * s, wave * kSlabs + x, lane);
+            }
+#pragma unroll
+            for (int t = 2 * s; t < kTiles; ++t) {
+                const Parts<3> f = row_operand<C, 3, true>(square, C * C, 16 * t + c, 4 * s + g);
+#pragma unroll
+                for (int x = 0; x < kSlabs; ++x) q1[x][t] = product(f, kx[x], q1[x][t]);
+                if (kSlabs > 1 && t % 2 == 1) in_this_order();
+            }
+#pragma unroll
+            for (int t = 0; t < 2 * (s + 1); ++t) {
+                const Parts<3> f = column_operand<C, false, 3, true>(square, C * C, 32 * s, t, lane);
+#pragma unroll
+                for (int x = 0; x < kSlabs; ++x) k1[x][t] = product(f, qx[x], k1[x][t]);
+                if (kSlabs > 1 && t % 2 == 1) in_this_order();
+            }
+        }
+        __syncthreads();                                     // P makes way for B + B^T
+#pragma unroll
+        for (int i = 0; i < kLowEach; ++i) {
+            int st, ct;
+            if (!tile_of(i, st, ct)) break;
+            const int t = 16 * ct + c, s = 16 * st + 4 * g, place = mat_at<C, true>(t, s / 8) + s % 8;
+            const float bq[4] = {bb[i][0], bb[i][1], bb[i][2], bb[i][3]};
+            const Split3 bs = split3(bq);
+            const u32x2_t parts[3] = {bs.h, bs.m, bs.l};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                uint16_t *to = square + k * C * C;
+                if (st != ct) *reinterpret_cast<u32x2_t *>(to + place) = parts[k];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint16_t e = (uint16_t)(parts[k][r / 2] >> (16 * (r & 1)));
+                    if (st != ct || s + r <= t) to[mat_at<C, true>(s + r, t / 8) + t % 8] = e;
+                    if (st == ct && s + r <= t) to[place + r] = e;        // on the diagonal both triangles are in one tile
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kBlocks; ++s) {
+            Parts<P> kx[kSlabs];
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) kx[x] = column_operand<D, false, P, true>(kS, C * D, 32 * s, wave * kSlabs + x, lane);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                const Parts<3> f = row_operand<C, 3, true>(square, C * C, 16 * t + c, 4 * s + g);
+#pragma unroll
+                for (int x = 0; x < kSlabs; ++x) k1[x][t] = product(f, kx[x], k1[x][t]);
+                if (kSlabs > 1 && t % 2 == 1) in_this_order();
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            f32x4 dot = {0, 0, 0, 0};
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) {
+                const int slab = wave * kSlabs + x;
+                f32x4 qd = q1[x][t], kd = k1[x][t];
+                dot += column_values<D, P, true>(qS, C * D, 16 * t + 4 * g, slab, lane).sum() * qd - column_values<D, P, true>(kS, C * D, 16 * t + 4 * g, slab, lane).sum() * kd;
+                if constexpr (kShared) {
+                    if (h > hk * per) qd += sums[0][x * kTiles + t][tid], kd += sums[1][x * kTiles + t][tid];
+                    sums[0][x * kTiles + t][tid] = qd, sums[1][x * kTiles + t][tid] = kd;
+                }
+                if (n == all - 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * t + 4 * g + r >= left) qd[r] = kd[r] = 0.0f;
+                    store_tile<T>(dqr, 16 * t + 4 * g, 16 * slab, ldd, qd, lane);
+                    store_tile<T>(dkr, 16 * t + 4 * g, 16 * slab, ldd, kd, lane);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = row_sum16(dot[r]);
+                if (c == 0) red[wave][16 * t + 4 * g + r] = v;
+            }
+            if (kSlabs > 1) in_this_order();
+        }
+        into = wave_sum(fmaf(gates[C - 1], both, into));
+        if (lane == 0) ends[wave] = into;
+        __syncthreads();
+        if (wave == 0) {
+            double sum = 0.0;
+            if (lane < C) {
+                sum = -2.0 * (double)miss[lane];
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    sum += (double)red[w][lane];
+                    if (lane == C - 1) sum += (double)ends[w];
+                }
+            }
+#pragma unroll
+            for (int k = 1; k < C; k *= 2) {
+                const double from = __shfl_down(sum, k);
+                if (lane + k < C) sum += from;
+            }
+            if (lane < C && t0 + lane < a.N) {
+                const size_t at = (row0 + lane) * a.H + h;
+                if (a.dg != nullptr) a.dg[at] = lane < left ? (float)sum : 0.0f;
+                a.dbeta[at] = lane < left ? db[lane] : 0.0f;
+            }
+        }
+    }
 }
 }  // namespace
 
@@ -367,7 +483,7 @@ hipError_t launch_delta_bwd(const DeltaArgs &a, int dtype, hipStream_t s) {
 #define LA_STATES(T, D) delta_states_bwd_kernel<T, D><<<head_grid(a), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_STATES)
     const unsigned units = (unsigned)((long)a.B * a.Hk * a.K);
-#define LA_CHUNKS(T, D) delta_chunks_bwd_kernel<T, D><<<units, 4 * D, 0, s>>>(a)
+#define LA_CHUNKS(T, D) a.H > a.Hk ? delta_chunks_bwd_kernel<T, D, true><<<units, D == 32 ? 128 : 256, 0, s>>>(a) : delta_chunks_bwd_kernel<T, D, false><<<units, D == 32 ? 128 : 256, 0, s>>>(a)
     LA_BY_WIDTH(LA_CHUNKS)
     return hipGetLastError();
 }
