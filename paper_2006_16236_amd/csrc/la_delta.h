@@ -203,15 +203,40 @@ __device__ __forceinline__ int length_of(const DeltaArgs &a, int b) {
 // ---- through the chunks -----------------------------------------------------------------------------
 constexpr int kCols = 64;                                    // columns of a workgroup, 16 a wave
 
+// What a workgroup of a pass does: 64 columns of one piece of one head.
+//   kWhole: the pass itself;  kStates: only the state behind the piece (backward: before it);  kTransitions: so too, and with
+//   columns of the unit matrix behind those of V.
+enum PassKind { kWhole, kStates, kTransitions };
+struct Task {
+    int bh, b, h, len, piece, first, count;        // chunks first .. first + count - 1
+    int m0, cols;
+    bool unit;                                     // columns of the unit matrix
+    bool start, end;                               // the sequence's first piece, its last one
+};
 // The workgroups of a head's column blocks share its queries, keys and matrices: eight ids apart, they run on one XCD and
-// find them in its L2.
-__device__ __forceinline__ bool head_and_columns(const DeltaArgs &a, int &bh, int &m0) {
-    const int blocks = (a.M + kCols - 1) / kCols, x = blockIdx.x % 8, y = blockIdx.x / 8;
-    bh = y / blocks * 8 + x;
-    m0 = y % blocks * kCols;
-    return bh < a.B * a.H;
+// find them in its L2.  False: nothing to do.
+template <PassKind kKind, bool kBack> __device__ __forceinline__ bool task_of(const DeltaArgs &a, int C, int D, Task &t) {
+    const int own = (a.M + kCols - 1) / kCols, blocks = own + (kKind == kTransitions ? (D + kCols - 1) / kCols : 0);
+    const int pieces = kKind == kWhole ? a.pieces : a.pieces - 1, x = blockIdx.x % 8, y = blockIdx.x / 8, head = y / blocks * 8 + x, block = y % blocks;
+    if (head >= a.B * a.H * pieces) return false;
+    t.bh = head / pieces, t.piece = head % pieces + (kKind != kWhole && kBack ? 1 : 0);
+    t.b = t.bh / a.H, t.h = t.bh % a.H;
+    t.unit = block >= own;
+    t.m0 = (t.unit ? block - own : block) * kCols;
+    const int width = t.unit ? D : a.M;
+    t.cols = width - t.m0 < kCols ? width - t.m0 : kCols;
+    t.len = length_of(a, t.b);
+    const int chunks = (t.len + C - 1) / C, last = chunks > 0 ? (chunks - 1) / a.length : 0;
+    t.start = t.piece == 0, t.end = t.piece == last;
+    t.first = t.piece * a.length;
+    t.count = chunks - t.first < a.length ? chunks - t.first : a.length;
+    if (t.piece > last || (kKind != kWhole && !kBack && t.end)) return false;
+    return !t.unit || (!t.start && !t.end);        // the first and the last piece start from a state that is there
 }
-inline unsigned head_grid(const DeltaArgs &a) { return (unsigned)((a.B * a.H + 7) / 8 * 8 * ((a.M + kCols - 1) / kCols)); }
+inline unsigned task_grid(const DeltaArgs &a, PassKind kind) {
+    const int blocks = (a.M + kCols - 1) / kCols + (kind == kTransitions ? (a.D + kCols - 1) / kCols : 0), pieces = kind == kWhole ? a.pieces : a.pieces - 1;
+    return (unsigned)((a.B * a.H * pieces + 7) / 8 * 8 * blocks);
+}
 
 // Rows of a tensor as the range check of a buffer descriptor sees them: loads behind the last one's `width` elements give zeros,
 // stores there are left out.  The whole offset goes into the lane's own address, which is what is checked.
@@ -245,10 +270,11 @@ template <typename T, int D> struct Chunked {
     alignas(16) uint16_t k[kTok], q[kTok], v[kVal], z[kTri], m[kTri];
     alignas(16) float gates[3 * Ch::C];
 };
-template <typename T, int D> struct Fetch {
+// kLean: without Q, M (and V where no columns are asked for): what a pass for states alone needs
+template <typename T, int D, bool kLean> struct Fetch {
     using Ch = Chunk<T>;
     static constexpr int C = Ch::C, kTok = C * D / 8, kTokEach = (kTok + 255) / 256, kVal = C * kCols / 8, kValEach = (kVal + 255) / 256;
-    static constexpr int kTri = Ch::kTri / 8, kTriEach = (2 * kTri + 255) / 256;
+    static constexpr int kTri = Ch::kTri / 8, kMats = kLean ? 1 : 2, kTriEach = (kMats * kTri + 255) / 256;
     static_assert(2 * kTri % 256 == 0 && kVal % 256 == 0, "whole turns of 256 threads");
     Eight<T> k[kTokEach], q[kTokEach], v[kValEach];
     Eight<float> tri[kTriEach];
@@ -266,7 +292,7 @@ template <typename T, int D> struct Fetch {
         for (int j = 0; j < kTokEach; ++j) {
             const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
             k[j] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * e);
-            q[j] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * e);
+            if (!kLean) q[j] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * e);
         }
 #pragma unroll
         for (int j = 0; j < kValEach; ++j) {
@@ -275,7 +301,7 @@ template <typename T, int D> struct Fetch {
         }
         const float *m = a.tri + unit * 2 * Ch::kTri;
 #pragma unroll
-        for (int j = 0; j < kTriEach; ++j) __builtin_memcpy(tri[j].w, m + 8 * (tid + 256 * j), sizeof(tri[j].w));
+        for (int j = 0; j < kTriEach; ++j) __builtin_memcpy(tri[j].w, m + 8 * ((tid + 256 * j) % (kMats * kTri)), sizeof(tri[j].w));
         gate = a.gate[unit * 4 * C + tid % (2 * C)];
         beta = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(br, tid * a.H * 4, 0, 0));
     }
@@ -285,7 +311,7 @@ template <typename T, int D> struct Fetch {
             const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
             if (kTok % 256 != 0 && i >= kTok) break;
             park_eight<T>(to.k + mat_at<D>(t, piece), C * D, k[j]);
-            park_eight<T>(to.q + mat_at<D>(t, piece), C * D, q[j]);
+            if (!kLean) park_eight<T>(to.q + mat_at<D>(t, piece), C * D, q[j]);
         }
 #pragma unroll
         for (int j = 0; j < kValEach; ++j) {
@@ -295,29 +321,31 @@ template <typename T, int D> struct Fetch {
 #pragma unroll
         for (int j = 0; j < kTriEach; ++j) {
             const int i = tid + 256 * j, at = i < kTri ? i : i - kTri;
+            if (kMats * kTri % 256 != 0 && i >= kMats * kTri) break;
             park_eight<float>((i < kTri ? to.z : to.m) + mat_at<32>(at / 4, at % 4), Ch::kTri, tri[j]);
         }
         if (tid < 2 * C) to.gates[tid] = gate;
         if (tid < C) to.gates[2 * C + tid] = beta;
     }
 };
-// The fetching waves: chunks first, first + by, .. of `count`.  The others meet the same barriers: one before their first chunk, and
-// one behind each.
-template <typename T, int D> __device__ __forceinline__ void fetch_chunks(Chunked<T, D> (&to)[2], const DeltaArgs &a, int bh, int len, int first, int by, int count,
-                                                                          const T *values, long ldv, int cols, int tid) {
+// The fetching waves of a task, its chunks forwards or backwards.  The others meet the same barriers: one before their first
+// chunk, and one behind each.
+template <typename T, int D, bool kLean, bool kBack> __device__ __forceinline__ void fetch_chunks(Chunked<T, D> (&to)[2], const DeltaArgs &a, const Task &task, const T *values,
+                                                                                                  long ldv, int tid) {
     constexpr int C = Chunk<T>::C;
-    const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
-    Fetch<T, D> f;
+    Fetch<T, D, kLean> f;
     const auto load = [&](int i) {
-        const int chunk = first + by * (i < count ? i : count - 1);
-        f.load(a, (long)bh * a.K + chunk, (size_t)b * a.N + (size_t)chunk * C, len - chunk * C, hk, h, values, ldv, cols, tid);
+        if (i >= task.count) i = task.count - 1;
+        const int chunk = task.first + (kBack ? task.count - 1 - i : i);
+        f.load(a, (long)task.bh * a.K + chunk, (size_t)task.b * a.N + (size_t)chunk * C, task.len - chunk * C, task.h / (a.H / a.Hk), task.h,
+               values + (size_t)task.h * a.M + task.m0, ldv, task.unit ? 0 : task.cols, tid);
     };
-    if (count == 0) return;
+    if (task.count <= 0) return;
     load(0);
     f.park(to[0], tid);
     load(1);
     __syncthreads();
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; i < task.count; ++i) {
         f.park(to[(i + 1) & 1], tid);
         load(i + 2);
         __syncthreads();
@@ -369,7 +397,7 @@ template <typename T> __device__ __forceinline__ void store_tile(Range r, int ro
     else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, at, 0, 0);
 }
 template <int D> __device__ __forceinline__ void store_state(float *state, int column, int M, int lane, const f32x4 (&S)[D / 16]) {
-    const Range r = range_of(state, D, M, M);
+    const Range r = range_of(state, D, M, M);                // M: of the whole state
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) store_tile<float>(r, paired(t, 4 * (lane / 16)), column, M, S[t], lane);
 }

@@ -169,37 +169,46 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
 // depends on a branch.
-template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void delta_fwd_kernel(const DeltaArgs a) {
+template <typename T, int D, PassKind kKind, bool kKeep> __global__ __launch_bounds__(512) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
+    constexpr bool kOutputs = kKind == kWhole;
     __shared__ Chunked<T, D> buffers[2];
-    int bh, m0;
-    if (!head_and_columns(a, bh, m0)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, m = m0 + wave * 16 + c;
-    const int b = bh / a.H, h = bh % a.H, len = length_of(a, b), chunks = (len + C - 1) / C;
-    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, ldo = a.H * a.M;
-    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M;
+    Task task;
+    if (!task_of<kKind, false>(a, C, D, task)) return;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, m = task.m0 + wave * 16 + c;
+    const int h = task.h, len = task.len, count = task.count, ldo = a.H * a.M;
+    const size_t seq = (size_t)task.b * a.N, state = (size_t)task.bh * D * a.M, piece = (size_t)task.bh * a.pieces + task.piece;
     if (wave >= 4) {
-        fetch_chunks<T, D>(buffers, a, bh, len, 0, 1, chunks, (const T *)a.v + (size_t)h * a.M + m0, a.ldv, cols, tid - 256);
+        fetch_chunks<T, D, !kOutputs, false>(buffers, a, task, (const T *)a.v, a.ldv, tid - 256);
         return;
     }
-    if (wave * 16 >= cols) {                                 // no columns (M is a multiple of 16)
-        if (chunks > 0) __syncthreads();
-        for (int chunk = 0; chunk < chunks; ++chunk) __syncthreads();
+    if (wave * 16 >= task.cols) {                            // no columns (M is a multiple of 16)
+        if (count > 0) __syncthreads();
+        for (int i = 0; i < count; ++i) __syncthreads();
         return;
     }
     f32x4 S[D / 16];
-    load_state<D>(a.h0 == nullptr ? nullptr : a.h0 + state, m, a.M, g, S);
+    const float *from = task.start ? (a.h0 == nullptr ? nullptr : a.h0 + state) : kOutputs ? a.piece_state + piece * D * a.M : nullptr;
+    load_state<D>(from, m, a.M, g, S);
+    if (kKind == kTransitions && task.unit) {
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = paired(t, 4 * g + r) == m ? 1.0f : 0.0f;
+    }
     loads_done();
     Parts<3> sp[kSteps];                                     // the state as an operand
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) sp[s] = cut(S[2 * s], S[2 * s + 1]);
-    if (chunks > 0) __syncthreads();
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        const long unit = (long)bh * a.K + chunk;
+    const int most = a.o == nullptr ? 0 : C;                 // no outputs are asked for: stores go nowhere
+    if (count > 0) __syncthreads();
+    for (int i = 0; i < count; ++i) {
+        const int chunk = task.first + i;
+        const long unit = (long)task.bh * a.K + chunk;
         const size_t row0 = seq + (size_t)chunk * C;
         const int left = len - chunk * C;
-        const Chunked<T, D> &in = buffers[chunk & 1];
+        const Chunked<T, D> &in = buffers[i & 1];
         const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
         const auto rows = [&](const uint16_t *mat, int s, Parts<P> (&f)[kTiles]) {
 #pragma unroll
@@ -217,7 +226,7 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
         for (int s = 0; s < kSteps; ++s) {
             if (s + 1 < kSteps) rows(in.k, s + 1, f[(s + 1) % 2]);
             else {
-                rows(in.q, 0, f[kSteps % 2]);
+                if (kOutputs) rows(in.q, 0, f[kSteps % 2]);
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     v[t] = column_values<kCols, P>(in.v, C * kCols, paired(t, 4 * g), wave, lane);
@@ -234,12 +243,14 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
         for (int t = 0; t < kTiles; ++t) rest[t] = v[t].sum() - since[t] * ks[t];
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(strength[2 * s] * rest[2 * s]), finite(strength[2 * s + 1] * rest[2 * s + 1]));
+        if constexpr (kOutputs) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s + 1 < kSteps) rows(in.q, s + 1, f[(kSteps + s + 1) % 2]);
-            products(f[(kSteps + s) % 2], first<kOut>(sp[s]), qs);
+            for (int s = 0; s < kSteps; ++s) {
+                if (s + 1 < kSteps) rows(in.q, s + 1, f[(kSteps + s + 1) % 2]);
+                products(f[(kSteps + s) % 2], first<kOut>(sp[s]), qs);
+            }
+            side_by_side<kSteps * kTiles * (P == 1 ? 2 : 6)>();
         }
-        side_by_side<kSteps * kTiles * (P == 1 ? 2 : 6)>();
         in_this_order();
         // ... and of what the chunk's earlier tokens write
 #pragma unroll
@@ -254,8 +265,9 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             qs[t] *= since[t];
+            if constexpr (kOutputs)
 #pragma unroll
-            for (int i = 0; i <= t / 2; ++i) mf[t][i] = row_operand<32, kOut>(in.m, Ch::kTri, tri_row<C>(paired(t, c), i), g);
+                for (int i = 0; i <= t / 2; ++i) mf[t][i] = row_operand<32, kOut>(in.m, Ch::kTri, tri_row<C>(paired(t, c), i), g);
             since[t] = gate4(1, t);
         }
 #pragma unroll
@@ -267,8 +279,9 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
         }
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) rest[t] = finite(strength[t] * rest[t]);
+        if constexpr (kOutputs)
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s) u[s] = cut_to<kOut>(rest[2 * s], rest[2 * s + 1]);
+            for (int s = 0; s < kBlocks; ++s) u[s] = cut_to<kOut>(rest[2 * s], rest[2 * s + 1]);
         constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;      // tiles of the state at a time
         Parts<P> kt[2][kGroup];
         const auto columns = [&](int n) {                    // n counts (group, block)
@@ -277,15 +290,15 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
         };
         in_this_order();
         columns(0);
-        lower_products<kOut - 1>(mf, u, qs);
+        if constexpr (kOutputs) lower_products<kOut - 1>(mf, u, qs);
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(since[2 * s] * rest[2 * s]), finite(since[2 * s + 1] * rest[2 * s + 1]));
         const float whole = in.gates[C - 1];
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) S[t] *= whole;
-        side_by_side<(kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
+        if (kOutputs) side_by_side<(kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
         in_this_order();
-        const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, a.o == nullptr ? 0 : left < C ? left : C, ldo, a.M);
+        const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, left < most ? left : most, ldo, a.M);
 #pragma unroll
         for (int n = 0; n < kGroups * kBlocks; ++n) {
             if (n + 1 < kGroups * kBlocks) columns(n + 1);
@@ -295,7 +308,7 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
             products(kt[n % 2], x[n % kBlocks], part);
 #pragma unroll
             for (int t = 0; t < kGroup; ++t) S[n / kBlocks * kGroup + t] = part[t];
-            if (n == 0) {
+            if (kOutputs && n == 0) {
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) store_tile<T>(r, paired(t, 4 * g), m - c, ldo, a.scale * qs[t], lane);
             }
@@ -313,9 +326,92 @@ template <typename T, int D, bool kKeep> __global__ __launch_bounds__(512) void 
         for (int i = (kGroups - 1) * kGroup / 2; i < kSteps; ++i) sp[i] = cut(S[2 * i], S[2 * i + 1]);
         __syncthreads();
     }
-    if (a.h1 != nullptr) store_state<D>(a.h1 + state, m - c, a.M, lane, S);
-    if (a.o != nullptr)                                      // tokens behind the sequence
-        for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.o + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);
+    if constexpr (kOutputs) {
+        if (!task.end) return;
+        if (a.h1 != nullptr) store_state<D>(a.h1 + state, m - c, a.M, lane, S);
+        if (a.o != nullptr)                                  // tokens behind the sequence
+            for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.o + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);
+    } else if (task.unit) {
+        store_state<D>(a.transition + piece * D * D, m - c, D, lane, S);
+    } else {
+        store_state<D>(a.piece_state + (piece + 1) * D * a.M, m - c, a.M, lane, S);
+    }
+}
+
+// ---- from piece to piece -----------------------------------------------------------------------------
+// Forwards S_{j+1} = F_j S_j + (what piece j leaves of a zero state), j = 1 .. last - 1; backwards E_{j-1} = F_j^T E_j + .., j = last - 1
+// .. 1.  64 columns a workgroup; a wave has some rows of the transitions F, on their way a piece ahead, and all of the
+// columns, which the waves hand each other through LDS.
+template <int D, bool kBack> __global__ __launch_bounds__(256) void delta_join_kernel(const DeltaArgs a, float *states, int C) {
+    constexpr int kEach = D <= 64 ? 1 : D / 64, kSteps = D / 32;
+    __shared__ alignas(16) uint16_t sS[2][3 * kCols * D];
+    const int blocks = (a.M + kCols - 1) / kCols, bh = blockIdx.x / blocks, m0 = blockIdx.x % blocks * kCols;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16;
+    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, chunks = (length_of(a, bh / a.H) + C - 1) / C, last = chunks > 0 ? (chunks - 1) / a.length : 0;
+    const bool mine = wave * kEach * 16 < D;                 // of 32 rows two waves have none
+    float *state = states + (size_t)bh * a.pieces * D * a.M;
+    const float *transition = a.transition + (size_t)bh * a.pieces * D * D;
+    const int count = last - 1;
+    if (count <= 0) return;
+    const auto from = [&](int i) { return kBack ? last - 1 - i : 1 + i; };              // the i-th piece, and the state it starts from
+    f32x4 rows[kEach][kSteps][2];
+    const auto load_rows = [&](int piece) {
+        const float *f = transition + (size_t)piece * D * D;
+#pragma unroll
+        for (int x = 0; x < kEach; ++x)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int row = mine ? 16 * (wave * kEach + x) + c : c, at = 32 * s + 8 * g;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) rows[x][s][i / 4][i % 4] = kBack ? f[(at + i) * D + row] : f[row * D + at + i];
+            }
+    };
+    const auto park = [&](uint16_t *to, int x, int ct, f32x4 v) {                       // rows 4g .. of the tile, column 16 ct + c
+        const float q[4] = {v[0], v[1], v[2], v[3]};
+        const Split3 p = split3(q);
+        const int row = 16 * (wave * kEach + x) + 4 * g, at = mat_at<D, true>(16 * ct + c, row / 8) + row % 8;
+        *reinterpret_cast<u32x2_t *>(to + at) = p.h;
+        *reinterpret_cast<u32x2_t *>(to + kCols * D + at) = p.m;
+        *reinterpret_cast<u32x2_t *>(to + 2 * kCols * D + at) = p.l;
+    };
+    const auto load_tile = [&](const float *s, int x, int ct) {
+        const Range r = range_of(s, mine ? D : 0, a.M, a.M);
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, ((16 * (wave * kEach + x) + 4 * g + i) * a.M + m0 + 16 * ct + c) * 4, 0, 0));
+        return v;
+    };
+    load_rows(from(0));
+#pragma unroll
+    for (int x = 0; x < kEach; ++x)
+        for (int ct = 0; 16 * ct < cols; ++ct) {
+            const f32x4 v = load_tile(state + (size_t)from(0) * D * a.M, x, ct);
+            if (mine) park(sS[0], x, ct, v);
+        }
+    __syncthreads();
+    for (int i = 0; i < count; ++i) {
+        const int piece = from(i), to = kBack ? piece - 1 : piece + 1;
+        Parts<3> f[kEach][kSteps];
+#pragma unroll
+        for (int x = 0; x < kEach; ++x)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) f[x][s] = cut(rows[x][s][0], rows[x][s][1]);
+        load_rows(from(i + 1 < count ? i + 1 : i));
+        for (int ct = 0; 16 * ct < cols; ++ct) {
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) {
+                f32x4 v = load_tile(state + (size_t)to * D * a.M, x, ct);
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) v = product(f[x][s], row_operand<D, 3, true>(sS[i & 1], kCols * D, 16 * ct + c, 4 * s + g), v);
+                if (mine) {
+                    park(sS[(i + 1) & 1], x, ct, v);
+                    store_tile<float>(range_of(state + (size_t)to * D * a.M, D, a.M, a.M), 16 * (wave * kEach + x) + 4 * g, m0 + 16 * ct, a.M, v, lane);
+                }
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // ---- one token ------------------------------------------------------------------------------------------
@@ -371,11 +467,26 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_step_k
 }
 }  // namespace
 
+void launch_join(const DeltaArgs &a, int dtype, bool back, hipStream_t s) {
+    const unsigned grid = (unsigned)(a.B * a.H * ((a.M + kCols - 1) / kCols));
+    const int C = delta_chunk(dtype);
+    float *states = back ? a.piece_dstate : a.piece_state;
+#define LA_JOIN(D) back ? delta_join_kernel<D, true><<<grid, 256, 0, s>>>(a, states, C) : delta_join_kernel<D, false><<<grid, 256, 0, s>>>(a, states, C)
+    if (a.D == 32) LA_JOIN(32);
+    else if (a.D == 64) LA_JOIN(64);
+    else LA_JOIN(128);
+}
+
 hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
     const unsigned units = (unsigned)((long)a.B * a.H * a.K);
 #define LA_LOCAL(T, D) delta_local_kernel<T, D><<<units, 256, 0, s>>>(a)
     LA_BY_WIDTH(LA_LOCAL)
-#define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, true><<<head_grid(a), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, false><<<head_grid(a), 512, 0, s>>>(a)
+    if (a.pieces > 1) {
+#define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<task_grid(a, kTransitions), 512, 0, s>>>(a)
+        LA_BY_WIDTH(LA_PIECES)
+        if (a.pieces > 2) launch_join(a, dtype, false, s);
+    }
+#define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, kWhole, true><<<task_grid(a, kWhole), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, kWhole, false><<<task_grid(a, kWhole), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_PASS)
     return hipGetLastError();
 }

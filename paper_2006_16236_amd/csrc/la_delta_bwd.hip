@@ -20,36 +20,38 @@ namespace la {
 namespace {
 
 // As the forward: 16 columns of dS' a wave; products that y does not wait for (Q^T e^G dO) run beside the cutting of values.
-template <typename T, int D> __global__ __launch_bounds__(512) void delta_states_bwd_kernel(const DeltaArgs a) {
+template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) void delta_states_bwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kSteps = D / 32;
+    constexpr bool kOutputs = kKind == kWhole;
     __shared__ Chunked<T, D> buffers[2];
-    int bh, m0;
-    if (!head_and_columns(a, bh, m0)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16, m = m0 + wave * 16 + c;
-    const int b = bh / a.H, h = bh % a.H, len = length_of(a, b), chunks = (len + C - 1) / C;
-    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, ldo = a.H * a.M;
-    const size_t seq = (size_t)b * a.N, state = (size_t)bh * D * a.M;
+    Task task;
+    if (!task_of<kKind, true>(a, C, D, task)) return;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, m = task.m0 + wave * 16 + c;
+    const int h = task.h, len = task.len, count = task.count, ldo = a.H * a.M;
+    const size_t seq = (size_t)task.b * a.N, state = (size_t)task.bh * D * a.M, piece = (size_t)task.bh * a.pieces + task.piece;
     if (wave >= 4) {
-        fetch_chunks<T, D>(buffers, a, bh, len, chunks - 1, -1, chunks, (const T *)a.dO + (size_t)h * a.M + m0, ldo, cols, tid - 256);
+        fetch_chunks<T, D, false, true>(buffers, a, task, (const T *)a.dO, ldo, tid - 256);
         return;
     }
-    if (wave * 16 >= cols) {
-        if (chunks > 0) __syncthreads();
-        for (int chunk = 0; chunk < chunks; ++chunk) __syncthreads();
+    if (wave * 16 >= task.cols) {
+        if (count > 0) __syncthreads();
+        for (int i = 0; i < count; ++i) __syncthreads();
         return;
     }
     f32x4 S[D / 16];                                         // dS'
-    load_state<D>(a.dh1 == nullptr ? nullptr : a.dh1 + state, m, a.M, g, S);
+    const float *from = task.end ? (a.dh1 == nullptr ? nullptr : a.dh1 + state) : kOutputs ? a.piece_dstate + piece * D * a.M : nullptr;
+    load_state<D>(from, m, a.M, g, S);
     loads_done();
     Parts<3> sp[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) sp[s] = cut(S[2 * s], S[2 * s + 1]);
-    for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.dv + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);      // tokens behind the sequence
-    if (chunks > 0) __syncthreads();
-    for (int i = 0; i < chunks; ++i) {
-        const int chunk = chunks - 1 - i, left = len - chunk * C;
-        const long unit = (long)bh * a.K + chunk;
+    if (kOutputs && task.end)
+        for (int n = len + g; n < a.N; n += 4) store_elem<false>((T *)a.dv + (seq + n) * ldo + (size_t)h * a.M + m, 0.0f);      // tokens behind the sequence
+    if (count > 0) __syncthreads();
+    for (int i = 0; i < count; ++i) {
+        const int chunk = task.first + count - 1 - i, left = len - chunk * C;
+        const long unit = (long)task.bh * a.K + chunk;
         const Chunked<T, D> &in = buffers[i & 1];
         const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
         f32x4 y[kTiles], w[kTiles];
@@ -70,7 +72,7 @@ template <typename T, int D> __global__ __launch_bounds__(512) void delta_states
         rows(0);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) y[t] = w[t] = f32x4{0, 0, 0, 0};
-        store_state<D>(a.dstate + (size_t)unit * D * a.M, m - c, a.M, lane, S);
+        if constexpr (kOutputs) store_state<D>(a.dstate + (size_t)unit * D * a.M, m - c, a.M, lane, S);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             if (s + 1 < kSteps) rows(s + 1);
@@ -137,7 +139,7 @@ template <typename T, int D> __global__ __launch_bounds__(512) void delta_states
         for (int n = 0; n < kGroups * kBlocks; ++n) {
             if (n + 1 < kGroups * kBlocks) columns(in.k, n + 1);
             update(n, x[n % kBlocks]);
-            if (n == 0) {
+            if (kOutputs && n == 0) {
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     store_tile<float>(wr, paired(t, 4 * g), m - c, a.M, y[t], lane);
@@ -158,7 +160,8 @@ template <typename T, int D> __global__ __launch_bounds__(512) void delta_states
         for (int j = (kGroups - 1) * kGroup / 2; j < kSteps; ++j) sp[j] = cut(S[2 * j], S[2 * j + 1]);
         __syncthreads();
     }
-    if (a.dh0 != nullptr) store_state<D>(a.dh0 + state, m - c, a.M, lane, S);
+    if constexpr (!kOutputs) store_state<D>(a.piece_dstate + (piece - 1) * D * a.M, m - c, a.M, lane, S);
+    else if (task.start && a.dh0 != nullptr) store_state<D>(a.dh0 + state, m - c, a.M, lane, S);
 }
 
 // A workgroup takes one chunk and the heads that share its queries and keys, one after the other; a wave has kSlabs times 16
@@ -480,7 +483,12 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
 }  // namespace
 
 hipError_t launch_delta_bwd(const DeltaArgs &a, int dtype, hipStream_t s) {
-#define LA_STATES(T, D) delta_states_bwd_kernel<T, D><<<head_grid(a), 512, 0, s>>>(a)
+    if (a.pieces > 1) {
+#define LA_PIECES(T, D) delta_states_bwd_kernel<T, D, kStates><<<task_grid(a, kStates), 512, 0, s>>>(a)
+        LA_BY_WIDTH(LA_PIECES)
+        if (a.pieces > 2) launch_join(a, dtype, true, s);
+    }
+#define LA_STATES(T, D) delta_states_bwd_kernel<T, D, kWhole><<<task_grid(a, kWhole), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_STATES)
     const unsigned units = (unsigned)((long)a.B * a.Hk * a.K);
 #define LA_CHUNKS(T, D) a.H > a.Hk ? delta_chunks_bwd_kernel<T, D, true><<<units, D == 32 ? 128 : 256, 0, s>>>(a) : delta_chunks_bwd_kernel<T, D, false><<<units, D == 32 ? 128 : 256, 0, s>>>(a)

@@ -5,6 +5,7 @@
 #include <stddef.h>
 
 #include "../../include/la.h"
+#include "la_delta_cut.h"
 #include "la_layer.h"
 
 namespace la {
@@ -37,8 +38,11 @@ struct DeltaArgs {
     float *state;                    // [unit][D][M]: the state before each chunk, or NULL
     float *write;                    // [unit][C][M]: backward, the gradient of what a token writes
     float *dstate;                   // [unit][D][M]: backward, the gradient of the state behind each chunk
+    float *piece_state;              // [B H][pieces][D][M]: of a cut sequence, the state before each piece
+    float *transition;               // [B H][pieces][D][D]: what a piece makes of the state before it
+    float *piece_dstate;             // [B H][pieces][D][M]: backward, the gradient of the state behind each piece
     long ldq, ldk, ldv;
-    int B, N, H, Hk, D, M, K;
+    int B, N, H, Hk, D, M, K, pieces, length;      // length: chunks a piece
     float scale;
 };
 // the lower 32 x 32 blocks of a C x C matrix, those of a block column behind each other
@@ -47,6 +51,8 @@ inline int delta_chunk(int dtype) { return dtype == 0 ? 32 : 64; }
 // chunk-local matrices, then outputs, states and what is kept (o, h1, miss, state: each may be NULL)
 hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s);
 hipError_t launch_delta_bwd(const DeltaArgs &a, int dtype, hipStream_t s);
+// the states before (behind) the pieces of cut sequences from those that each piece leaves of none
+void launch_join(const DeltaArgs &a, int dtype, bool back, hipStream_t s);
 // one token of every sequence: h [B, H, D, M] in and out
 hipError_t launch_delta_step(const DeltaArgs &a, float *h, int dtype, hipStream_t s);
 

@@ -47,12 +47,13 @@ int delta_sizes(int B, int N, int H, int Hk, int D, int M, la_dtype t, int flags
     const int C = la::delta_chunk(t);
     if ((double)H * M > kMostApart || (double)Hk * D > kMostApart || (double)B * N * H * (M > D ? M : D) >= kMostElements) return LA_ERR_SHAPE;
     if (((double)B * H + 8) * ((N + (double)C - 1) / C) >= kMostUnits || ((double)B * H + 8) * ((M + 63) / 64) >= kMostUnits) return LA_ERR_SHAPE;
+    // a sequence is cut only where its pieces are at most 64 and there are few of them: their grids are far smaller
     return LA_OK;
 }
 bool bad_apart(int ld, int width) { return ld < width || ld > kMostApart; }
 struct Delta {
     la::DeltaArgs a{};
-    size_t tri, gate, rows, state;
+    size_t tri, gate, rows, state, pieces, transitions;
     Delta(int B, int N, int H, int Hk, int D, int M, float scale, la_dtype t) {
         const int C = la::delta_chunk(t);
         a.B = B, a.N = N, a.H = H, a.Hk = Hk, a.D = D, a.M = M, a.scale = scale;
@@ -62,10 +63,17 @@ struct Delta {
         gate = units * 4 * C * sizeof(float);
         rows = units * C * M * sizeof(float);
         state = units * D * M * sizeof(float);
+        const la::DeltaCut cut = la::delta_cut_of((long)B * H, D, M, a.K);
+        a.pieces = cut.pieces, a.length = cut.length;
+        const size_t cuts = cut.pieces > 1 ? (size_t)B * H * cut.pieces : 0;
+        pieces = cuts * D * M * sizeof(float), transitions = cuts * D * D * sizeof(float);
     }
-    size_t fwd_bytes(bool keep) const { return align256(tri) + align256(gate) + (keep ? align256(rows) + align256(state) : 0); }
-    size_t bwd_bytes(bool given) const { return align256(rows) + align256(state) + (given ? 0 : fwd_bytes(true)); }
+    size_t fwd_bytes(bool keep) const {
+        return align256(tri) + align256(gate) + align256(pieces) + align256(transitions) + (keep ? align256(rows) + align256(state) : 0);
+    }
+    size_t bwd_bytes(bool given) const { return align256(rows) + align256(state) + align256(pieces) + (given ? 0 : fwd_bytes(true)); }
     void carve_fwd(Carver &cv, bool keep) {
+        a.piece_state = static_cast<float *>(cv.take(pieces)), a.transition = static_cast<float *>(cv.take(transitions));
         a.tri = static_cast<float *>(cv.take(tri)), a.gate = static_cast<float *>(cv.take(gate));
         if (keep) a.miss = static_cast<float *>(cv.take(rows)), a.state = static_cast<float *>(cv.take(state));
     }
@@ -181,6 +189,7 @@ int la_delta_bwd(const void *q, int ldq, const void *k, int ldk, const void *v, 
     a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
     Carver cv{static_cast<char *>(ws), 0};
     a.write = static_cast<float *>(cv.take(d.rows)), a.dstate = static_cast<float *>(cv.take(d.state));
+    a.piece_dstate = static_cast<float *>(cv.take(d.pieces));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (given) {
         Carver kept{static_cast<char *>(const_cast<void *>(fwd_ws)), 0};     // read only
