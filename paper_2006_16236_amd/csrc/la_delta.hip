@@ -374,42 +374,54 @@ template <int D, bool kBack> __global__ __launch_bounds__(256) void delta_join_k
         *reinterpret_cast<u32x2_t *>(to + kCols * D + at) = p.m;
         *reinterpret_cast<u32x2_t *>(to + 2 * kCols * D + at) = p.l;
     };
-    const auto load_tile = [&](const float *s, int x, int ct) {
-        const Range r = range_of(s, mine ? D : 0, a.M, a.M);
-        f32x4 v;
+    constexpr int kColTiles = kCols / 16;
+    f32x4 v[kColTiles][kEach];
+    const auto load_tiles = [&](int piece) {                 // what is there of its state; zeros in columns that are none
+        const Range r = range_of(state + (size_t)piece * D * a.M, mine ? D : 0, a.M, a.M);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, ((16 * (wave * kEach + x) + 4 * g + i) * a.M + m0 + 16 * ct + c) * 4, 0, 0));
-        return v;
+        for (int ct = 0; ct < kColTiles; ++ct)
+#pragma unroll
+            for (int x = 0; x < kEach; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 16 * ct + c < cols ? ((16 * (wave * kEach + x) + 4 * g + i) * a.M + m0 + 16 * ct + c) * 4 : 0x7fffff00;
+                    v[ct][x][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+                }
     };
     load_rows(from(0));
+    load_tiles(from(0));
+    if (mine)
 #pragma unroll
-    for (int x = 0; x < kEach; ++x)
-        for (int ct = 0; 16 * ct < cols; ++ct) {
-            const f32x4 v = load_tile(state + (size_t)from(0) * D * a.M, x, ct);
-            if (mine) park(sS[0], x, ct, v);
-        }
+        for (int ct = 0; ct < kColTiles; ++ct)
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) park(sS[0], x, ct, v[ct][x]);
     __syncthreads();
     for (int i = 0; i < count; ++i) {
         const int piece = from(i), to = kBack ? piece - 1 : piece + 1;
+        load_tiles(to);
         Parts<3> f[kEach][kSteps];
 #pragma unroll
         for (int x = 0; x < kEach; ++x)
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) f[x][s] = cut(rows[x][s][0], rows[x][s][1]);
         load_rows(from(i + 1 < count ? i + 1 : i));
-        for (int ct = 0; 16 * ct < cols; ++ct) {
+        const Range r = range_of(state + (size_t)to * D * a.M, mine ? D : 0, a.M, a.M);
 #pragma unroll
-            for (int x = 0; x < kEach; ++x) {
-                f32x4 v = load_tile(state + (size_t)to * D * a.M, x, ct);
+        for (int ct = 0; ct < kColTiles; ++ct) {
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) v = product(f[x][s], row_operand<D, 3, true>(sS[i & 1], kCols * D, 16 * ct + c, 4 * s + g), v);
-                if (mine) {
-                    park(sS[(i + 1) & 1], x, ct, v);
-                    store_tile<float>(range_of(state + (size_t)to * D * a.M, D, a.M, a.M), 16 * (wave * kEach + x) + 4 * g, m0 + 16 * ct, a.M, v, lane);
-                }
+            for (int s = 0; s < kSteps; ++s) {
+                const Parts<3> y = row_operand<D, 3, true>(sS[i & 1], kCols * D, 16 * ct + c, 4 * s + g);
+#pragma unroll
+                for (int x = 0; x < kEach; ++x) v[ct][x] = product(f[x][s], y, v[ct][x]);
             }
         }
+#pragma unroll
+        for (int ct = 0; ct < kColTiles; ++ct)
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) {
+                if (mine) park(sS[(i + 1) & 1], x, ct, v[ct][x]);
+                if (16 * ct < cols) store_tile<float>(r, 16 * (wave * kEach + x) + 4 * g, m0 + 16 * ct, a.M, v[ct][x], lane);
+            }
         __syncthreads();
     }
 }
