@@ -219,3 +219,85 @@ def selective_scan(x, dt, A, Bt, Ct, D=None, z=None, dt_bias=None, state=None, l
     inputs = (x, dt, A, Bt, Ct, D, z, dt_bias, state)
     keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)   # the states a backward needs
     return _SelectiveScan.apply(*inputs, lengths, bool(softplus), keep)
+
+
+# ---- the gated delta rule and what stands before it --------------------------------------------------
+
+class _QkNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, freq, pos, lengths, norm, adjacent, eps):
+        ctx.set_materialize_grads(False)
+        q, k = _rows(q), _rows(k)
+        wq, wk, freq, pos, lengths = (_dense(t) for t in (wq, wk, freq, pos, lengths))
+        yq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        yk = None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        _l.la_qk_fwd(q, yq, k=k, yk=yk, wq=wq, wk=wk, freq=freq, pos=pos, lengths=lengths, norm=norm, adjacent=adjacent, eps=eps)
+        ctx.save_for_backward(q, k, wq, wk, freq, pos, lengths)
+        ctx.how = dict(norm=norm, adjacent=adjacent, eps=eps)
+        return yq if k is None else (yq, yk)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dyq, dyk=None):
+        q, k, wq, wk, freq, pos, lengths = ctx.saved_tensors
+        if dyq is None and dyk is None:
+            return (None,) * 10
+        need = ctx.needs_input_grad
+        dyq = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if dyq is None else _dense(dyq)
+        dq, dk = torch.empty(q.shape, dtype=q.dtype, device=q.device), None
+        if k is not None:
+            dyk = torch.zeros(k.shape, dtype=k.dtype, device=k.device) if dyk is None else _dense(dyk)
+            dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        dwq, dwk = _wanted(need[2], wq), _wanted(need[3], wk)
+        _l.la_qk_bwd(q, dyq, dq, k=k, dyk=dyk, dk=dk, wq=wq, wk=wk, freq=freq, pos=pos, lengths=lengths, dwq=dwq, dwk=dwk, **ctx.how)
+        return dq, dk, dwq, dwk, None, None, None, None, None, None
+
+
+def qk_norm(q, k=None, wq=None, wk=None, freq=None, pos=None, lengths=None, norm="rms", adjacent: bool = False, eps: float = 1e-6):
+    """(q, k) with each head of q [B, N, H, D] and k [B, N, Hk, D] normed ("rms", "l2" for unit length, or None) and weighted with wq, wk
+    [D] fp32, and its first 2 len(freq) elements turned by pos * freq: pairs i and i + len(freq), or neighbours.  pos [B, N] int32 (None:
+    0 .. N - 1), lengths [B] int32: rows behind it are zero.  Without k, q alone.  Differentiable in q, k, wq, wk."""
+    return _QkNorm.apply(q, k, wq, wk, freq, pos, lengths, norm, bool(adjacent), float(eps))
+
+
+def _rows8(t):
+    """As _rows, the tokens a multiple of eight elements apart."""
+    t = _rows(t)
+    return t if t.shape[1] == 1 and t.shape[0] == 1 or t.stride(1 if t.shape[1] > 1 else 0) % 8 == 0 else _dense(t.clone(memory_format=torch.contiguous_format))
+
+
+class _GatedDelta(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, g, beta, state, lengths, scale, keep):
+        ctx.set_materialize_grads(False)
+        q, k, v = (_rows8(t) for t in (q, k, v))
+        g, beta, state, lengths = (_dense(t) for t in (g, beta, state, lengths))
+        o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        h1 = torch.empty((v.shape[0], v.shape[2], q.shape[3], v.shape[3]), dtype=torch.float32, device=v.device)
+        ws = _l.la_delta_fwd(q, k, v, g, beta, o, h0=state, h1=h1, lengths=lengths, scale=scale, keep=keep)
+        ctx.save_for_backward(q, k, v, g, beta, state, lengths, ws if keep else None)
+        ctx.scale = scale
+        return o, h1
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do, dh1):
+        q, k, v, g, beta, state, lengths, ws = ctx.saved_tensors
+        if do is None and dh1 is None:
+            return (None,) * 9
+        do = torch.zeros(v.shape, dtype=v.dtype, device=v.device) if do is None else _dense(do)
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dg, dbeta, dh0 = None if g is None else _new(g), _new(beta), _wanted(ctx.needs_input_grad[5], state)
+        _l.la_delta_bwd(q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, h0=state, dh1=_dense(dh1), dh0=dh0, lengths=lengths, scale=ctx.scale,
+                        fwd_ws=ws)
+        return dq, dk, dv, dg, dbeta, dh0, None, None, None
+
+
+def gated_delta(q, k, v, g, beta, state=None, lengths=None, scale=None):
+    """(o, next state): gated delta rule of q, k [B, N, Hk, D] (keys of about unit length, see qk_norm), v [B, N, H, M] with logarithms of
+    the decay g (or None) and strengths beta [B, N, H] fp32; H / Hk neighbouring states share a head of q, k.  state [B, H, D, M] fp32:
+    that before the first token (None: zero); the next one continues the sequence here or in la_delta_step.  scale (None: D ** -0.5) is
+    that of the outputs.  lengths as in causal_conv."""
+    inputs = (q, k, v, g, beta, state)
+    keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)      # what a backward starts from
+    return _GatedDelta.apply(*inputs, lengths, None if scale is None else float(scale), keep)

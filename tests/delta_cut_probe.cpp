@@ -1,0 +1,16 @@
+// The cut of the gated delta rule (csrc/la_delta_cut.h) on its own: reads sizes from stdin, prints how sequences are cut.
+//   in   heads D M chunks
+//   out  pieces length
+#include <cstdio>
+
+#include "../paper_2006_16236_amd/csrc/la_delta_cut.h"
+
+int main() {
+    long heads;
+    int D, M, chunks;
+    while (std::scanf("%ld %d %d %d", &heads, &D, &M, &chunks) == 4) {
+        const la::DeltaCut c = la::delta_cut_of(heads, D, M, chunks);
+        std::printf("%d %d\n", c.pieces, c.length);
+    }
+    return 0;
+}
