@@ -182,7 +182,8 @@ template <typename T, int G> __global__ __launch_bounds__(256) void qk_bwd_kerne
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 f0[i] *= inv, f1[i] *= inv;
-                const float s0 = real ? g0[i] * f0[i] : 0.0f, s1 = real ? g1[i] * f1[i] : 0.0f;
+                // a place without a head has no length either: 0 * inf with eps = 0
+                const float s0 = live && real ? g0[i] * f0[i] : 0.0f, s1 = live && real ? g1[i] * f1[i] : 0.0f;
                 sq[i] += isq ? s0 : 0.0f, sq[4 + i] += isq ? s1 : 0.0f;
                 sk[i] += isq ? 0.0f : s0, sk[4 + i] += isq ? 0.0f : s1;
                 g0[i] *= isq ? wq[i] : wk[i], g1[i] *= isq ? wq[4 + i] : wk[4 + i];

@@ -73,6 +73,19 @@ def test_qk(case, dtype):
         check("dw" + name, host(got["dw" + name]), want["dw"], mag["dw"], "f32", 2 * k + 64 + 80 + (tokens / 1024 + 1) * (heads + 1))
 
 
+@pytest.mark.parametrize("kind", ["rms", "l2"])
+def test_gradients_without_eps(kind, monkeypatch):
+    """eps = 0: what is left over of a wave's places for heads, three of sixteen here, has no length to divide by."""
+    monkeypatch.setattr(f"{__name__}.EPS", 0.0)
+    c = Case("f32", 2, 5, 2, 1, 24, 16, kind, True, False, None, 0, True)
+    got = c.run()
+    for name, x, w, dy in (("q", c.q, c.wq, c.dyq), ("k", c.k, c.wk, c.dyk)):
+        args = (x, w, c.freq, c.pos, None, kind, False, 0.0, dy)
+        want, mag = ref.qk(*args), ref.qk(*args, mag=True)
+        check("d" + name, host(got["d" + name]), want["dx"], mag["dx"], "f32", 2 * 20 + 14)       # as above
+        check("dw" + name, host(got["dw" + name]), want["dw"], mag["dw"], "f32", 2 * 20 + 64 + 80 + 2)
+
+
 def test_a_single_tensor_without_anything():
     d = Data(3, "f32")
     x = d.array(2, 5, 3, 24)
