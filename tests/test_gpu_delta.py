@@ -170,6 +170,17 @@ def test_outputs_before_a_token_do_not_depend_on_it(dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_decay_that_is_no_number_shows(dtype):
+    c = Case(18, dtype, 1, 130, 2, 1, 64, 48)
+    x, more = c.inputs()
+    x[3][0, 40, 0] = float("nan")
+    out, _, _ = c.outputs()
+    la.la_delta_fwd(*x, **out, **more)
+    assert out["o"][0, 40:, 0].isnan().all() and out["h1"][0, 0].isnan().all()
+    assert not out["o"][0, :40].isnan().any() and not out["o"][0, :, 1].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_behind_a_sequence_may_hold_anything(dtype):
     c = Case(13, dtype, 3, 100, 2, 1, 64, 48, [100, 33, 0])
     a = c.run()
