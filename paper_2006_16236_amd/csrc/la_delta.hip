@@ -19,11 +19,12 @@ namespace la {
 namespace {
 
 // ---- chunk-local matrices ------------------------------------------------------------------------
-// One workgroup a unit: decays, masked products of queries and keys, and the triangular system by blocks of 16.  The inverse
-// t = (1 + A beta)^-1 of the diagonal blocks comes by substitution, one block in each lane group and one column a lane, the
-// blocks below it from those above, t_ij = -t_ii sum_k (A beta)_ik t_kj, a diagonal at a time, and Z = t A.  All in fp32
-// (v_mfma_f32_16x16x4: lane (c, g) supplies elements 4g + q of its row c, register q of a result is that of the next operand).
-// One wave with a column of Z a lane, 2016 dependent steps, took 25 us instead of 14 for one chunk of 64 sequences.
+// One workgroup a unit: decays, masked products of queries and keys, and the triangular system (1 + A beta) Z = A by blocks
+// of 16.  The inverse of the diagonal blocks comes by substitution, one block in each lane group and one column a lane; then a
+// wave has a block column of Z, Z_ij = (1 + A beta)_ii^-1 (A_ij - sum_k (A beta)_ik Z_kj), whose products feed each other in
+// registers.  All in fp32 (v_mfma_f32_16x16x4: lane (c, g) supplies elements 4g + q of its row c, register q of a result is that
+// of the next operand).  Every step waits for the one before, so what counts is how many workgroups a compute unit holds: four (three
+// of 128 columns).  8 x 2048 x 16 heads of 128 bf16: 63 us, 3.8 TB/s of tokens and matrices; one chunk of 64 x 8 heads of 64: 10.
 constexpr int kTriStride = 68;                               // floats between rows: 16 rows' 16-byte reads meet all banks
 __device__ __forceinline__ f32x4 times(f32x4 rows, f32x4 columns, f32x4 acc) {
 #pragma unroll
@@ -40,7 +41,17 @@ __device__ __forceinline__ f32x4 block_columns(const float *m, int i, int j, int
     for (int q = 0; q < 4; ++q) v[q] = m[(16 * i + 4 * g + q) * kTriStride + 16 * j + c];
     return v;
 }
-template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_kernel(const DeltaArgs a) {
+// of the lane n places before in its row of 16 (zero without one), and of one lane
+template <int n> __device__ __forceinline__ double lane_before(double v) {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], 0x110 + n, 0xf, 0xf, true),
+                                              (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], 0x110 + n, 0xf, 0xf, true)});
+}
+__device__ __forceinline__ double value_of(double v, int lane) {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_readlane((int)w[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane)});
+}
+template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4) void delta_local_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kTokens = 2 * P * C * D * (int)sizeof(uint16_t), kTri = C * kTriStride * (int)sizeof(float);
     __shared__ alignas(16) char space[kTokens > kTri ? kTokens : kTri];
@@ -48,9 +59,9 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
     __shared__ alignas(16) float gh[C], gl[C], bt[C];
     uint16_t *kS = reinterpret_cast<uint16_t *>(space), *qS = kS + P * C * D;
     float *inv = reinterpret_cast<float *>(space);           // takes their place
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c = lane % 16, g = lane / 16;
-    const long unit = blockIdx.x;
-    const int chunk = (int)(unit % a.K), bh = (int)(unit / a.K), b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16;
+    const unsigned unit = blockIdx.x;                        // below 2^23
+    const int chunk = (int)(unit % (unsigned)a.K), bh = (int)(unit / (unsigned)a.K), b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
     const int len = length_of(a, b), t0 = chunk * C, left = len - t0;
     if (left <= 0) return;                                   // no later launch reads this unit
     const size_t row0 = (size_t)b * a.N + t0;
@@ -67,17 +78,17 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         kq[j][0] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * (int)sizeof(T));
         kq[j][1] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * (int)sizeof(T));
     }
-    float *gate = a.gate + unit * 4 * C;
+    float *gate = a.gate + (size_t)unit * 4 * C;
     if (wave == 0) {
         // sums of many small logarithms, and differences of such sums: fp64, kept as two fp32.  Below -1000 a factor is zero
         // either way, and sums stay finite (a decay to nothing is g = -inf).
         double sum = (double)(gate_in < -1000.0f ? -1000.0f : gate_in);      // a NaN stays one
+        sum += lane_before<1>(sum), sum += lane_before<2>(sum), sum += lane_before<4>(sum), sum += lane_before<8>(sum);
+        double before = 0.0;                                 // and over the rows of 16 lanes
 #pragma unroll
-        for (int d = 1; d < C; d *= 2) {
-            const double from = __shfl_up(sum, d);
-            if (lane >= d) sum += from;
-        }
-        const double whole = __shfl(sum, C - 1);
+        for (int r = 1; r < C / 16; ++r) before += g >= r ? value_of(sum, 16 * r - 1) : 0.0;
+        sum += before;
+        const double whole = value_of(sum, C - 1);
         if (lane < C) {
             const float hi = (float)sum, lo = (float)(sum - (double)hi);
             gh[lane] = hi, gl[lane] = lo, bt[lane] = beta_in;
@@ -93,74 +104,87 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
         park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, kq[j][1]);
     }
     __syncthreads();
-    float *zOut = a.tri + unit * 2 * Ch::kTri, *mOut = zOut + Ch::kTri;
-    for (int i = wave; i < kTiles * kTiles; i += 4) {        // tiles (rt, ct) of 16 x 16, the diagonals dealt to all waves
-        const int rt = i / kTiles, ct = (i + rt) % kTiles;
-        if (ct / 2 > rt / 2) continue;                       // a 32 x 32 block above the diagonal
-        f32x4 kk = {0, 0, 0, 0}, qk = {0, 0, 0, 0};
-        if (ct <= rt) {
+    float *zOut = a.tri + (size_t)unit * 2 * Ch::kTri, *mOut = zOut + Ch::kTri;
+    constexpr int kLow = kTiles * (kTiles + 1) / 2, kLowEach = (kLow + 3) / 4;
+    f32x4 kk[kLowEach], qk[kLowEach];
+    int rt[kLowEach], ct[kLowEach];                          // tiles of 16 x 16 on and below the diagonal
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                const Parts<P> y = row_operand<D, P, true>(kS, C * D, 16 * ct + c, 4 * s + g);
-                kk = product(row_operand<D, P, true>(kS, C * D, 16 * rt + c, 4 * s + g), y, kk);
-                qk = product(row_operand<D, P, true>(qS, C * D, 16 * rt + c, 4 * s + g), y, qk);
-            }
-        }
-        const int s = 16 * ct + c;
+    for (int n = 0; n < kLowEach; ++n) {
+        const int i = wave + 4 * n < kLow ? wave + 4 * n : kLow - 1;        // the last one again, which is not stored twice
+        rt[n] = i < 1 ? 0 : i < 3 ? 1 : i < 6 ? 2 : 3, ct[n] = i - rt[n] * (rt[n] + 1) / 2;
+        kk[n] = qk[n] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = 16 * rt + 4 * g + r;
-            const float decay = s <= t ? expf((gh[t] - gh[s]) + (gl[t] - gl[s])) : 0.0f;
-            if (ct <= rt) low[t * kTriStride + s] = s < t ? kk[r] * decay : 0.0f;
-            mOut[tri_row<C>(t, ct / 2) * 32 + s % 32] = s <= t ? qk[r] * decay : 0.0f;
+        for (int s = 0; s < D / 32; ++s) {
+            const Parts<P> y = row_operand<D, P, true>(kS, C * D, 16 * ct[n] + c, 4 * s + g);
+            kk[n] = product(row_operand<D, P, true>(kS, C * D, 16 * rt[n] + c, 4 * s + g), y, kk[n]);
+            qk[n] = product(row_operand<D, P, true>(qS, C * D, 16 * rt[n] + c, 4 * s + g), y, qk[n]);
         }
     }
-    __syncthreads();                                         // K and Q make way for the inverse
+#pragma unroll
+    for (int n = 0; n < kLowEach; ++n) {
+        if (wave + 4 * n >= kLow) break;
+        const int s = 16 * ct[n] + c, first = 16 * rt[n] + 4 * g;
+        const f32x4 hi = *reinterpret_cast<const f32x4 *>(gh + first) - gh[s], lo = *reinterpret_cast<const f32x4 *>(gl + first) - gl[s];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = first + r;
+            const float decay = s <= t ? expf(hi[r] + lo[r]) : 0.0f;
+            low[t * kTriStride + s] = s < t ? kk[n][r] * decay : 0.0f;
+            mOut[tri_row<C>(t, ct[n] / 2) * 32 + s % 32] = s <= t ? qk[n][r] * decay : 0.0f;
+            if (rt[n] == ct[n] && rt[n] % 2 == 0) mOut[tri_row<C>(t, ct[n] / 2) * 32 + 16 + c] = 0.0f;     // right of it, in the same 32 x 32
+        }
+    }
+    __syncthreads();                                         // K and Q make way for the inverses
     if (wave == 0 && g < kTiles) {
+        f32x4 f[16][4];
+#pragma unroll
+        for (int r = 1; r < 16; ++r)
+#pragma unroll
+            for (int q = 0; 4 * q < r; ++q) f[r][q] = *reinterpret_cast<const f32x4 *>(low + (16 * g + r) * kTriStride + 16 * g + 4 * q);
         float x[16], y[16];                                  // column c of block (g, g), and beta times it
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             float v = r == c ? 1.0f : 0.0f, u = 0.0f;
-            f32x4 f[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (4 * q < r) f[q] = *reinterpret_cast<const f32x4 *>(low + (16 * g + r) * kTriStride + 16 * g + 4 * q);
 #pragma unroll
             for (int s = 0; s < r; ++s) {
-                if (s % 2 == 0) v = fmaf(-f[s / 4][s % 4], y[s], v);
-                else u = fmaf(-f[s / 4][s % 4], y[s], u);
+                if (s % 2 == 0) v = fmaf(-f[r][s / 4][s % 4], y[s], v);
+                else u = fmaf(-f[r][s / 4][s % 4], y[s], u);
             }
             x[r] = v + u, y[r] = bt[16 * g + r] * x[r];
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) inv[(16 * g + r) * kTriStride + 16 * g + c] = x[r];
     }
-    __syncthreads();
+    f32x4 z[kTiles], ab[kTiles][kTiles];                     // block column `wave`: what is left of A, and -(A beta)
+    const int j = wave;
+    if (j < kTiles) {
 #pragma unroll
-    for (int d = 1; d < kTiles; ++d) {
-        const int i = d + wave, j = wave;
-        if (i < kTiles) {
-            f32x4 sum = {0, 0, 0, 0}, t = {0, 0, 0, 0};
-            for (int k = j; k < i; ++k)
-                sum = times(block_rows(low, i, k, c, g) * *reinterpret_cast<const f32x4 *>(bt + 16 * k + 4 * g), block_columns(inv, k, j, c, g), sum);
-            t = times(block_rows(inv, i, i, c, g), finite(sum), t);
+        for (int i = 0; i < kTiles; ++i) {
+            if (i >= j) z[i] = block_columns(low, i, j, c, g);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) inv[(16 * i + 4 * g + r) * kTriStride + 16 * j + c] = -t[r];
+            for (int k = 0; k < i; ++k)
+                if (k >= j) ab[i][k] = -block_rows(low, i, k, c, g) * *reinterpret_cast<const f32x4 *>(bt + 16 * k + 4 * g);
         }
-        __syncthreads();
     }
-    // block (i, j) of Z is i - j + 1 products: 20 of them, five a wave (of 32 tokens 4, in three waves)
-    for (int n = 0; n < kTiles * kTiles; ++n) {
-        const int i = n / kTiles, j = n % kTiles;
-        constexpr int kOf4[16] = {0, -1, -1, -1, 1, 3, -1, -1, 2, 3, 3, -1, 0, 1, 2, 3};
-        if ((kTiles == 4 ? kOf4[n] : n == 1 ? -1 : n % 4) != wave) continue;
-        f32x4 z = {0, 0, 0, 0};
-        for (int k = j; k <= i; ++k) z = times(block_rows(inv, i, k, c, g), finite(block_columns(low, k, j, c, g)), z);
+    __syncthreads();
+    if (j < kTiles) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = 16 * i + 4 * g + r;
-            zOut[tri_row<C>(t, j / 2) * 32 + (16 * j + c) % 32] = z[r];
-            if (i == j && i % 2 == 0) zOut[tri_row<C>(t, j / 2) * 32 + 16 + c] = 0.0f;     // the tile right of the diagonal's
+        for (int k = 0; k < kTiles; ++k) {
+            if (k < j) continue;
+            z[k] = times(block_rows(inv, k, k, c, g), finite(z[k]), f32x4{0, 0, 0, 0});
+            const f32x4 y = finite(z[k]);
+#pragma unroll
+            for (int i = k + 1; i < kTiles; ++i) z[i] = times(ab[i][k], y, z[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            if (i < j) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * i + 4 * g + r;
+                zOut[tri_row<C>(t, j / 2) * 32 + (16 * j + c) % 32] = z[i][r];
+                if (i == j && i % 2 == 0) zOut[tri_row<C>(t, j / 2) * 32 + 16 + c] = 0.0f;
+            }
         }
     }
 }
@@ -169,23 +193,28 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_local_
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
 // depends on a branch.
-template <typename T, int D, PassKind kKind, bool kKeep> __global__ __launch_bounds__(512) void delta_fwd_kernel(const DeltaArgs a) {
+// kOne: sequences of one chunk at most.  There is nothing to fetch ahead, so the working waves fetch it themselves, and two
+// workgroups of half the threads and LDS share a compute unit (64 x 33 tokens, 8 heads of 64 bf16: 11 us instead of 15).
+template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __global__ __launch_bounds__(kOne ? 256 : 512) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
     constexpr bool kOutputs = kKind == kWhole;
-    __shared__ Chunked<T, D> buffers[2];
+    __shared__ Chunked<T, D> buffers[kOne ? 1 : 2];
     Task task;
     if (!task_of<kKind, false>(a, C, D, task)) return;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, m = task.m0 + wave * 16 + c;
     const int h = task.h, len = task.len, count = task.count, ldo = a.H * a.M;
     const size_t seq = (size_t)task.b * a.N, state = (size_t)task.bh * D * a.M, piece = (size_t)task.bh * a.pieces + task.piece;
-    if (wave >= 4) {
+    if constexpr (kOne) {
+        if (count > 0) fetch_only<T, D>(buffers[0], a, task, (const T *)a.v, a.ldv, tid);
+    } else if (wave >= 4) {
         fetch_chunks<T, D, !kOutputs, false>(buffers, a, task, (const T *)a.v, a.ldv, tid - 256);
         return;
     }
     if (wave * 16 >= task.cols) {                            // no columns (M is a multiple of 16)
         if (count > 0) __syncthreads();
-        for (int i = 0; i < count; ++i) __syncthreads();
+        if constexpr (!kOne)
+            for (int i = 0; i < count; ++i) __syncthreads();
         return;
     }
     f32x4 S[D / 16];
@@ -208,7 +237,7 @@ template <typename T, int D, PassKind kKind, bool kKeep> __global__ __launch_bou
         const long unit = (long)task.bh * a.K + chunk;
         const size_t row0 = seq + (size_t)chunk * C;
         const int left = len - chunk * C;
-        const Chunked<T, D> &in = buffers[i & 1];
+        const Chunked<T, D> &in = buffers[kOne ? 0 : i & 1];
         const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
         const auto rows = [&](const uint16_t *mat, int s, Parts<P> (&f)[kTiles]) {
 #pragma unroll
@@ -324,7 +353,8 @@ template <typename T, int D, PassKind kKind, bool kKeep> __global__ __launch_bou
         }
 #pragma unroll
         for (int i = (kGroups - 1) * kGroup / 2; i < kSteps; ++i) sp[i] = cut(S[2 * i], S[2 * i + 1]);
-        __syncthreads();
+        if constexpr (kOne) break;
+        else __syncthreads();
     }
     if constexpr (kOutputs) {
         if (!task.end) return;
@@ -497,6 +527,11 @@ hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
 #define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<task_grid(a, kTransitions), 512, 0, s>>>(a)
         LA_BY_WIDTH(LA_PIECES)
         if (a.pieces > 2) launch_join(a, dtype, false, s);
+    }
+    if (a.K == 1 && a.state == nullptr) {
+#define LA_ONE(T, D) delta_fwd_kernel<T, D, kWhole, false, true><<<task_grid(a, kWhole), 256, 0, s>>>(a)
+        LA_BY_WIDTH(LA_ONE)
+        return hipGetLastError();
     }
 #define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, kWhole, true><<<task_grid(a, kWhole), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, kWhole, false><<<task_grid(a, kWhole), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_PASS)

@@ -170,6 +170,19 @@ def test_outputs_before_a_token_do_not_depend_on_it(dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [(3, 1, 2, 1, 32, 16), (3, 29, 4, 2, 64, 80), (2, 32, 2, 2, 128, 128), (5, 64, 3, 1, 64, 64), (3, 65, 2, 1, 64, 48)])
+def test_with_and_without_what_the_backward_needs(sizes, dtype):
+    """Sequences of one chunk go another way without it: the same outputs."""
+    B, N = sizes[:2]
+    for lengths in (None, [N, N // 2, 0, 1, N - 1][:B]):
+        c = Case(19, dtype, *sizes, lengths)
+        a, b = c.run(back=True), c.run(back=False)
+        for n in ("o", "h1"):
+            assert torch.equal(a[n], b[n]), n
+            ref.check(n, host(b[n]), c.want(), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_decay_that_is_no_number_shows(dtype):
     c = Case(18, dtype, 1, 130, 2, 1, 64, 48)
     x, more = c.inputs()
