@@ -169,7 +169,7 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
 // during the turn before, and two workgroups share a compute unit: with all columns of eight waves at once, one workgroup, half
 // of the time went to waiting for loads (8 x 2048 x 16 heads of 128 bf16: 462 us).
 // kShared: sums over more than one head wait in LDS.
-template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 ? 128 : 256, kShared ? 1 : 2) void delta_chunks_bwd_kernel(const DeltaArgs a) {
+template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 ? 128 : 256, kShared && D != 64 ? 1 : 2) void delta_chunks_bwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kWaves = D == 32 ? 2 : 4, kThreads = 64 * kWaves;
     constexpr int kSlabs = D / 16 / kWaves, kTurn = 32, kPieces = kTurn / 8;
@@ -179,7 +179,7 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
     __shared__ alignas(16) uint16_t kS[P * C * D], qS[P * C * D], work[kWork];
     __shared__ alignas(16) float gates[4 * C], bt[C], miss[C], db[C], red[kWaves][C], ends[kWaves];
     __shared__ f32x4 sums[kShared ? 2 : 1][kShared ? kSlabs * kTiles : 1][kShared ? kThreads : 1];      // dQ, dK so far
-    uint16_t *uS = work, *wS = work + 3 * C * kTurn, *oS = work + 6 * C * kTurn, *square = work;          // U, dV, dO; P, then B + B^T
+    uint16_t *uS = work, *wS = work + 3 * C * kTurn, *oS = work + 6 * C * kTurn, *square = work;          // U, dV, dO; P, then B
     int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int chunk = (int)(blockIdx.x % a.K), bk = (int)(blockIdx.x / a.K), b = bk / a.Hk, hk = bk % a.Hk, per = a.H / a.Hk;
@@ -207,8 +207,9 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
     Eight<float> us[kEach], ys[kEach], s0[kSlabs], s1[kSlabs];
     Eight<T> vs[kEach], os[kEach];
     float gate_in[kGateEach], beta_in;
-    const auto load = [&](int n) {
-        const int h = hk * per + n / turns, m0 = n % turns * kTurn, cols = a.M - m0 < kTurn ? a.M - m0 : kTurn;
+    const auto load = [&](int turn) {
+        const int n = turn < all ? turn : 0, h = hk * per + n / turns, m0 = n % turns * kTurn;
+        const int cols = turn >= all ? 0 : a.M - m0 < kTurn ? a.M - m0 : kTurn;          // nothing behind the last turn
         const long unit = (long)(b * a.H + h) * a.K + chunk;
         const Range ur = range_of(a.miss + (size_t)unit * C * a.M + m0, C, a.M, cols), yr = range_of(a.write + (size_t)unit * C * a.M + m0, C, a.M, cols);
         const Range vr = range_of((const T *)a.v + row0 * a.ldv + (size_t)h * a.M + m0, rows, a.ldv, cols);
@@ -258,13 +259,14 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
     }
     f32x4 q1[kSlabs][kTiles], k1[kSlabs][kTiles], k2[kSlabs][kTiles], p[kLowEach], bb[kLowEach];
     float both = 0.0f;                                       // <S, dS'>
-    // the wave's i-th tile of a lower triangle: rows 16 ct.., columns 16 st..
-    const auto tile_of = [&](int i, int &st, int &ct) {
-        st = wave + i * kWaves, ct = 0;
-        if (st >= kLow) return false;
-        while (st > ct) st -= ++ct;
-        return true;
-    };
+    // the wave's tiles of a lower triangle: columns 16 st .. of s, rows 16 ct .. of t; where it has fewer, the last one again, not stored
+    int st[kLowEach], ct[kLowEach];
+#pragma unroll
+    for (int i = 0; i < kLowEach; ++i) {
+        const int at = wave + i * kWaves < kLow ? wave + i * kWaves : kLow - 1;
+        ct[i] = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3, st[i] = at - ct[i] * (ct[i] + 1) / 2;
+    }
+    const auto own = [&](int i) { return wave + i * kWaves < kLow; };
     for (int n = 0; n < all; ++n) {
         const int h = hk * per + n / turns;
         load_states(n);
@@ -304,15 +306,13 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
             dots += dpp_move<0x4E>(dots), dbs += dpp_move<0x4E>(dbs);
             if (piece == 0) miss[t] += dots, db[t] += dbs;
         }
-        load(n + 1 < all ? n + 1 : n);
+        load(n + 1);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kLowEach; ++i) {                 // P^T and B^T: rows s, columns t >= s
-            int st, ct;
-            if (!tile_of(i, st, ct)) break;
-            const Parts<3> u = row_operand<kTurn, 3, true>(uS, C * kTurn, 16 * st + c, g);
-            p[i] = product(u, row_operand<kTurn, P, true>(oS, C * kTurn, 16 * ct + c, g), p[i]);
-            bb[i] = product(u, row_operand<kTurn, 3, true>(wS, C * kTurn, 16 * ct + c, g), bb[i]);
+            const Parts<3> u = row_operand<kTurn, 3, true>(uS, C * kTurn, 16 * st[i] + c, g);
+            p[i] = product(u, row_operand<kTurn, P, true>(oS, C * kTurn, 16 * ct[i] + c, g), p[i]);
+            bb[i] = product(u, row_operand<kTurn, 3, true>(wS, C * kTurn, 16 * ct[i] + c, g), bb[i]);
         }
 #pragma unroll
         for (int x = 0; x < kSlabs; ++x) {                   // one after the other: their operands together are too many registers
@@ -331,26 +331,33 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
         if (n % turns != turns - 1) continue;
         tid = here(tid), lane = tid % kWave, c = lane % 16, g = lane / 16;
         __syncthreads();                                     // U, dV, dO make way for P
+        // rows t, columns s of a lower triangle in LDS
+        const auto park_low = [&](int i, const float (&v)[4]) {
+            const int t = 16 * ct[i] + c, s = 16 * st[i] + 4 * g;
+            const Split3 w = split3(v);
+            const u32x2_t parts[3] = {w.h, w.m, w.l};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x2_t *>(square + k * C * C + mat_at<C, true>(t, s / 8) + s % 8) = parts[k];
+        };
 #pragma unroll
         for (int i = 0; i < kLowEach; ++i) {
-            int st, ct;
-            if (!tile_of(i, st, ct)) break;
-            const int t = 16 * ct + c, s = 16 * st + 4 * g, place = mat_at<C, true>(t, s / 8) + s % 8;
-            float pq[4];
+            const int t = 16 * ct[i] + c, s = 16 * st[i] + 4 * g;
+            const f32x4 hi = gates[2 * C + t] - *reinterpret_cast<const f32x4 *>(gates + 2 * C + s), lo = gates[3 * C + t] - *reinterpret_cast<const f32x4 *>(gates + 3 * C + s);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float decay = s + r <= t ? expf((gates[2 * C + t] - gates[2 * C + s + r]) + (gates[3 * C + t] - gates[3 * C + s + r])) : 0.0f;
-                pq[r] = s + r <= t ? a.scale * p[i][r] * decay : 0.0f;
+                const float decay = s + r <= t ? expf(hi[r] + lo[r]) : 0.0f;
+                p[i][r] = s + r <= t ? a.scale * p[i][r] * decay : 0.0f;
                 bb[i][r] = s + r < t ? -bb[i][r] * decay : 0.0f;
             }
-            const Split3 ps = split3(pq);
-            const u32x2_t parts[3] = {ps.h, ps.m, ps.l};
+        }
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                *reinterpret_cast<u32x2_t *>(square + k * C * C + place) = parts[k];
-                // the tile right above the diagonal, which products over 32 tokens read
-                if (st == ct && ct % 2 == 0) *reinterpret_cast<u32x2_t *>(square + k * C * C + mat_at<C, true>(t, (s + 16) / 8) + s % 8) = u32x2_t{0, 0};
-            }
+        for (int i = 0; i < kLowEach; ++i) {
+            if (!own(i)) break;
+            park_low(i, {p[i][0], p[i][1], p[i][2], p[i][3]});
+            // the tile right above the diagonal, which products over 32 tokens read
+            if (st[i] == ct[i] && ct[i] % 2 == 0)
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x2_t *>(square + k * C * C + mat_at<C, true>(16 * ct[i] + c, 2 * st[i] + 2 + g / 2) + 4 * (g & 1)) = u32x2_t{0, 0};
         }
         __syncthreads();
         float into = 0.0f;
@@ -368,7 +375,7 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
             }
             if (kSlabs > 1) in_this_order();
         }
-        // products with a square matrix in LDS, from the left: its rows, and of P its columns too
+        // products with a lower triangle in LDS, from the left: with its rows, and with its columns
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) {
             Parts<P> kx[kSlabs], qx[kSlabs];
@@ -392,26 +399,11 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
                 if (kSlabs > 1 && t % 2 == 1) in_this_order();
             }
         }
-        __syncthreads();                                     // P makes way for B + B^T
+        __syncthreads();                                     // P makes way for B
 #pragma unroll
         for (int i = 0; i < kLowEach; ++i) {
-            int st, ct;
-            if (!tile_of(i, st, ct)) break;
-            const int t = 16 * ct + c, s = 16 * st + 4 * g, place = mat_at<C, true>(t, s / 8) + s % 8;
-            const float bq[4] = {bb[i][0], bb[i][1], bb[i][2], bb[i][3]};
-            const Split3 bs = split3(bq);
-            const u32x2_t parts[3] = {bs.h, bs.m, bs.l};
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                uint16_t *to = square + k * C * C;
-                if (st != ct) *reinterpret_cast<u32x2_t *>(to + place) = parts[k];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint16_t e = (uint16_t)(parts[k][r / 2] >> (16 * (r & 1)));
-                    if (st != ct || s + r <= t) to[mat_at<C, true>(s + r, t / 8) + t % 8] = e;
-                    if (st == ct && s + r <= t) to[place + r] = e;        // on the diagonal both triangles are in one tile
-                }
-            }
+            if (!own(i)) break;
+            park_low(i, {bb[i][0], bb[i][1], bb[i][2], bb[i][3]});
         }
         __syncthreads();
 #pragma unroll
@@ -420,8 +412,15 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) kx[x] = column_operand<D, false, P, true>(kS, C * D, 32 * s, wave * kSlabs + x, lane);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
+            for (int t = 2 * s; t < kTiles; ++t) {
                 const Parts<3> f = row_operand<C, 3, true>(square, C * C, 16 * t + c, 4 * s + g);
+#pragma unroll
+                for (int x = 0; x < kSlabs; ++x) k1[x][t] = product(f, kx[x], k1[x][t]);
+                if (kSlabs > 1 && t % 2 == 1) in_this_order();
+            }
+#pragma unroll
+            for (int t = 0; t < 2 * (s + 1); ++t) {
+                const Parts<3> f = column_operand<C, false, 3, true>(square, C * C, 32 * s, t, lane);
 #pragma unroll
                 for (int x = 0; x < kSlabs; ++x) k1[x][t] = product(f, kx[x], k1[x][t]);
                 if (kSlabs > 1 && t % 2 == 1) in_this_order();
