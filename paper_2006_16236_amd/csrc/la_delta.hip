@@ -370,14 +370,16 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
 
 // ---- from piece to piece -----------------------------------------------------------------------------
 // Forwards S_{j+1} = F_j S_j + (what piece j leaves of a zero state), j = 1 .. last - 1; backwards E_{j-1} = F_j^T E_j + .., j = last - 1
-// .. 1.  64 columns a workgroup; a wave has some rows of the transitions F, on their way a piece ahead, and all of the
-// columns, which the waves hand each other through LDS.
+// .. 1.  kJoin columns a workgroup; a wave has some rows of the transitions F, on their way a piece ahead, and all of the
+// columns, which the waves hand each other through LDS.  A piece waits for the one before, so few columns: with 64, 6.5 us a piece of
+// 16 heads of 128 x 128 and 2.6 of 64 x 64, with 16, 4.9 and 1.5.
+constexpr int kJoin = 16;
 template <int D, bool kBack> __global__ __launch_bounds__(256) void delta_join_kernel(const DeltaArgs a, float *states, int C) {
     constexpr int kEach = D <= 64 ? 1 : D / 64, kSteps = D / 32;
-    __shared__ alignas(16) uint16_t sS[2][3 * kCols * D];
-    const int blocks = (a.M + kCols - 1) / kCols, bh = blockIdx.x / blocks, m0 = blockIdx.x % blocks * kCols;
+    __shared__ alignas(16) uint16_t sS[2][3 * kJoin * D];
+    const int blocks = (a.M + kJoin - 1) / kJoin, bh = blockIdx.x / blocks, m0 = blockIdx.x % blocks * kJoin;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16;
-    const int cols = a.M - m0 < kCols ? a.M - m0 : kCols, chunks = (length_of(a, bh / a.H) + C - 1) / C, last = chunks > 0 ? (chunks - 1) / a.length : 0;
+    const int cols = a.M - m0 < kJoin ? a.M - m0 : kJoin, chunks = (length_of(a, bh / a.H) + C - 1) / C, last = chunks > 0 ? (chunks - 1) / a.length : 0;
     const bool mine = wave * kEach * 16 < D;                 // of 32 rows two waves have none
     float *state = states + (size_t)bh * a.pieces * D * a.M;
     const float *transition = a.transition + (size_t)bh * a.pieces * D * D;
@@ -401,10 +403,10 @@ template <int D, bool kBack> __global__ __launch_bounds__(256) void delta_join_k
         const Split3 p = split3(q);
         const int row = 16 * (wave * kEach + x) + 4 * g, at = mat_at<D, true>(16 * ct + c, row / 8) + row % 8;
         *reinterpret_cast<u32x2_t *>(to + at) = p.h;
-        *reinterpret_cast<u32x2_t *>(to + kCols * D + at) = p.m;
-        *reinterpret_cast<u32x2_t *>(to + 2 * kCols * D + at) = p.l;
+        *reinterpret_cast<u32x2_t *>(to + kJoin * D + at) = p.m;
+        *reinterpret_cast<u32x2_t *>(to + 2 * kJoin * D + at) = p.l;
     };
-    constexpr int kColTiles = kCols / 16;
+    constexpr int kColTiles = kJoin / 16;
     f32x4 v[kColTiles][kEach];
     const auto load_tiles = [&](int piece) {                 // what is there of its state; zeros in columns that are none
         const Range r = range_of(state + (size_t)piece * D * a.M, mine ? D : 0, a.M, a.M);
@@ -440,7 +442,7 @@ template <int D, bool kBack> __global__ __launch_bounds__(256) void delta_join_k
         for (int ct = 0; ct < kColTiles; ++ct) {
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
-                const Parts<3> y = row_operand<D, 3, true>(sS[i & 1], kCols * D, 16 * ct + c, 4 * s + g);
+                const Parts<3> y = row_operand<D, 3, true>(sS[i & 1], kJoin * D, 16 * ct + c, 4 * s + g);
 #pragma unroll
                 for (int x = 0; x < kEach; ++x) v[ct][x] = product(f[x][s], y, v[ct][x]);
             }
@@ -510,7 +512,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void delta_step_k
 }  // namespace
 
 void launch_join(const DeltaArgs &a, int dtype, bool back, hipStream_t s) {
-    const unsigned grid = (unsigned)(a.B * a.H * ((a.M + kCols - 1) / kCols));
+    const unsigned grid = (unsigned)(a.B * a.H * ((a.M + kJoin - 1) / kJoin));
     const int C = delta_chunk(dtype);
     float *states = back ? a.piece_dstate : a.piece_state;
 #define LA_JOIN(D) back ? delta_join_kernel<D, true><<<grid, 256, 0, s>>>(a, states, C) : delta_join_kernel<D, false><<<grid, 256, 0, s>>>(a, states, C)
