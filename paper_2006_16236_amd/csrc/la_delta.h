@@ -105,6 +105,13 @@ __device__ __forceinline__ f32x4 finite(f32x4 v) {
     return v;
 }
 
+// e^(hi + lo) = 2^(hi log2 e) 2^(what that product's rounding and lo leave), to 2^-22.  Below 2^-126 it is zero.
+__device__ __forceinline__ float decay_of(float hi, float lo) {
+    constexpr float kLog2e = 1.44269504f, kRest = (float)(1.4426950408889634 - (double)kLog2e), kLn2 = 0.693147181f;
+    const float p = hi * kLog2e, rest = fmaf(hi, kLog2e, -p) + fmaf(hi, kRest, lo * kLog2e);
+    return __builtin_amdgcn_exp2f(p) * fmaf(rest, kLn2, 1.0f);
+}
+
 // ---- matrices of bf16 parts in LDS --------------------------------------------------------------
 // Rows of COLS elements in pieces of eight (16 bytes), the pieces of a row exchanged by a function of the row such that a wave's
 // reads below take 4.4 cycles, the least for 1 KB (measured; others took 8 or 16): 16-byte reads of one piece of 16 paired

@@ -128,7 +128,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeo
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = first + r;
-            const float decay = s <= t ? expf(hi[r] + lo[r]) : 0.0f;
+            const float decay = s <= t ? decay_of(hi[r], lo[r]) : 0.0f;
             low[t * kTriStride + s] = s < t ? kk[n][r] * decay : 0.0f;
             mOut[tri_row<C>(t, ct[n] / 2) * 32 + s % 32] = s <= t ? qk[n][r] * decay : 0.0f;
             if (rt[n] == ct[n] && rt[n] % 2 == 0) mOut[tri_row<C>(t, ct[n] / 2) * 32 + 16 + c] = 0.0f;     // right of it, in the same 32 x 32

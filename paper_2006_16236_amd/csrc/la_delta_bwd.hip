@@ -345,7 +345,7 @@ template <typename T, int D, bool kShared> __global__ __launch_bounds__(D == 32 
             const f32x4 hi = gates[2 * C + t] - *reinterpret_cast<const f32x4 *>(gates + 2 * C + s), lo = gates[3 * C + t] - *reinterpret_cast<const f32x4 *>(gates + 3 * C + s);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float decay = s + r <= t ? expf(hi[r] + lo[r]) : 0.0f;
+                const float decay = s + r <= t ? decay_of(hi[r], lo[r]) : 0.0f;
                 p[i][r] = s + r <= t ? a.scale * p[i][r] * decay : 0.0f;
                 bb[i][r] = s + r < t ? -bb[i][r] * decay : 0.0f;
             }
