@@ -262,10 +262,10 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
                     since[t] = gate4(0, t), strength[t] = gate4(2, t);
                 }
             }
-            in_this_order();
+            in_this_order<D>();
             products(f[s % 2], sp[s], ks);
         }
-        in_this_order();
+        in_this_order<D>();
         // Q S beside what the tokens miss of the state before the chunk
         Parts<3> x[kBlocks], zf[kTiles][kBlocks];
 #pragma unroll
@@ -278,9 +278,9 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
                 if (s + 1 < kSteps) rows(in.q, s + 1, f[(kSteps + s + 1) % 2]);
                 products(f[(kSteps + s) % 2], first<kOut>(sp[s]), qs);
             }
-            side_by_side<kSteps * kTiles * (P == 1 ? 2 : 6)>();
+            side_by_side<D, kSteps * kTiles * (P == 1 ? 2 : 6)>();
         }
-        in_this_order();
+        in_this_order<D>();
         // ... and of what the chunk's earlier tokens write
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i)
@@ -289,7 +289,7 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) ks[t] = f32x4{0, 0, 0, 0};
         lower_products<2>(zf, x, ks);
-        in_this_order();
+        in_this_order<D>();
         Parts<kOut> mf[kTiles][kBlocks], u[kBlocks];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -317,7 +317,7 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
 #pragma unroll
             for (int t = 0; t < kGroup; ++t) kt[n % 2][t] = column_operand<D, true, P>(in.k, C * D, 32 * (n % kBlocks), n / kBlocks * kGroup + t, lane);
         };
-        in_this_order();
+        in_this_order<D>();
         columns(0);
         if constexpr (kOutputs) lower_products<kOut - 1>(mf, u, qs);
 #pragma unroll
@@ -325,8 +325,8 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
         const float whole = in.gates[C - 1];
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) S[t] *= whole;
-        if (kOutputs) side_by_side<(kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
-        in_this_order();
+        if (kOutputs) side_by_side<D, (kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
+        in_this_order<D>();
         const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, left < most ? left : most, ldo, a.M);
 #pragma unroll
         for (int n = 0; n < kGroups * kBlocks; ++n) {
@@ -348,8 +348,8 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
                     sp[i] = cut(S[2 * i], S[2 * i + 1]);
                 }
             }
-            if (n == 0 || n % kBlocks == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
-            in_this_order();
+            if (n == 0 || n % kBlocks == 0) side_by_side<D, kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order<D>();
         }
 #pragma unroll
         for (int i = (kGroups - 1) * kGroup / 2; i < kSteps; ++i) sp[i] = cut(S[2 * i], S[2 * i + 1]);

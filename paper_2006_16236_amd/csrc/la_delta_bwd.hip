@@ -81,14 +81,14 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
                 for (int x = 0; x < kBlocks; ++x) o[x] = column_operand<kCols, false, P>(in.v, C * kCols, 32 * x, wave, lane);
                 upper(in.m, tri);
             }
-            in_this_order();
+            in_this_order<D>();
             products(f[s % 2], sp[s], y);
         }
-        in_this_order();
+        in_this_order<D>();
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) out[t] = column_values<kCols, P>(in.v, C * kCols, paired(t, 4 * g), wave, lane);
         upper_products<2>(tri, o, w);
-        in_this_order();
+        in_this_order<D>();
         // dU, and beside it the state's share of the outputs
         constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;
         Parts<P> kt[2][kGroup];
@@ -104,7 +104,7 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) S[t] *= whole;
         columns(in.q, 0);
-        in_this_order();
+        in_this_order<D>();
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) y[t] = a.scale * w[t] + gate4(1, t) * y[t], w[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -121,20 +121,20 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
         for (int n = 0; n < kGroups * kBlocks; ++n) {
             if (n + 1 < kGroups * kBlocks) columns(in.q, n + 1);
             update(n, x[n % kBlocks]);
-            if (n == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
-            in_this_order();
+            if (n == 0) side_by_side<D, kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order<D>();
         }
         upper(in.z, tri);
         upper_products<2>(tri, z, w);
         columns(in.k, 0);
-        in_this_order();
+        in_this_order<D>();
         const Range wr = range_of(a.write + (size_t)unit * C * a.M, C, a.M, a.M);
         const Range vr = range_of((T *)a.dv + (seq + (size_t)chunk * C) * ldo + (size_t)h * a.M, left < C ? left : C, ldo, a.M);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) y[t] -= w[t], w[t] = gate4(2, t) * y[t];       // w: dV
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) x[s] = cut(-gate4(0, 2 * s) * w[2 * s], -gate4(0, 2 * s + 1) * w[2 * s + 1]);
-        in_this_order();
+        in_this_order<D>();
 #pragma unroll
         for (int n = 0; n < kGroups * kBlocks; ++n) {
             if (n + 1 < kGroups * kBlocks) columns(in.k, n + 1);
@@ -153,8 +153,8 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
                     sp[j] = cut(S[2 * j], S[2 * j + 1]);
                 }
             }
-            if (n % kBlocks == 0) side_by_side<kGroup * (P == 1 ? 3 : 6)>();
-            in_this_order();
+            if (n % kBlocks == 0) side_by_side<D, kGroup * (P == 1 ? 3 : 6)>();
+            in_this_order<D>();
         }
 #pragma unroll
         for (int j = (kGroups - 1) * kGroup / 2; j < kSteps; ++j) sp[j] = cut(S[2 * j], S[2 * j + 1]);
