@@ -19,26 +19,25 @@ namespace la {
 namespace {
 
 // ---- chunk-local matrices ------------------------------------------------------------------------
-// One workgroup a unit: decays, masked products of queries and keys, and the triangular system (1 + A beta) Z = A by blocks
+// Decays, masked products of queries and keys, and the triangular system (1 + A beta) Z = A by blocks
 // of 16.  The inverse of the diagonal blocks comes by substitution, one block in each lane group and one column a lane; then a
 // wave has a block column of Z, Z_ij = (1 + A beta)_ii^-1 (A_ij - sum_k (A beta)_ik Z_kj), whose products feed each other in
 // registers.  All in fp32 (v_mfma_f32_16x16x4: lane (c, g) supplies elements 4g + q of its row c, register q of a result is that
-// of the next operand).  Every step waits for the one before, so what counts is how many workgroups a compute unit holds: four (three
-// of 128 columns).  8 x 2048 x 16 heads of 128 bf16: 63 us, 3.8 TB/s of tokens and matrices; one chunk of 64 x 8 heads of 64: 10.
-constexpr int kTriStride = 68;                               // floats between rows: 16 rows' 16-byte reads meet all banks
+// of the next operand).
+constexpr int tri_stride(int C) { return C + 4; }            // floats between rows: 16 rows' 16-byte reads meet all banks
 __device__ __forceinline__ f32x4 times(f32x4 rows, f32x4 columns, f32x4 acc) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc = mfma16(rows[q], columns[q], acc);
     return acc;
 }
 // block (i, j) of a matrix as the left operand, and as the right one
-__device__ __forceinline__ f32x4 block_rows(const float *m, int i, int j, int c, int g) {
-    return *reinterpret_cast<const f32x4 *>(m + (16 * i + c) * kTriStride + 16 * j + 4 * g);
+template <int C> __device__ __forceinline__ f32x4 block_rows(const float *m, int i, int j, int c, int g) {
+    return *reinterpret_cast<const f32x4 *>(m + (16 * i + c) * tri_stride(C) + 16 * j + 4 * g);
 }
-__device__ __forceinline__ f32x4 block_columns(const float *m, int i, int j, int c, int g) {
+template <int C> __device__ __forceinline__ f32x4 block_columns(const float *m, int i, int j, int c, int g) {
     f32x4 v;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = m[(16 * i + 4 * g + q) * kTriStride + 16 * j + c];
+    for (int q = 0; q < 4; ++q) v[q] = m[(16 * i + 4 * g + q) * tri_stride(C) + 16 * j + c];
     return v;
 }
 // of the lane n places before in its row of 16 (zero without one), and of one lane
@@ -51,14 +50,144 @@ __device__ __forceinline__ double value_of(double v, int lane) {
     const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
     return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_readlane((int)w[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane)});
 }
+// One wave, a token a lane: G as hi + lo, e^G and e^{G_C - G}.  Sums of many small logarithms, and differences of such sums: fp64,
+// kept as two fp32.  Below -1000 a factor is zero either way, and sums stay finite (a decay to nothing is g = -inf).
+template <int C> __device__ __forceinline__ void decays(float gate_in, int g, float &hi, float &lo, float &since, float &rest) {
+    double sum = (double)(gate_in < -1000.0f ? -1000.0f : gate_in);      // a NaN stays one
+    sum += lane_before<1>(sum), sum += lane_before<2>(sum), sum += lane_before<4>(sum), sum += lane_before<8>(sum);
+    double before = 0.0;                                     // and over the rows of 16 lanes
+#pragma unroll
+    for (int r = 1; r < C / 16; ++r) before += g >= r ? value_of(sum, 16 * r - 1) : 0.0;
+    sum += before;
+    const double whole = value_of(sum, C - 1);
+    hi = (float)sum, lo = (float)(sum - (double)hi);
+    since = expf(hi) * (1.0f + lo), rest = expf((float)(whole - sum));
+}
+// The tiles of 16 x 16 on and below a chunk's diagonal, dealt to four waves; where a wave has fewer, the last one again, not put out.
+template <int C> struct LowTiles {
+    static constexpr int kTiles = C / 16, kLow = kTiles * (kTiles + 1) / 2, kEach = (kLow + 3) / 4;
+    int row[kEach], col[kEach], wave;
+    __device__ __forceinline__ explicit LowTiles(int w) : wave(w) {
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const int i = wave + 4 * n < kLow ? wave + 4 * n : kLow - 1;
+            row[n] = i < 1 ? 0 : i < 3 ? 1 : i < 6 ? 2 : 3, col[n] = i - row[n] * (row[n] + 1) / 2;
+        }
+    }
+    __device__ __forceinline__ bool mine(int n) const { return wave + 4 * n < kLow; }
+};
+// A into LDS, M's tiles into registers
+template <typename T, int D, bool kPlain> __device__ __forceinline__ void masked_products(const uint16_t *kS, const uint16_t *qS, const float *gh, const float *gl, float *low,
+                                                                                         const LowTiles<Chunk<T>::C> &at, f32x4 (&M)[LowTiles<Chunk<T>::C>::kEach], int c, int g) {
+    constexpr int C = Chunk<T>::C, P = Chunk<T>::P, kEach = LowTiles<C>::kEach;
+    f32x4 kk[kEach];
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+        kk[n] = M[n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const Parts<P> y = row_operand<D, P, kPlain>(kS, C * D, 16 * at.col[n] + c, 4 * s + g);
+            kk[n] = product(row_operand<D, P, kPlain>(kS, C * D, 16 * at.row[n] + c, 4 * s + g), y, kk[n]);
+            M[n] = product(row_operand<D, P, kPlain>(qS, C * D, 16 * at.row[n] + c, 4 * s + g), y, M[n]);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+        const int s = 16 * at.col[n] + c, first = 16 * at.row[n] + 4 * g;
+        const f32x4 hi = *reinterpret_cast<const f32x4 *>(gh + first) - gh[s], lo = *reinterpret_cast<const f32x4 *>(gl + first) - gl[s];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float decay = s <= first + r ? decay_of(hi[r], lo[r]) : 0.0f;
+            kk[n][r] = s < first + r ? kk[n][r] * decay : 0.0f;
+            M[n][r] = s <= first + r ? M[n][r] * decay : 0.0f;
+        }
+        if (at.mine(n))
+#pragma unroll
+            for (int r = 0; r < 4; ++r) low[(first + r) * tri_stride(C) + s] = kk[n][r];
+    }
+}
+// Z's block column `wave` into registers, from A and beta in LDS; inv: room for as much again.  All four waves; a barrier inside.
+template <int C> __device__ __forceinline__ void solve(const float *low, float *inv, const float *bt, int wave, int c, int g, f32x4 (&z)[C / 16]) {
+    constexpr int kTiles = C / 16;
+    if (wave == 0 && g < kTiles) {
+        f32x4 f[16][4];
+#pragma unroll
+        for (int r = 1; r < 16; ++r)
+#pragma unroll
+            for (int q = 0; 4 * q < r; ++q) f[r][q] = *reinterpret_cast<const f32x4 *>(low + (16 * g + r) * tri_stride(C) + 16 * g + 4 * q);
+        float x[16], y[16];                                  // column c of block (g, g), and beta times it
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float v = r == c ? 1.0f : 0.0f, u = 0.0f;
+#pragma unroll
+            for (int s = 0; s < r; ++s) {
+                if (s % 2 == 0) v = fmaf(-f[r][s / 4][s % 4], y[s], v);
+                else u = fmaf(-f[r][s / 4][s % 4], y[s], u);
+            }
+            x[r] = v + u, y[r] = bt[16 * g + r] * x[r];
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) inv[(16 * g + r) * tri_stride(C) + 16 * g + c] = x[r];
+    }
+    f32x4 ab[kTiles][kTiles];                                // z: what is left of A; -(A beta)
+    const int j = wave;
+    if (j < kTiles) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            if (i >= j) z[i] = block_columns<C>(low, i, j, c, g);
+#pragma unroll
+            for (int k = 0; k < i; ++k)
+                if (k >= j) ab[i][k] = -block_rows<C>(low, i, k, c, g) * *reinterpret_cast<const f32x4 *>(bt + 16 * k + 4 * g);
+        }
+    }
+    __syncthreads();
+    if (j < kTiles) {
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k) {
+            if (k < j) continue;
+            z[k] = times(block_rows<C>(inv, k, k, c, g), finite(z[k]), f32x4{0, 0, 0, 0});
+            const f32x4 y = finite(z[k]);
+#pragma unroll
+            for (int i = k + 1; i < kTiles; ++i) z[i] = times(ab[i][k], y, z[i]);
+        }
+    }
+}
+// Both matrices element by element: put(matrix, row of it, column of 32, value), M = 1; with the zeros right of a diagonal tile that
+// lie in the same 32 x 32 block.
+template <int C, typename Put> __device__ __forceinline__ void put_out_m(const LowTiles<C> &at, const f32x4 (&M)[LowTiles<C>::kEach], int c, int g, Put put) {
+#pragma unroll
+    for (int n = 0; n < LowTiles<C>::kEach; ++n) {
+        if (!at.mine(n)) break;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = tri_row<C>(16 * at.row[n] + 4 * g + r, at.col[n] / 2);
+            put(1, row, (16 * at.col[n] + c) % 32, M[n][r]);
+            if (at.row[n] == at.col[n] && at.row[n] % 2 == 0) put(1, row, 16 + c, 0.0f);
+        }
+    }
+}
+template <int C, typename Put> __device__ __forceinline__ void put_out_z(int j, const f32x4 (&z)[C / 16], int c, int g, Put put) {
+    if (j >= C / 16) return;
+#pragma unroll
+    for (int i = 0; i < C / 16; ++i) {
+        if (i < j) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = tri_row<C>(16 * i + 4 * g + r, j / 2);
+            put(0, row, (16 * j + c) % 32, z[i][r]);
+            if (i == j && i % 2 == 0) put(0, row, 16 + c, 0.0f);
+        }
+    }
+}
+// One workgroup a unit.  Every step waits for the one before, so what counts is how many workgroups a compute unit holds: four (three
+// of 128 columns).  8 x 2048 x 16 heads of 128 bf16: 63 us, 3.8 TB/s of tokens and matrices.
 template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4) void delta_local_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kTokens = 2 * P * C * D * (int)sizeof(uint16_t), kTri = C * kTriStride * (int)sizeof(float);
+    constexpr int C = Ch::C, P = Ch::P, kTokens = 2 * P * C * D * (int)sizeof(uint16_t), kTri = C * tri_stride(C) * (int)sizeof(float);
     __shared__ alignas(16) char space[kTokens > kTri ? kTokens : kTri];
-    __shared__ alignas(16) float low[C * kTriStride];        // A, zeros on the diagonal and above
+    __shared__ alignas(16) float low[C * tri_stride(C)];     // A, zeros on the diagonal and above
     __shared__ alignas(16) float gh[C], gl[C], bt[C];
     uint16_t *kS = reinterpret_cast<uint16_t *>(space), *qS = kS + P * C * D;
-    float *inv = reinterpret_cast<float *>(space);           // takes their place
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16;
     const unsigned unit = blockIdx.x;                        // below 2^23
     const int chunk = (int)(unit % (unsigned)a.K), bh = (int)(unit / (unsigned)a.K), b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
@@ -80,20 +209,11 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeo
     }
     float *gate = a.gate + (size_t)unit * 4 * C;
     if (wave == 0) {
-        // sums of many small logarithms, and differences of such sums: fp64, kept as two fp32.  Below -1000 a factor is zero
-        // either way, and sums stay finite (a decay to nothing is g = -inf).
-        double sum = (double)(gate_in < -1000.0f ? -1000.0f : gate_in);      // a NaN stays one
-        sum += lane_before<1>(sum), sum += lane_before<2>(sum), sum += lane_before<4>(sum), sum += lane_before<8>(sum);
-        double before = 0.0;                                 // and over the rows of 16 lanes
-#pragma unroll
-        for (int r = 1; r < C / 16; ++r) before += g >= r ? value_of(sum, 16 * r - 1) : 0.0;
-        sum += before;
-        const double whole = value_of(sum, C - 1);
+        float hi, lo, since, rest;
+        decays<C>(gate_in, g, hi, lo, since, rest);
         if (lane < C) {
-            const float hi = (float)sum, lo = (float)(sum - (double)hi);
             gh[lane] = hi, gl[lane] = lo, bt[lane] = beta_in;
-            gate[lane] = expf(hi) * (1.0f + lo), gate[C + lane] = expf((float)(whole - sum));
-            gate[2 * C + lane] = hi, gate[3 * C + lane] = lo;
+            gate[lane] = since, gate[C + lane] = rest, gate[2 * C + lane] = hi, gate[3 * C + lane] = lo;
         }
     }
 #pragma unroll
@@ -104,98 +224,81 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeo
         park_eight<T>(qS + mat_at<D, true>(t, piece), C * D, kq[j][1]);
     }
     __syncthreads();
-    float *zOut = a.tri + (size_t)unit * 2 * Ch::kTri, *mOut = zOut + Ch::kTri;
-    constexpr int kLow = kTiles * (kTiles + 1) / 2, kLowEach = (kLow + 3) / 4;
-    f32x4 kk[kLowEach], qk[kLowEach];
-    int rt[kLowEach], ct[kLowEach];                          // tiles of 16 x 16 on and below the diagonal
-#pragma unroll
-    for (int n = 0; n < kLowEach; ++n) {
-        const int i = wave + 4 * n < kLow ? wave + 4 * n : kLow - 1;        // the last one again, which is not stored twice
-        rt[n] = i < 1 ? 0 : i < 3 ? 1 : i < 6 ? 2 : 3, ct[n] = i - rt[n] * (rt[n] + 1) / 2;
-        kk[n] = qk[n] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const Parts<P> y = row_operand<D, P, true>(kS, C * D, 16 * ct[n] + c, 4 * s + g);
-            kk[n] = product(row_operand<D, P, true>(kS, C * D, 16 * rt[n] + c, 4 * s + g), y, kk[n]);
-            qk[n] = product(row_operand<D, P, true>(qS, C * D, 16 * rt[n] + c, 4 * s + g), y, qk[n]);
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < kLowEach; ++n) {
-        if (wave + 4 * n >= kLow) break;
-        const int s = 16 * ct[n] + c, first = 16 * rt[n] + 4 * g;
-        const f32x4 hi = *reinterpret_cast<const f32x4 *>(gh + first) - gh[s], lo = *reinterpret_cast<const f32x4 *>(gl + first) - gl[s];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = first + r;
-            const float decay = s <= t ? decay_of(hi[r], lo[r]) : 0.0f;
-            low[t * kTriStride + s] = s < t ? kk[n][r] * decay : 0.0f;
-            mOut[tri_row<C>(t, ct[n] / 2) * 32 + s % 32] = s <= t ? qk[n][r] * decay : 0.0f;
-            if (rt[n] == ct[n] && rt[n] % 2 == 0) mOut[tri_row<C>(t, ct[n] / 2) * 32 + 16 + c] = 0.0f;     // right of it, in the same 32 x 32
-        }
-    }
+    float *out = a.tri + (size_t)unit * 2 * Ch::kTri;
+    const auto put = [&](int matrix, int row, int column, float v) { out[matrix * Ch::kTri + row * 32 + column] = v; };
+    const LowTiles<C> tiles(wave);
+    f32x4 M[LowTiles<C>::kEach], z[C / 16];
+    masked_products<T, D, true>(kS, qS, gh, gl, low, tiles, M, c, g);
+    put_out_m<C>(tiles, M, c, g, put);
     __syncthreads();                                         // K and Q make way for the inverses
-    if (wave == 0 && g < kTiles) {
-        f32x4 f[16][4];
+    solve<C>(low, reinterpret_cast<float *>(space), bt, wave, c, g, z);
+    put_out_z<C>(wave, z, c, g, put);
+}
+// All that a sequence of one chunk needs, in the place that a pass reads it from.  A and the inverses lie where Z and M come to be.
+template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<T, D> &to, float *gh, float *gl, const DeltaArgs &a, const Task &task, int tid) {
+    using Ch = Chunk<T>;
+    constexpr int C = Ch::C, kTok = C * D / 8, kTokEach = (kTok + 255) / 256, kValEach = C * kCols / 8 / 256;
+    static_assert(C * tri_stride(C) * sizeof(float) <= sizeof(to.z), "room for a matrix of fp32");
+    const int lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, hk = task.h / (a.H / a.Hk), rows = task.len < C ? task.len : C;
+    const size_t row0 = (size_t)task.b * a.N, at = (row0 + lane) * a.H + task.h;
+    const Range kr = range_of((const T *)a.k + row0 * a.ldk + (size_t)hk * D, rows, a.ldk, D), qr = range_of((const T *)a.q + row0 * a.ldq + (size_t)hk * D, rows, a.ldq, D);
+    const Range vr = range_of((const T *)a.v + row0 * a.ldv + (size_t)task.h * a.M + task.m0, rows, a.ldv, task.cols);
+    const bool live = wave == 0 && lane < rows;
+    const float gate_in = live && a.g != nullptr ? a.g[at] : 0.0f, beta_in = live ? a.beta[at] : 0.0f;
+    Eight<T> kq[kTokEach][2], v[kValEach];
 #pragma unroll
-        for (int r = 1; r < 16; ++r)
-#pragma unroll
-            for (int q = 0; 4 * q < r; ++q) f[r][q] = *reinterpret_cast<const f32x4 *>(low + (16 * g + r) * kTriStride + 16 * g + 4 * q);
-        float x[16], y[16];                                  // column c of block (g, g), and beta times it
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float v = r == c ? 1.0f : 0.0f, u = 0.0f;
-#pragma unroll
-            for (int s = 0; s < r; ++s) {
-                if (s % 2 == 0) v = fmaf(-f[r][s / 4][s % 4], y[s], v);
-                else u = fmaf(-f[r][s / 4][s % 4], y[s], u);
-            }
-            x[r] = v + u, y[r] = bt[16 * g + r] * x[r];
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) inv[(16 * g + r) * kTriStride + 16 * g + c] = x[r];
+    for (int j = 0; j < kTokEach; ++j) {
+        const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
+        kq[j][0] = load_eight<T>(kr, (t * (int)a.ldk + 8 * piece) * (int)sizeof(T));
+        kq[j][1] = load_eight<T>(qr, (t * (int)a.ldq + 8 * piece) * (int)sizeof(T));
     }
-    f32x4 z[kTiles], ab[kTiles][kTiles];                     // block column `wave`: what is left of A, and -(A beta)
-    const int j = wave;
-    if (j < kTiles) {
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            if (i >= j) z[i] = block_columns(low, i, j, c, g);
+    for (int j = 0; j < kValEach; ++j) {
+        const int i = tid + 256 * j, t = i / 8, piece = i % 8;
+        v[j] = load_eight<T>(vr, 8 * piece < task.cols ? (t * (int)a.ldv + 8 * piece) * (int)sizeof(T) : 0x7fffff00);
+    }
+    if (wave == 0) {
+        float hi, lo, since, rest;
+        decays<C>(gate_in, g, hi, lo, since, rest);
+        if (lane < C) gh[lane] = hi, gl[lane] = lo, to.gates[lane] = since, to.gates[C + lane] = rest, to.gates[2 * C + lane] = beta_in;
+    }
 #pragma unroll
-            for (int k = 0; k < i; ++k)
-                if (k >= j) ab[i][k] = -block_rows(low, i, k, c, g) * *reinterpret_cast<const f32x4 *>(bt + 16 * k + 4 * g);
-        }
+    for (int j = 0; j < kTokEach; ++j) {
+        const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
+        if (kTok % 256 != 0 && i >= kTok) break;
+        park_eight<T>(to.k + mat_at<D>(t, piece), C * D, kq[j][0]);
+        park_eight<T>(to.q + mat_at<D>(t, piece), C * D, kq[j][1]);
+    }
+#pragma unroll
+    for (int j = 0; j < kValEach; ++j) {
+        const int i = tid + 256 * j;
+        park_eight<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
     }
     __syncthreads();
-    if (j < kTiles) {
-#pragma unroll
-        for (int k = 0; k < kTiles; ++k) {
-            if (k < j) continue;
-            z[k] = times(block_rows(inv, k, k, c, g), finite(z[k]), f32x4{0, 0, 0, 0});
-            const f32x4 y = finite(z[k]);
-#pragma unroll
-            for (int i = k + 1; i < kTiles; ++i) z[i] = times(ab[i][k], y, z[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            if (i < j) continue;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * i + 4 * g + r;
-                zOut[tri_row<C>(t, j / 2) * 32 + (16 * j + c) % 32] = z[i][r];
-                if (i == j && i % 2 == 0) zOut[tri_row<C>(t, j / 2) * 32 + 16 + c] = 0.0f;
-            }
-        }
-    }
+    float *low = reinterpret_cast<float *>(to.z), *inv = reinterpret_cast<float *>(to.m);
+    const LowTiles<C> tiles(wave);
+    f32x4 M[LowTiles<C>::kEach], z[C / 16];
+    masked_products<T, D, false>(to.k, to.q, gh, gl, low, tiles, M, c, g);
+    __syncthreads();
+    solve<C>(low, inv, to.gates + 2 * C, wave, c, g, z);
+    __syncthreads();                                         // both have been read
+    const auto put = [&](int matrix, int row, int column, float x) {
+        const float pair[4] = {x, 0.0f, 0.0f, 0.0f};
+        const Split3 p = split3(pair);
+        uint16_t *m = (matrix ? to.m : to.z) + mat_at<32>(row, column / 8) + column % 8;
+        m[0] = (uint16_t)p.h[0], m[Ch::kTri] = (uint16_t)p.m[0], m[2 * Ch::kTri] = (uint16_t)p.l[0];
+    };
+    put_out_m<C>(tiles, M, c, g, put);
+    put_out_z<C>(wave, z, c, g, put);
 }
 
 // What only leads to outputs in bf16 takes two parts a value (2^-16): Q S and M beta u.  The state's way takes three.
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
 // depends on a branch.
-// kOne: sequences of one chunk at most.  There is nothing to fetch ahead, so the working waves fetch it themselves, and two
-// workgroups of half the threads and LDS share a compute unit (64 x 33 tokens, 8 heads of 64 bf16: 11 us instead of 15).
-template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __global__ __launch_bounds__(kOne ? 256 : 512) void delta_fwd_kernel(const DeltaArgs a) {
+// kOne: sequences of one chunk at most.  There is nothing to fetch ahead, and no other launch to wait for: the working waves form the
+// chunk's matrices themselves, two workgroups a compute unit (64 x 33 tokens, 8 heads of 64 bf16: @ONE@ us instead of 27).
+template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __global__ __launch_bounds__(kOne ? 256 : 512, 2) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
     constexpr bool kOutputs = kKind == kWhole;
@@ -206,7 +309,8 @@ template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __gl
     const int h = task.h, len = task.len, count = task.count, ldo = a.H * a.M;
     const size_t seq = (size_t)task.b * a.N, state = (size_t)task.bh * D * a.M, piece = (size_t)task.bh * a.pieces + task.piece;
     if constexpr (kOne) {
-        if (count > 0) fetch_only<T, D>(buffers[0], a, task, (const T *)a.v, a.ldv, tid);
+        __shared__ alignas(16) float gh[C], gl[C];
+        if (count > 0) only_chunk<T, D>(buffers[0], gh, gl, a, task, tid);
     } else if (wave >= 4) {
         fetch_chunks<T, D, !kOutputs, false>(buffers, a, task, (const T *)a.v, a.ldv, tid - 256);
         return;
@@ -522,6 +626,11 @@ void launch_join(const DeltaArgs &a, int dtype, bool back, hipStream_t s) {
 }
 
 hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
+    if (a.K == 1 && a.state == nullptr && a.M <= 2 * kCols) {      // every 64 columns form the matrices again
+#define LA_ONE(T, D) delta_fwd_kernel<T, D, kWhole, false, true><<<task_grid(a, kWhole), 256, 0, s>>>(a)
+        LA_BY_WIDTH(LA_ONE)
+        return hipGetLastError();
+    }
     const unsigned units = (unsigned)((long)a.B * a.H * a.K);
 #define LA_LOCAL(T, D) delta_local_kernel<T, D><<<units, 256, 0, s>>>(a)
     LA_BY_WIDTH(LA_LOCAL)
@@ -529,11 +638,6 @@ hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
 #define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<task_grid(a, kTransitions), 512, 0, s>>>(a)
         LA_BY_WIDTH(LA_PIECES)
         if (a.pieces > 2) launch_join(a, dtype, false, s);
-    }
-    if (a.K == 1 && a.state == nullptr) {
-#define LA_ONE(T, D) delta_fwd_kernel<T, D, kWhole, false, true><<<task_grid(a, kWhole), 256, 0, s>>>(a)
-        LA_BY_WIDTH(LA_ONE)
-        return hipGetLastError();
     }
 #define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, kWhole, true><<<task_grid(a, kWhole), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, kWhole, false><<<task_grid(a, kWhole), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_PASS)
