@@ -362,6 +362,12 @@ template <typename T, int D, bool kLean, bool kBack> __device__ __forceinline__ 
         __syncthreads();
     }
 }
+// A task's first chunk, by 256 threads that all work on it behind the next barrier
+template <typename T, int D> __device__ __forceinline__ void fetch_only(Chunked<T, D> &to, const DeltaArgs &a, const Task &task, const T *values, long ldv, int tid) {
+    Fetch<T, D, false> f;
+    f.load(a, (long)task.bh * a.K, (size_t)task.b * a.N, task.len, task.h / (a.H / a.Hk), task.h, values + (size_t)task.h * a.M + task.m0, ldv, task.cols, tid);
+    f.park(to, tid);
+}
 // The loads of a state before the first chunk: waited for here, so that the loop need not wait for them with everything else.
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 // Values in LDS, of P parts: rows row0 .. + 3 of the lane's group, column of this lane, and their sum in fp32.

@@ -296,19 +296,24 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
 // depends on a branch.
-// kOne: sequences of one chunk at most.  There is nothing to fetch ahead, and no other launch to wait for: the working waves form the
-// chunk's matrices themselves, two workgroups a compute unit (64 x 33 tokens, 8 heads of 64 bf16: @ONE@ us instead of 27).
-template <typename T, int D, PassKind kKind, bool kKeep, bool kOne = false> __global__ __launch_bounds__(kOne ? 256 : 512, 2) void delta_fwd_kernel(const DeltaArgs a) {
+// Sequences of one chunk at most have nothing to fetch ahead: the working waves fetch it themselves (kAlone), two workgroups of half
+// the threads and LDS a compute unit, or form its matrices too (kAll), with no launch to wait for.  64 x 33 tokens, 8 heads of 64 bf16:
+// 26.5 us as a pass, 18.8 alone, 15.6 all in one.  Every 64 columns form the matrices again: with two such blocks no slower (1024 heads
+// of 64 tokens and 128 x 128: 80 and 77 us), with four (64 x 256) 90 us alone and 122 as a pass.
+enum OneChunk { kPass, kAlone, kAll };
+template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> __global__ __launch_bounds__(kHow != kPass ? 256 : 512, 2) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
-    constexpr bool kOutputs = kKind == kWhole;
+    constexpr bool kOutputs = kKind == kWhole, kOne = kHow != kPass;
     __shared__ Chunked<T, D> buffers[kOne ? 1 : 2];
     Task task;
     if (!task_of<kKind, false>(a, C, D, task)) return;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, m = task.m0 + wave * 16 + c;
     const int h = task.h, len = task.len, count = task.count, ldo = a.H * a.M;
     const size_t seq = (size_t)task.b * a.N, state = (size_t)task.bh * D * a.M, piece = (size_t)task.bh * a.pieces + task.piece;
-    if constexpr (kOne) {
+    if constexpr (kHow == kAlone) {
+        if (count > 0) fetch_only<T, D>(buffers[0], a, task, (const T *)a.v, a.ldv, tid);
+    } else if constexpr (kHow == kAll) {
         __shared__ alignas(16) float gh[C], gl[C];
         if (count > 0) only_chunk<T, D>(buffers[0], gh, gl, a, task, tid);
     } else if (wave >= 4) {
@@ -626,9 +631,10 @@ void launch_join(const DeltaArgs &a, int dtype, bool back, hipStream_t s) {
 }
 
 hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
-    if (a.K == 1 && a.state == nullptr && a.M <= 2 * kCols) {      // every 64 columns form the matrices again
-#define LA_ONE(T, D) delta_fwd_kernel<T, D, kWhole, false, true><<<task_grid(a, kWhole), 256, 0, s>>>(a)
-        LA_BY_WIDTH(LA_ONE)
+    const bool one = a.K == 1 && a.state == nullptr;
+    if (one && a.M <= 2 * kCols) {
+#define LA_ALL(T, D) delta_fwd_kernel<T, D, kWhole, false, kAll><<<task_grid(a, kWhole), 256, 0, s>>>(a)
+        LA_BY_WIDTH(LA_ALL)
         return hipGetLastError();
     }
     const unsigned units = (unsigned)((long)a.B * a.H * a.K);
@@ -638,6 +644,11 @@ hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
 #define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<task_grid(a, kTransitions), 512, 0, s>>>(a)
         LA_BY_WIDTH(LA_PIECES)
         if (a.pieces > 2) launch_join(a, dtype, false, s);
+    }
+    if (one) {
+#define LA_ALONE(T, D) delta_fwd_kernel<T, D, kWhole, false, kAlone><<<task_grid(a, kWhole), 256, 0, s>>>(a)
+        LA_BY_WIDTH(LA_ALONE)
+        return hipGetLastError();
     }
 #define LA_PASS(T, D) a.state != nullptr ? delta_fwd_kernel<T, D, kWhole, true><<<task_grid(a, kWhole), 512, 0, s>>>(a) : delta_fwd_kernel<T, D, kWhole, false><<<task_grid(a, kWhole), 512, 0, s>>>(a)
     LA_BY_WIDTH(LA_PASS)
