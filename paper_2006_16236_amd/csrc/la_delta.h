@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "la_delta_cut.h"
 #include "la_mixer.h"
 
 namespace la {
@@ -275,13 +276,13 @@ template <typename T> __device__ __forceinline__ void store_value(Range r, int b
 // A chunk in LDS, and on its way there: K, Q, a workgroup's columns of V (or dO), the chunk-local matrices, the factors of the
 // decay and beta.  Four waves of a workgroup do nothing else: they cut the next chunk's values into parts and write them to the
 // other of two buffers while the four others work, one barrier a chunk, and have the one after that on its way from memory.
-template <typename T, int D> struct Chunked {
+// kLean: without Q and M, what a pass for states alone needs.
+template <typename T, int D, bool kLean = false> struct Chunked {
     using Ch = Chunk<T>;
     static constexpr int kTok = Ch::P * Ch::C * D, kVal = Ch::P * Ch::C * kCols, kTri = 3 * Ch::kTri;
-    alignas(16) uint16_t k[kTok], q[kTok], v[kVal], z[kTri], m[kTri];
+    alignas(16) uint16_t k[kTok], q[kLean ? 8 : kTok], v[kVal], z[kTri], m[kLean ? 8 : kTri];
     alignas(16) float gates[3 * Ch::C];
 };
-// kLean: without Q, M (and V where no columns are asked for): what a pass for states alone needs
 template <typename T, int D, bool kLean> struct Fetch {
     using Ch = Chunk<T>;
     static constexpr int C = Ch::C, kTok = C * D / 8, kTokEach = (kTok + 255) / 256, kVal = C * kCols / 8, kValEach = (kVal + 255) / 256;
@@ -316,7 +317,7 @@ template <typename T, int D, bool kLean> struct Fetch {
         gate = a.gate[unit * 4 * C + tid % (2 * C)];
         beta = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(br, tid * a.H * 4, 0, 0));
     }
-    __device__ __forceinline__ void park(Chunked<T, D> &to, int tid) const {
+    __device__ __forceinline__ void park(Chunked<T, D, kLean> &to, int tid) const {
 #pragma unroll
         for (int j = 0; j < kTokEach; ++j) {
             const int i = tid + 256 * j, t = i / (D / 8), piece = i % (D / 8);
@@ -341,7 +342,7 @@ template <typename T, int D, bool kLean> struct Fetch {
 };
 // The fetching waves of a task, its chunks forwards or backwards.  The others meet the same barriers: one before their first
 // chunk, and one behind each.
-template <typename T, int D, bool kLean, bool kBack> __device__ __forceinline__ void fetch_chunks(Chunked<T, D> (&to)[2], const DeltaArgs &a, const Task &task, const T *values,
+template <typename T, int D, bool kLean, bool kBack> __device__ __forceinline__ void fetch_chunks(Chunked<T, D, kLean> (&to)[2], const DeltaArgs &a, const Task &task, const T *values,
                                                                                                   long ldv, int tid) {
     constexpr int C = Chunk<T>::C;
     Fetch<T, D, kLean> f;

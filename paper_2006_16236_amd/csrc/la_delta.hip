@@ -301,11 +301,11 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
 // 26.5 us as a pass, 18.8 alone, 15.6 all in one.  Every 64 columns form the matrices again: with two such blocks no slower (1024 heads
 // of 64 tokens and 128 x 128: 80 and 77 us), with four (64 x 256) 90 us alone and 122 as a pass.
 enum OneChunk { kPass, kAlone, kAll };
-template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> __global__ __launch_bounds__(kHow != kPass ? 256 : 512, 2) void delta_fwd_kernel(const DeltaArgs a) {
+template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> __global__ __launch_bounds__(kHow != kPass ? 256 : 512, kKind == kTransitions && two_lean(sizeof(T), D) ? 4 : 2) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
     constexpr bool kOutputs = kKind == kWhole, kOne = kHow != kPass;
-    __shared__ Chunked<T, D> buffers[kOne ? 1 : 2];
+    __shared__ Chunked<T, D, !kOutputs> buffers[kOne ? 1 : 2];
     Task task;
     if (!task_of<kKind, false>(a, C, D, task)) return;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), c = lane % 16, g = lane / 16, m = task.m0 + wave * 16 + c;
@@ -346,7 +346,7 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
         const long unit = (long)task.bh * a.K + chunk;
         const size_t row0 = seq + (size_t)chunk * C;
         const int left = len - chunk * C;
-        const Chunked<T, D> &in = buffers[kOne ? 0 : i & 1];
+        const Chunked<T, D, !kOutputs> &in = buffers[kOne ? 0 : i & 1];
         const auto gate4 = [&](int which, int t) { return *reinterpret_cast<const f32x4 *>(in.gates + which * C + paired(t, 4 * g)); };
         const auto rows = [&](const uint16_t *mat, int s, Parts<P> (&f)[kTiles]) {
 #pragma unroll
@@ -641,7 +641,11 @@ hipError_t launch_delta_fwd(const DeltaArgs &a, int dtype, hipStream_t s) {
 #define LA_LOCAL(T, D) delta_local_kernel<T, D><<<units, 256, 0, s>>>(a)
     LA_BY_WIDTH(LA_LOCAL)
     if (a.pieces > 1) {
-#define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<task_grid(a, kTransitions), 512, 0, s>>>(a)
+        // where there is a compute unit for each workgroup, LDS that nobody uses keeps two from sharing one (5 x 1531 tokens, 6 heads of
+        // 64 x 80 fp32, 240 workgroups: the call 65 us instead of 71)
+        const long work = (long)a.B * a.H * ((a.M + kCols - 1) / kCols * (a.pieces - 1) + (a.D + kCols - 1) / kCols * (a.pieces - 2));
+        const unsigned grid = task_grid(a, kTransitions), spare = work <= 256 ? 34 * 1024 : 0;
+#define LA_PIECES(T, D) delta_fwd_kernel<T, D, kTransitions, false><<<grid, 512, spare, s>>>(a)
         LA_BY_WIDTH(LA_PIECES)
         if (a.pieces > 2) launch_join(a, dtype, false, s);
     }

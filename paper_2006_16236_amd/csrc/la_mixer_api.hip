@@ -63,7 +63,7 @@ struct Delta {
         gate = units * 4 * C * sizeof(float);
         rows = units * C * M * sizeof(float);
         state = units * D * M * sizeof(float);
-        const la::DeltaCut cut = la::delta_cut_of((long)B * H, D, M, a.K);
+        const la::DeltaCut cut = la::delta_cut_of((long)B * H, D, M, a.K, esize_of(t));
         a.pieces = cut.pieces, a.length = cut.length;
         const size_t cuts = cut.pieces > 1 ? (size_t)B * H * cut.pieces : 0;
         pieces = cuts * D * M * sizeof(float), transitions = cuts * D * D * sizeof(float);
