@@ -5,6 +5,8 @@
 // part and the four that go with them of the second, or eight neighbours.  Sums over a head are sums over G lanes.
 // A wave takes the heads of one token 64 / G at a time: its lanes' four angles are then formed once per token, and the
 // queries and keys of a token are one list of H + Hk heads.
+// Memory bounds both directions: 8 x 2048 tokens, 16 + 16 heads of 128 bf16, forward 50 us (5.3 TB/s), backward 85 (4.7 TB/s); one
+// token of 64 sequences, 8 + 8 heads of 64, is 4.5 us, the launch and two trips to memory.
 #include <hip/hip_runtime.h>
 
 #include "la_mixer.h"

@@ -48,7 +48,7 @@ def test_the_workspaces_have_room_for_the_pieces(cuts):
     lib = binding.raw()
     up = lambda n: -(-n // 256) * 256
     rng = random.Random(6)
-    for code, C, tri in ((0, 32, 1024), (1, 64, 3072)):
+    for code, C, tri in ((0, 32, 32 * 32), (1, 64, 96 * 32)):
         some = [(rng.randint(1, 5), rng.randint(1, 9), rng.choice((32, 64, 128)), 16 * rng.randint(1, 12), int(2 ** rng.uniform(0, 15))) for _ in range(300)]
         for (B, H, D, M, N), (pieces, _) in zip(some, cuts([(B * H, D, M, -(-N // C)) for B, H, D, M, N in some], 2 if code else 4)):
             units, cut = B * H * -(-N // C), B * H * pieces if pieces > 1 else 0
