@@ -183,6 +183,13 @@ def test_pieces_of_sequences_of_different_lengths(D_, M_, dtype):
     Case(D_, dtype, 5, 1100, 1, 1, D_, M_, [1100, 700, 150, 0, 64]).check()
 
 
+@pytest.mark.parametrize("D_,M_,dtype", [(64, 64, "f32"), (32, 32, "bf16")])
+def test_more_pieces_than_compute_units(D_, M_, dtype):
+    """24 heads of 32 chunks: eight pieces each, whose transitions are 312 workgroups."""
+    n = 1024 if dtype == "f32" else 2048
+    Case(D_ + 1, dtype, 3, n - 1, 8, 4, D_, M_, [n - 1, 7, n // 2]).check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_sequence_of_a_batch_alone_is_the_same_within_the_bounds(dtype):
     """Alone it goes in pieces, beside 63 others it does not."""
