@@ -22,10 +22,9 @@ __device__ __forceinline__ int paired(int tile, int i) { return 32 * (tile >> 1)
 template <int P> struct Parts {
     bf16x8_t p[P];
 };
-// kLast = 1: down to 2^-8 only, for values that are rounded to bf16 next
-template <int kLast = 2, int PA, int PB> __device__ __forceinline__ f32x4 product(const Parts<PA> &a, const Parts<PB> &b, f32x4 acc) {
+template <int PA, int PB> __device__ __forceinline__ f32x4 product(const Parts<PA> &a, const Parts<PB> &b, f32x4 acc) {
 #pragma unroll
-    for (int s = kLast; s >= 0; --s)                          // the small part products first
+    for (int s = 2; s >= 0; --s)                              // the small part products first
 #pragma unroll
         for (int i = 0; i <= s; ++i)
             if (i < PA && s - i < PB) acc = mfma32_bf16(a.p[i], b.p[s - i], acc);
@@ -37,9 +36,9 @@ __device__ __forceinline__ Parts<3> cut(f32x4 lo, f32x4 hi) {
     return Parts<3>{{cat_parts(a.h, b.h), cat_parts(a.m, b.m), cat_parts(a.l, b.l)}};
 }
 // N products with one right operand, a part product of all of them at a time: what follows on each other goes to other results
-template <int kLast = 2, int N, int PA, int PB> __device__ __forceinline__ void products(const Parts<PA> (&a)[N], const Parts<PB> &b, f32x4 (&acc)[N]) {
+template <int N, int PA, int PB> __device__ __forceinline__ void products(const Parts<PA> (&a)[N], const Parts<PB> &b, f32x4 (&acc)[N]) {
 #pragma unroll
-    for (int s = kLast; s >= 0; --s)
+    for (int s = 2; s >= 0; --s)
 #pragma unroll
         for (int i = 0; i <= s; ++i)
             if (i < PA && s - i < PB) {
@@ -48,11 +47,11 @@ template <int kLast = 2, int N, int PA, int PB> __device__ __forceinline__ void 
             }
 }
 // acc[t] += tri[t][s] b[s] over the 32 x 32 blocks on and below the diagonal
-template <int kLast, int N, int S, int PA, int PB> __device__ __forceinline__ void lower_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
+template <int N, int S, int PA, int PB> __device__ __forceinline__ void lower_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int k = kLast; k >= 0; --k)
+        for (int k = 2; k >= 0; --k)
 #pragma unroll
             for (int i = 0; i <= k; ++i)
                 if (i < PA && k - i < PB) {
@@ -61,11 +60,11 @@ template <int kLast, int N, int S, int PA, int PB> __device__ __forceinline__ vo
                 }
 }
 // the same with the transposed matrix: acc[t] += tri[s][t]^T b[s], blocks s >= t / 2 of block column t / 2
-template <int kLast, int N, int S, int PA, int PB> __device__ __forceinline__ void upper_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
+template <int N, int S, int PA, int PB> __device__ __forceinline__ void upper_products(const Parts<PA> (&tri)[N][S], const Parts<PB> (&b)[S], f32x4 (&acc)[N]) {
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int k = kLast; k >= 0; --k)
+        for (int k = 2; k >= 0; --k)
 #pragma unroll
             for (int i = 0; i <= k; ++i)
                 if (i < PA && k - i < PB) {
@@ -87,21 +86,6 @@ template <int D, int N> __device__ __forceinline__ void side_by_side() {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
         }
-}
-template <int P> __device__ __forceinline__ Parts<P> cut_to(f32x4 lo, f32x4 hi) {
-    if constexpr (P == 3) {
-        return cut(lo, hi);
-    } else {
-        const float x[4] = {lo[0], lo[1], lo[2], lo[3]}, y[4] = {hi[0], hi[1], hi[2], hi[3]};
-        const Split2 a = split2(x), b = split2(y);
-        return Parts<2>{{cat_parts(a.h, b.h), cat_parts(a.m, b.m)}};
-    }
-}
-template <int P> __device__ __forceinline__ Parts<P> first(const Parts<3> &x) {
-    Parts<P> y;
-#pragma unroll
-    for (int i = 0; i < P; ++i) y.p[i] = x.p[i];
-    return y;
 }
 // A value that a later token of the chunk may have spoiled: its products with masked zeros have to be zeros.
 __device__ __forceinline__ f32x4 finite(f32x4 v) {

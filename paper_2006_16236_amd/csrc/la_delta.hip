@@ -292,7 +292,8 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
     put_out_z<C>(wave, z, c, g, put);
 }
 
-// What only leads to outputs in bf16 takes two parts a value (2^-16): Q S and M beta u.  The state's way takes three.
+// All products take three parts a value, also Q S and M beta u for outputs in bf16: they may cancel, and two parts (2^-16) of a state of 2^17
+// were up to 1 off (8 x 2048 x 16 heads of 128 bf16, training step: 733 -> 741 us, one prompt of 32768 tokens 654 -> 677).
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
 // the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
 // depends on a branch.  Of 128 x 128 bf16 a chunk is 180 matrix instructions of 16 cycles, some 450 vector ones of 4, and waits: 3.0 us;
@@ -305,7 +306,7 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
 enum OneChunk { kPass, kAlone, kAll };
 template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> __global__ __launch_bounds__(kHow != kPass ? 256 : 512, kKind == kTransitions && two_lean(sizeof(T), D) ? 4 : 2) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
-    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kOut = P == 1 ? 2 : 3, kSteps = D / 32;
+    constexpr int C = Ch::C, P = Ch::P, kTiles = Ch::kTiles, kBlocks = Ch::kBlocks, kSteps = D / 32;
     constexpr bool kOutputs = kKind == kWhole, kOne = kHow != kPass;
     __shared__ Chunked<T, D, !kOutputs> buffers[kOne ? 1 : 2];
     Task task;
@@ -387,9 +388,9 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 if (s + 1 < kSteps) rows(in.q, s + 1, f[(kSteps + s + 1) % 2]);
-                products(f[(kSteps + s) % 2], first<kOut>(sp[s]), qs);
+                products(f[(kSteps + s) % 2], sp[s], qs);
             }
-            side_by_side<D, kSteps * kTiles * (P == 1 ? 2 : 6)>();
+            side_by_side<D, kSteps * kTiles * (P == 1 ? 3 : 6)>();
         }
         in_this_order<D>();
         // ... and of what the chunk's earlier tokens write
@@ -399,16 +400,15 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
             for (int t = 2 * i; t < kTiles; ++t) zf[t][i] = row_operand<32, 3>(in.z, Ch::kTri, tri_row<C>(paired(t, c), i), g);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) ks[t] = f32x4{0, 0, 0, 0};
-        lower_products<2>(zf, x, ks);
+        lower_products(zf, x, ks);
         in_this_order<D>();
-        Parts<kOut> mf[kTiles][kBlocks], u[kBlocks];
+        Parts<3> mf[kTiles][kBlocks], u[kBlocks];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             qs[t] *= since[t];
             if constexpr (kOutputs)
 #pragma unroll
-                for (int i = 0; i <= t / 2; ++i) mf[t][i] = row_operand<32, kOut>(in.m, Ch::kTri, tri_row<C>(paired(t, c), i), g);
-            since[t] = gate4(1, t);
+                for (int i = 0; i <= t / 2; ++i) mf[t][i] = row_operand<32, 3>(in.m, Ch::kTri, tri_row<C>(paired(t, c), i), g);
         }
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) rest[t] -= ks[t];
@@ -421,7 +421,7 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
         for (int t = 0; t < kTiles; ++t) rest[t] = finite(strength[t] * rest[t]);
         if constexpr (kOutputs)
 #pragma unroll
-            for (int s = 0; s < kBlocks; ++s) u[s] = cut_to<kOut>(rest[2 * s], rest[2 * s + 1]);
+            for (int s = 0; s < kBlocks; ++s) u[s] = cut(rest[2 * s], rest[2 * s + 1]);
         constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;      // tiles of the state at a time
         Parts<P> kt[2][kGroup];
         const auto columns = [&](int n) {                    // n counts (group, block)
@@ -430,13 +430,15 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
         };
         in_this_order<D>();
         columns(0);
-        if constexpr (kOutputs) lower_products<kOut - 1>(mf, u, qs);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) since[t] = gate4(1, t);
+        if constexpr (kOutputs) lower_products(mf, u, qs);
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(since[2 * s] * rest[2 * s]), finite(since[2 * s + 1] * rest[2 * s + 1]));
         const float whole = in.gates[C - 1];
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) S[t] *= whole;
-        if (kOutputs) side_by_side<D, (kTiles == 4 ? 6 : 2) * (P == 1 ? 3 : 6)>();
+        if (kOutputs) side_by_side<D, (kTiles == 4 ? 6 : 2) * 6>();
         in_this_order<D>();
         const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, left < most ? left : most, ldo, a.M);
 #pragma unroll

@@ -88,7 +88,7 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
         in_this_order<D>();
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) out[t] = column_values<kCols, P>(in.v, C * kCols, paired(t, 4 * g), wave, lane);
-        upper_products<2>(tri, o, w);
+        upper_products(tri, o, w);
         in_this_order<D>();
         // dU, and beside it the state's share of the outputs
         constexpr int kGroup = 4 < D / 16 ? 4 : D / 16, kGroups = D / 16 / kGroup;
@@ -126,7 +126,7 @@ template <typename T, int D, PassKind kKind> __global__ __launch_bounds__(512) v
             in_this_order<D>();
         }
         upper(in.z, tri);
-        upper_products<2>(tri, z, w);
+        upper_products(tri, z, w);
         columns(in.k, 0);
         in_this_order<D>();
         const Range wr = range_of(a.write + (size_t)unit * C * a.M, C, a.M, a.M);
