@@ -493,7 +493,8 @@ int la_qk_bwd(const void *q, int ldq, const void *k, int ldk, const float *wq, c
  * g [B,N,H]: logarithm of the decay, usually <= 0, -inf forgets everything before; NULL: no decay.  beta [B,N,H].  o [B,N,H,M].
  * h0 [B,H,D,M]: the state before token 0, or NULL (zero); h1 [B,H,D,M] out, or NULL: the state behind the last token, for
  * the next call or la_delta_step.  States stay bounded while beta |k|^2 is at most 2.  Steps whose logarithms are below -1000
- * count as -1000 (nothing is left either way).
+ * count as -1000 (nothing is left either way).  What is no finite number in k, v, g, beta or h0 shows as in la_delta_step: outputs from its
+ * token on, and the state behind, are not finite in the columns that it reaches, and the others are as without it.
  * LA_DELTA_KEEP: the workspace then holds, behind the call, what la_delta_bwd starts from.
  * ws: la_delta_fwd_workspace() bytes with the same flags.  LA_ERR_SHAPE: Hk does not divide H, or B * H chunks of 64 (bf16)
  * or 32 (fp32) tokens from 2^23 on.  LA_ERR_UNSUPPORTED: D, M, or an unknown flag.

@@ -169,6 +169,27 @@ template <typename T> __device__ __forceinline__ void park_eight(uint16_t *p, in
         park_eight(p, plane, x);
     }
 }
+// Values of eight columns.  Each by itself: the remainders of a pair above multiply the other one by zero, and a value that is no finite
+// number would spoil its neighbour's column.
+template <typename T> __device__ __forceinline__ void park_columns(uint16_t *p, int plane, const Eight<T> &e) {
+    if constexpr (sizeof(T) == 2) {
+        park_eight<T>(p, plane, e);
+    } else {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = e.get(i);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            u32x4_t part;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                part[i] = round_pair(x[2 * i], x[2 * i + 1]);
+                x[2 * i] -= __uint_as_float(part[i] << 16), x[2 * i + 1] -= __uint_as_float(part[i] & 0xffff0000u);
+            }
+            *reinterpret_cast<u32x4_t *>(p + k * plane) = part;
+        }
+    }
+}
 
 // The same number, of which the compiler knows nothing: what is computed from it is computed where it is used, instead of ahead of
 // a loop for all of its phases in registers that the loop has not got.
@@ -312,7 +333,7 @@ template <typename T, int D, bool kLean> struct Fetch {
 #pragma unroll
         for (int j = 0; j < kValEach; ++j) {
             const int i = tid + 256 * j;
-            park_eight<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
+            park_columns<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kTriEach; ++j) {

@@ -272,7 +272,7 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
 #pragma unroll
     for (int j = 0; j < kValEach; ++j) {
         const int i = tid + 256 * j;
-        park_eight<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
+        park_columns<T>(to.v + mat_at<kCols>(i / 8, i % 8), C * kCols, v[j]);
     }
     __syncthreads();
     float *low = reinterpret_cast<float *>(to.z), *inv = reinterpret_cast<float *>(to.m);
@@ -290,6 +290,23 @@ template <typename T, int D> __device__ __forceinline__ void only_chunk(Chunked<
     };
     put_out_m<C>(tiles, M, c, g, put);
     put_out_z<C>(wave, z, c, g, put);
+}
+
+// A token that writes what is no finite number spoils its column: its output, those behind it and the state are NaN, as token by token.
+// (What meets masked zeros is made finite, which would hide it.)  Here the outputs, behind a branch that is else not taken.
+template <int C, int N> __device__ __forceinline__ void spoil_outputs(const f32x4 (&written)[N], f32x4 (&out)[N], int g) {
+    int from = C;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (written[t][r] * 0.0f != 0.0f) from = min(from, paired(t, 4 * g + r));
+    from = min(from, __shfl_xor(from, 16));                  // over the lanes of a column
+    from = min(from, __shfl_xor(from, 32));
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[t][r] = paired(t, 4 * g + r) >= from ? __builtin_nanf("") : out[t][r];
 }
 
 // All products take three parts a value, also Q S and M beta u for outputs in bf16: they may cancel, and two parts (2^-16) of a state of 2^17
@@ -414,11 +431,20 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
         for (int t = 0; t < kTiles; ++t) rest[t] -= ks[t];
         if constexpr (kKeep) {
             const Range r = range_of(a.miss + (size_t)unit * C * a.M, C, a.M, a.M);
+            const int l = here(lane);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) store_tile<float>(r, paired(t, 4 * g), m - c, a.M, rest[t], lane);
+            for (int t = 0; t < kTiles; ++t) store_tile<float>(r, paired(t, 4 * (l / 16)), task.m0 + wave * 16, a.M, rest[t], l);
         }
+        float spoiled = 0.0f;                                // NaN where a token writes what is no finite number
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) rest[t] = finite(strength[t] * rest[t]);
+        for (int t = 0; t < kTiles; ++t) {
+            rest[t] *= strength[t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) spoiled = fmaf(rest[t][r], 0.0f, spoiled);
+        }
+        if (kOutputs && __any(spoiled != 0.0f)) spoil_outputs<C>(rest, qs, g);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) rest[t] = finite(rest[t]);
         if constexpr (kOutputs)
 #pragma unroll
             for (int s = 0; s < kBlocks; ++s) u[s] = cut(rest[2 * s], rest[2 * s + 1]);
@@ -436,8 +462,11 @@ template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> 
 #pragma unroll
         for (int s = 0; s < kBlocks; ++s) x[s] = cut(finite(since[2 * s] * rest[2 * s]), finite(since[2 * s + 1] * rest[2 * s + 1]));
         const float whole = in.gates[C - 1];
+        spoiled = add_halves(add_rows(spoiled));             // of the lanes of a column
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) S[t] *= whole;
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = fmaf(S[t][r], whole, spoiled);
         if (kOutputs) side_by_side<D, (kTiles == 4 ? 6 : 2) * 6>();
         in_this_order<D>();
         const Range r = range_of((T *)a.o + row0 * ldo + (size_t)h * a.M, left < most ? left : most, ldo, a.M);

@@ -51,3 +51,57 @@ def test_outputs_that_cancel(way, dtype):
     for t in range(N):
         want[:, :, t % D] = host(v[:, t])
     assert np.abs(host(h1) - want).max() <= room
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("way", WAYS, ids=lambda w: "x".join(map(str, w)))
+def test_what_is_no_finite_number_shows(way, dtype):
+    """In v of one column, in beta of one head, in a key, in a state handed in: outputs from its token on and the state behind have no finite
+    value where it reaches, as token by token; all others are as without it."""
+    B, N, H, Hk, D, M, keep = way
+    c = Case(21, dtype, *way[:6])
+    assert pieces(way[:6], dtype, keep) == (N == 1100)
+    per, b, col = H // Hk, B - 1, M - 3
+    clean = c.run(back=False)
+    if keep:
+        x, more = c.inputs()
+        out, _, _ = c.outputs()
+        la.la_delta_fwd(*x, **out, **more, keep=True)
+        assert all(torch.equal(out[n], clean[n]) for n in out)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        for at in sorted({0, 1, N // 2, N - 1}):
+            for what in ("v", "beta", "k", "h0"):
+                x, more = c.inputs()
+                hit = torch.zeros(B, N, H, M, dtype=torch.bool, device=DEV)
+                last = torch.zeros(B, H, D, M, dtype=torch.bool, device=DEV)
+                if what == "v":
+                    x[2][b, at, H - 1, col] = bad
+                    hit[b, at:, H - 1, col] = last[b, H - 1, :, col] = True
+                elif what == "beta":
+                    x[4][b, at, H - 1] = bad
+                    hit[b, at:, H - 1] = last[b, H - 1] = True
+                elif what == "k":
+                    x[1][b, at, Hk - 1, D // 2] = bad
+                    hit[b, at:, H - per:] = last[b, H - per:] = True
+                else:
+                    more["h0"] = more["h0"].clone()
+                    more["h0"][b, H - 1, D - 1, col] = bad
+                    hit[b, :, H - 1, col] = last[b, H - 1, :, col] = True
+                out, _, _ = c.outputs()
+                la.la_delta_fwd(*x, **out, **more, keep=keep)
+                where = (what, bad, at)
+                assert not out["o"][hit].isfinite().any() and not out["h1"][last].isfinite().any(), where
+                assert torch.equal(out["o"][~hit], clean["o"][~hit]) and torch.equal(out["h1"][~last], clean["h1"][~last]), where
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_token_by_itself_shows_it_too(dtype):
+    c = Case(22, dtype, 2, 1, 2, 1, 64, 48)
+    for bad in (float("nan"), float("inf")):
+        for what in range(1, 5):
+            x, _ = c.inputs()
+            x[what].view(-1)[-1] = bad if what != 3 else float("nan")
+            h, o = c.d.dev(c.h0, True), c.d.empty((2, 2, 48))
+            la.la_delta_step(*(t[:, 0].contiguous() for t in x), h, o)
+            hit = slice(47, 48) if what == 2 else slice(0, 48)
+            assert not o[1, 1, hit].isfinite().any() and not h[1, 1, :, hit].isfinite().any(), (bad, what)
