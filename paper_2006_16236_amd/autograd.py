@@ -248,7 +248,7 @@ class _QkNorm(torch.autograd.Function):
         if k is not None:
             dyk = torch.zeros(k.shape, dtype=k.dtype, device=k.device) if dyk is None else _dense(dyk)
             dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        dwq, dwk = _wanted(need[2], wq), _wanted(need[3], wk)
+        dwq, dwk = _wanted(need[2], wq), _wanted(need[3] and k is not None, wk)
         _l.la_qk_bwd(q, dyq, dq, k=k, dyk=dyk, dk=dk, wq=wq, wk=wk, freq=freq, pos=pos, lengths=lengths, dwq=dwq, dwk=dwk, **ctx.how)
         return dq, dk, dwq, dwk, None, None, None, None, None, None
 
@@ -256,7 +256,7 @@ class _QkNorm(torch.autograd.Function):
 def qk_norm(q, k=None, wq=None, wk=None, freq=None, pos=None, lengths=None, norm="rms", adjacent: bool = False, eps: float = 1e-6):
     """(q, k) with each head of q [B, N, H, D] and k [B, N, Hk, D] normed ("rms", "l2" for unit length, or None) and weighted with wq, wk
     [D] fp32, and its first 2 len(freq) elements turned by pos * freq: pairs i and i + len(freq), or neighbours.  pos [B, N] int32 (None:
-    0 .. N - 1), lengths [B] int32: rows behind it are zero.  Without k, q alone.  Differentiable in q, k, wq, wk."""
+    0 .. N - 1), lengths [B] int32: rows behind it are zero.  Without k, q alone; wk then takes no part.  Differentiable in q, k, wq, wk."""
     return _QkNorm.apply(q, k, wq, wk, freq, pos, lengths, norm, bool(adjacent), float(eps))
 
 
