@@ -147,13 +147,6 @@ template <typename T> struct Eight {
         else return __uint_as_float(w[i]);
     }
 };
-template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *p, bool live) {      // at any address
-    Eight<T> e;
-#pragma unroll
-    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) e.w[i] = 0;
-    if (live) __builtin_memcpy(e.w, p, sizeof(e.w));
-    return e;
-}
 __device__ __forceinline__ void park_eight(uint16_t *p, int plane, const float (&x)[8]) {
     const Parts<3> c = cut(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
 #pragma unroll
@@ -272,10 +265,6 @@ template <typename T> __device__ __forceinline__ Eight<T> load_eight(Range r, in
         for (int i = 0; i < 4; ++i) e.w[4 + i] = hi[i];
     }
     return e;
-}
-template <typename T> __device__ __forceinline__ void store_value(Range r, int byte, float v) {
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16_bits(v), r, byte, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, byte, 0, 0);
 }
 
 // A chunk in LDS, and on its way there: K, Q, a workgroup's columns of V (or dO), the chunk-local matrices, the factors of the
