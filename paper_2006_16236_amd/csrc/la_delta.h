@@ -74,7 +74,7 @@ template <int N, int S, int PA, int PB> __device__ __forceinline__ void upper_pr
 }
 // What is written before this point is issued before what is written behind it: the reads of operands that a later product
 // takes stay ahead of the products before that.  In the passes (D) not for heads of 32, where the compiler has registers to spare
-// and does better alone (8 x 784 x 8 heads of 32 bf16, training step: 102 -> 97 us; heads of 64: the same within 1 %; of 128: spills).
+// and does better alone (8 x 784 x 8 heads of 32 bf16, training step: 106 -> 103 us; heads of 64: the same within 1 %; of 128: spills).
 template <int D = 128> __device__ __forceinline__ void in_this_order() {
     if constexpr (D > 32) __builtin_amdgcn_sched_barrier(0);
 }

@@ -179,8 +179,8 @@ template <int C, typename Put> __device__ __forceinline__ void put_out_z(int j, 
         }
     }
 }
-// One workgroup a unit.  Every step waits for the one before, so what counts is how many workgroups a compute unit holds: four (three
-// of 128 columns).  8 x 2048 x 16 heads of 128 bf16: 63 us, 3.8 TB/s of tokens and matrices.
+// One workgroup a unit.  Every step waits for the one before, so what counts is how many workgroups a compute unit holds: three of 128
+// columns; else four in bf16, five of 64 columns and eight of 32 in fp32.  8 x 2048 x 16 heads of 128 bf16: 63 us, 3.8 TB/s of tokens and matrices.
 template <typename T, int D> __global__ __launch_bounds__(256, D == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4) void delta_local_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
     constexpr int C = Ch::C, P = Ch::P, kTokens = 2 * P * C * D * (int)sizeof(uint16_t), kTri = C * tri_stride(C) * (int)sizeof(float);
@@ -310,16 +310,17 @@ template <int C, int N> __device__ __forceinline__ void spoil_outputs(const f32x
 }
 
 // All products take three parts a value, also Q S and M beta u for outputs in bf16: they may cancel, and two parts (2^-16) of a state of 2^17
-// were up to 1 off (8 x 2048 x 16 heads of 128 bf16, training step: 733 -> 741 us, one prompt of 32768 tokens 654 -> 677).
+// were up to 1 off, where three are 2^-6 (with two, and without the test above: training step of 8 x 2048 x 16 heads of 128 bf16 733 us, now 743;
+// one prompt of 32768 tokens 650, now 673; training step of 8 x 784 x 8 heads of 32 bf16 98, now 103).
 // A chunk is one long chain of products with one working wave a SIMD, so the operands of each product are read from LDS while
-// the one before runs, products that the chain does not wait for run beside the cutting of values, and nothing in the loop
-// depends on a branch.  Of 128 x 128 bf16 a chunk is 180 matrix instructions of 16 cycles, some 450 vector ones of 4, and waits: 3.0 us;
-// 8 x 2048 x 16 heads with what the backward needs, 470 MB written: 205 us, 3.7 TB/s.  (16 columns a wave: a state of 128 rows and its parts
+// the one before runs, products that the chain does not wait for run beside the cutting of values, and the loop's one branch is
+// that of spoiled columns.  Of 128 x 128 bf16 a chunk is 216 matrix instructions of 16 cycles, some 520 vector ones of 4, and waits: 3.5 us;
+// 8 x 2048 x 16 heads with what the backward needs, 470 MB written: 228 us, 3.3 TB/s.  (16 columns a wave: a state of 128 rows and its parts
 // are 80 registers; 64 a workgroup: two buffers of a chunk are 157 KB of LDS.)
 // Sequences of one chunk at most have nothing to fetch ahead: the working waves fetch it themselves (kAlone), two workgroups of half
 // the threads and LDS a compute unit, or form its matrices too (kAll), with no launch to wait for.  64 x 33 tokens, 8 heads of 64 bf16:
-// 26.5 us as a pass, 18.8 alone, 15.6 all in one.  Every 64 columns form the matrices again: with two such blocks no slower (1024 heads
-// of 64 tokens and 128 x 128: 80 and 77 us), with four (64 x 256) 90 us alone and 122 as a pass.
+// 24.1 us as a pass, 20.0 alone, 17.1 all in one.  Every 64 columns form the matrices again: with two such blocks no slower (1024 heads
+// of 64 tokens and 128 x 128: 74 and 75 us), with four (64 x 256) 100 us, 83 alone and 118 as a pass.
 enum OneChunk { kPass, kAlone, kAll };
 template <typename T, int D, PassKind kKind, bool kKeep, OneChunk kHow = kPass> __global__ __launch_bounds__(kHow != kPass ? 256 : 512, kKind == kTransitions && two_lean(sizeof(T), D) ? 4 : 2) void delta_fwd_kernel(const DeltaArgs a) {
     using Ch = Chunk<T>;
